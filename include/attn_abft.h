@@ -332,6 +332,120 @@ const char* attn_abft_strerror(int status);
 int attn_abft_workspace_tensor(const attn_abft_config* cfg, int32_t which, size_t* offset);
 
 /* ---------------------------------------------------------------------------
+ * Attention over keys of another length (cross attention, self attention
+ * with a learned relative position bias, decoded tokens over a cache).
+ * For query i and key j of a sequence with n keys, query 0 at key position s:
+ *   S_ij = scale Q_i . K_j + bias[bucket(j - (s + i))][head]
+ *   O_i  = sum_j softmax_j(S_ij) V_j   over j < n, and j <= s + i if causal
+ * Each group of heads / kv_heads consecutive query heads shares one key head.
+ * A query without keys gets O = 0, and no gradient comes from it. K and V behind a
+ * sequence's n keys are not read, whatever they hold; a key that only the causal
+ * mask hides must be finite. These calls carry no checksums (the
+ * counterpart of ABFT_FLAG_UNPROTECTED): encode_checksums and
+ * verify_and_correct guard what they read and write while it is stored.
+ * Results do not depend on scheduling. Conventions as at the top; nothing
+ * is kept between calls, and calls that share neither workspace nor outputs
+ * may overlap.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch, q_len, k_len;  /* k_len: keys of the longest sequence; any of them
+                                   may be 0, lengths up to 2^29                   */
+  int32_t heads, kv_heads;      /* kv_heads divides heads                          */
+  int32_t head_dim;             /* 64 or 128                                       */
+  int32_t dtype;                /* ABFT_BF16 | ABFT_FP32 (every tensor; sums fp32)  */
+  int32_t causal;               /* 1: key j > query position s + i is masked       */
+  float   scale;                /* softmax scale; <= 0 -> 1/sqrt(head_dim)         */
+  int32_t buckets;              /* rows of the bias table; 0: no bias              */
+  int32_t max_distance;         /* bias only: see attn_rel_bucket                  */
+  int32_t bidirectional;
+} attn_cross_config;
+
+/* A tensor [batch, tokens, heads, head_dim]; strides in elements, the last
+ * one 1. data (device) and all strides are multiples of 16 bytes, a token
+ * stride is at most 16 MiB. Inputs may repeat memory (stride 0), outputs not.
+ * Strides of dimensions of extent 1 and tensors without elements are not
+ * looked at. */
+typedef struct {
+  const void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} attn_cross_tensor;
+
+/* Bucket of a relative position key - query. Two-sided (bidirectional = 1):
+ * buckets is even, the second half is for keys ahead (relative > 0); one-sided:
+ * keys ahead share bucket 0 with distance 0. Of a side's nb buckets, e = nb / 2
+ * (rounded down) hold one distance each, 0 .. e - 1; distance n >= e is in bucket
+ *   min(nb - 1, e + floor((nb - e) log(n / e) / log(max_distance / e))),
+ * evaluated exactly. nb >= 2, buckets <= 128, e < max_distance <= 1024.
+ * Host only. Returns the bucket or ABFT_ERR_INVALID. */
+int attn_rel_bucket(int64_t relative, int32_t buckets, int32_t max_distance,
+                    int32_t bidirectional);
+
+/* Bytes of device workspace the calls below need, the larger of forward and
+ * backward; 0 if the config is invalid. Its contents do not outlive a call. */
+size_t attn_cross_workspace_bytes(const attn_cross_config* cfg /* host */);
+
+/* Forward.
+ *   Q, O [batch, q_len, heads, head_dim], K, V [batch, k_len, kv_heads, head_dim]
+ *   bias (device) [buckets][heads] fp32, NULL when buckets == 0; an entry below
+ *     -1e30 (-INF among them) masks its bucket's pairs
+ *   k_lens (device) [batch] keys of each sequence, NULL: k_len for all; values
+ *     are taken into [0, k_len]
+ *   q_start (device) [batch] position of each sequence's query 0 among its keys
+ *     (a decoded token's is its sequence's length - 1), NULL: 0
+ *   lse (device) [batch][heads][q_len] fp32: log2 of the row's sum of
+ *     2^(S log2 e), -INF for a row without keys; what the backward takes. May be
+ *     NULL. */
+int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
+                       const attn_cross_tensor* K, const attn_cross_tensor* V, const float* bias,
+                       const int32_t* k_lens, const int32_t* q_start, const attn_cross_tensor* O,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward: dQ, dK, dV (as Q, K, V; zero behind a sequence's keys) and dbias
+ * [buckets][heads] fp32 (NULL when buckets == 0) from dO, the forward's inputs,
+ * its O and lse. */
+int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* dO,
+                        const attn_cross_tensor* Q, const attn_cross_tensor* K,
+                        const attn_cross_tensor* V, const attn_cross_tensor* O, const float* lse,
+                        const float* bias, const int32_t* k_lens, const int32_t* q_start,
+                        const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
+                        const attn_cross_tensor* dV, float* dbias, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Global norm of many gradient tensors, and clipping by it: the end of a
+ * training step, where gradients that no check has seen show up.
+ *   norm = sqrt(sum of all squares), coef = min(1, max_norm / norm),
+ *   out = coef * gradient
+ * Squares and sums are formed in 64 bits. Where an element is INF or NaN, so is
+ * the norm; the gradients are then left as they are (coef = 1) and nonfinite
+ * is the caller's cue to skip the step or to fall back to checkpoint/restore.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  const void* grad;   /* (device) numel contiguous elements                   */
+  void* out;          /* clip_gradients: result (device); grad itself, or memory
+                         that overlaps no tensor of the list                  */
+  int64_t numel;      /* may be 0 (the pointers are then not looked at)       */
+  int32_t dtype;      /* ABFT_BF16 | ABFT_FP32                                */
+  int32_t reserved;
+} abft_grad;
+
+typedef struct {
+  float norm, coef;
+  int64_t nonfinite;  /* elements that are INF or NaN                         */
+} abft_grad_stats;
+
+/* Bytes of device workspace for n tensors (0 for n < 0). */
+size_t clip_gradients_workspace_bytes(int32_t n);
+
+/* grads (host) n entries, any mix of types and sizes; stats (device, 8-byte
+ * aligned) receives norm and nonfinite (and coef: 1 from global_grad_norm).
+ * max_norm >= 0. An output that overlaps another one is ABFT_ERR_INVALID. */
+int global_grad_norm(const abft_grad* grads, int32_t n, abft_grad_stats* stats, void* workspace,
+                     size_t workspace_bytes, void* stream);
+int clip_gradients(const abft_grad* grads, int32_t n, double max_norm, abft_grad_stats* stats,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Adaptive detection frequencies (paper Sec. 4.5, Algorithm 1). Host-only
  * calls (no device memory, no stream): they choose how often each
  * protection section is checked and produce the `sections` mask of a

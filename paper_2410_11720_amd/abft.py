@@ -68,12 +68,32 @@ class FreqSection(ctypes.Structure):
                 ("cost", ctypes.c_double)]
 
 
+class CrossConfigC(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("q_len", ctypes.c_int32), ("k_len", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32),
+                ("bidirectional", ctypes.c_int32)]
+
+
+class CrossTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 REPORT_HEADER = 32  # bytes before the event array
 assert ctypes.sizeof(Event) == 40 and ctypes.sizeof(Fault) == 28
 
 _vp, _sz, _i32, _i64, _f32, _u32 = (ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32,
                                    ctypes.c_int64, ctypes.c_float, ctypes.c_uint32)
 _P = ctypes.POINTER(Config)
+_CP, _TP = ctypes.POINTER(CrossConfigC), ctypes.POINTER(CrossTensor)
 _sig = {
     "attn_abft_workspace_bytes": (_sz, [_P]),
     "attn_abft_report_bytes": (_sz, [_i32]),
@@ -100,6 +120,15 @@ _sig = {
                                                       ctypes.POINTER(FreqSection), _i32, _vp,
                                                       ctypes.c_double, _vp]),
     "attn_abft_sections_for_step": (_u32, [_vp, _i64]),
+    "attn_rel_bucket": (ctypes.c_int, [_i64, _i32, _i32, _i32]),
+    "attn_cross_workspace_bytes": (_sz, [_CP]),
+    "attn_cross_forward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _vp, _vp, _vp, _TP, _vp, _vp, _sz,
+                                          _vp]),
+    "attn_cross_backward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _TP, _TP, _vp, _vp, _vp, _vp, _TP,
+                                           _TP, _TP, _vp, _vp, _sz, _vp]),
+    "clip_gradients_workspace_bytes": (_sz, [_i32]),
+    "global_grad_norm": (ctypes.c_int, [_vp, _i32, _vp, _vp, _sz, _vp]),
+    "clip_gradients": (ctypes.c_int, [_vp, _i32, ctypes.c_double, _vp, _vp, _sz, _vp]),
     "attn_abft_forward_noalloc": (ctypes.c_int, [_P, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -402,3 +431,219 @@ class ProtectedAttention:
         return (view(q, T * 3 * H, (c.batch, S, 3 * H)),
                 view(a, c.batch * c.heads * S * S, (c.batch, c.heads, S, S)),
                 view(l, T * H, (c.batch, S, H)))
+
+
+# ---- attention over keys of another length ---------------------------------
+
+def attn_rel_bucket(relative: int, buckets: int, max_distance: int = 128,
+                    bidirectional: bool = True) -> int:
+    """Bucket of the relative position key - query (host only)."""
+    k = _lib.attn_rel_bucket(int(relative), buckets, max_distance, int(bidirectional))
+    if k < 0:
+        raise AbftError(f"attn_rel_bucket: {strerror(k)} ({k})")
+    return k
+
+
+@dataclasses.dataclass
+class CrossConfig:
+    batch: int
+    q_len: int
+    k_len: int
+    heads: int
+    head_dim: int
+    kv_heads: int = 0            # 0: one key head per query head
+    dtype: str = "bf16"          # "bf16" | "f32"
+    causal: bool = False
+    scale: float = 0.0
+    buckets: int = 0             # rows of the relative position bias table; 0: none
+    max_distance: int = 128
+    bidirectional: bool = True
+
+    def to_c(self) -> CrossConfigC:
+        return CrossConfigC(self.batch, self.q_len, self.k_len, self.heads,
+                            self.kv_heads or self.heads, self.head_dim,
+                            FP32 if self.dtype == "f32" else BF16, int(self.causal), self.scale,
+                            self.buckets, self.max_distance, int(self.bidirectional))
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+
+def attn_cross_workspace_bytes(cfg: CrossConfig) -> int:
+    c = cfg.to_c()
+    n = _lib.attn_cross_workspace_bytes(ctypes.byref(c))
+    if n == 0:
+        raise AbftError("invalid configuration")
+    return n
+
+
+class _on_device:
+    """Makes a tensor's device the current one for a call (most calls are on
+    it already)."""
+
+    def __init__(self, device):
+        self.guard = None
+        if device.index is not None and device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+class CrossAttention:
+    """Attention of q_len queries over k_len keys a sequence: owns the
+    workspace of one shape and the row statistics that the forward leaves for the
+    backward (`lse`), as ProtectedAttention does for its layer. Calls run on
+    the current stream of the tensors' device.
+
+    Q, O, dO, dQ [batch, q_len, heads, head_dim]; K, V, dK, dV [batch, k_len,
+    kv_heads, head_dim]; any strides with whole rows at multiples of 16 bytes
+    (views of packed projections, of a cache). bias, dbias [buckets, heads]
+    fp32; k_lens, q_start [batch] int32."""
+
+    def __init__(self, cfg: CrossConfig, device="cuda"):
+        self.cfg = cfg
+        self.device = torch.empty(0, device=device).device
+        self._c = cfg.to_c()
+        self.workspace = torch.empty(attn_cross_workspace_bytes(cfg), dtype=torch.uint8,
+                                     device=self.device)
+        self.lse = torch.empty((cfg.batch, cfg.heads, cfg.q_len), dtype=torch.float32,
+                               device=self.device)
+        kvh = cfg.kv_heads or cfg.heads
+        self._q_shape = (cfg.batch, cfg.q_len, cfg.heads, cfg.head_dim)
+        self._k_shape = (cfg.batch, cfg.k_len, kvh, cfg.head_dim)
+
+    def _tensor(self, t, name, shape):
+        if t.device != self.device or t.dtype != self.cfg.torch_dtype or t.shape != shape:
+            raise AbftError(f"{name}: expected {shape} {self.cfg.torch_dtype} on {self.device}, got "
+                            f"{tuple(t.shape)} {t.dtype} on {t.device}")
+        st = t.stride()
+        if st[3] != 1:
+            raise AbftError(f"{name}: the last dimension must be contiguous")
+        return CrossTensor(t.data_ptr(), st[0], st[1], st[2])
+
+    def _vector(self, t, name, shape, dtype):
+        if t is None:
+            return None
+        if t.device != self.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise AbftError(f"{name}: expected contiguous {shape} {dtype} on {self.device}, got "
+                            f"{tuple(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def _keys(self, bias, k_lens, q_start):
+        c = self.cfg
+        return (self._vector(bias, "bias", (c.buckets, c.heads), torch.float32),
+                self._vector(k_lens, "k_lens", (c.batch,), torch.int32),
+                self._vector(q_start, "q_start", (c.batch,), torch.int32))
+
+    def forward(self, Q, K, V, bias=None, k_lens=None, q_start=None, O=None):
+        if O is None:
+            O = torch.empty(self._q_shape, dtype=self.cfg.torch_dtype, device=self.device)
+        q, o = self._tensor(Q, "Q", self._q_shape), self._tensor(O, "O", self._q_shape)
+        k, v = self._tensor(K, "K", self._k_shape), self._tensor(V, "V", self._k_shape)
+        bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
+        with _on_device(self.device):
+            _check(_lib.attn_cross_forward(self._c, q, k, v, bias, k_lens, q_start, o,
+                                           self.lse.data_ptr(), self.workspace.data_ptr(),
+                                           self.workspace.numel(), _stream()),
+                   "attn_cross_forward")
+        return O
+
+    def backward(self, dO, Q, K, V, O, bias=None, k_lens=None, q_start=None, dQ=None, dK=None,
+                 dV=None, dbias=None):
+        c = self.cfg
+
+        def new(t, shape):
+            return t if t is not None else torch.empty(shape, dtype=c.torch_dtype,
+                                                       device=self.device)
+        dQ, dK, dV = new(dQ, self._q_shape), new(dK, self._k_shape), new(dV, self._k_shape)
+        if dbias is None and c.buckets:
+            dbias = torch.empty((c.buckets, c.heads), dtype=torch.float32, device=self.device)
+        qs = [self._tensor(t, n, self._q_shape) for t, n in ((dO, "dO"), (Q, "Q"), (O, "O"),
+                                                             (dQ, "dQ"))]
+        ks = [self._tensor(t, n, self._k_shape) for t, n in ((K, "K"), (V, "V"), (dK, "dK"),
+                                                             (dV, "dV"))]
+        bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
+        db = self._vector(dbias, "dbias", (c.buckets, c.heads), torch.float32)
+        with _on_device(self.device):
+            _check(_lib.attn_cross_backward(self._c, qs[0], qs[1], ks[0], ks[1], qs[2],
+                                            self.lse.data_ptr(), bias, k_lens, q_start, qs[3],
+                                            ks[2], ks[3], db, self.workspace.data_ptr(),
+                                            self.workspace.numel(), _stream()),
+                   "attn_cross_backward")
+        return dQ, dK, dV, dbias
+
+
+# ---- norm and clipping of gradients -------------------------------------------
+
+class GradStats:
+    """Views of the device statistics that global_grad_norm and clip_gradients
+    leave: `norm` and `coef` (fp32) and `nonfinite` (int64), of no dimension."""
+
+    def __init__(self, device):
+        self.raw = torch.zeros(2, dtype=torch.int64, device=device)
+        f = self.raw[:1].view(torch.float32)
+        self.norm, self.coef, self.nonfinite = f[0], f[1], self.raw[1]
+
+
+class GradientClip:
+    """Global norm of gradient tensors, and clipping by it: owns the
+    workspace for as many tensors as `grads` holds, and the statistics of the
+    last call (`stats`). Tensors are contiguous, bf16 or fp32, on one device."""
+
+    def __init__(self, grads):
+        grads = list(grads)
+        self.device = grads[0].device if grads else torch.empty(0, device="cuda").device
+        self._n = len(grads)
+        self.workspace = torch.empty(_lib.clip_gradients_workspace_bytes(self._n),
+                                     dtype=torch.uint8, device=self.device)
+        self.stats = GradStats(self.device)
+
+    def _list(self, grads, out):
+        n = len(grads)
+        if n > self._n:
+            raise AbftError(f"{n} gradients, made for {self._n}")
+        if len(out) != n:
+            raise AbftError(f"{n} gradients, {len(out)} outputs")
+        arr = (Grad * max(1, n))()
+        for i in range(n):
+            g, o = grads[i], out[i]
+            if g.dtype is torch.float32:
+                dt = FP32
+            elif g.dtype is torch.bfloat16:
+                dt = BF16
+            else:
+                raise AbftError(f"gradient {i}: {g.dtype}")
+            if g.device != self.device or not g.is_contiguous():
+                raise AbftError(f"gradient {i}: expected contiguous on {self.device}")
+            if o is not g and (o.dtype != g.dtype or o.device != g.device or
+                               o.shape != g.shape or not o.is_contiguous()):
+                raise AbftError(f"output {i}: expected contiguous, as the gradient")
+            a = arr[i]
+            a.grad, a.out, a.numel, a.dtype = g.data_ptr(), o.data_ptr(), g.numel(), dt
+        return arr, n
+
+    def norm(self, grads):
+        """Leaves the norm in `stats`, which it returns."""
+        arr, n = self._list(grads, grads)
+        with _on_device(self.device):
+            _check(_lib.global_grad_norm(arr, n, self.stats.raw.data_ptr(),
+                                         self.workspace.data_ptr(), self.workspace.numel(),
+                                         _stream()), "global_grad_norm")
+        return self.stats
+
+    def clip(self, grads, max_norm, out=None):
+        """Scales the gradients to a global norm of at most max_norm, in place
+        or into `out`; leaves norm, coef and nonfinite in `stats`."""
+        arr, n = self._list(grads, grads if out is None else out)
+        with _on_device(self.device):
+            _check(_lib.clip_gradients(arr, n, float(max_norm), self.stats.raw.data_ptr(),
+                                       self.workspace.data_ptr(), self.workspace.numel(),
+                                       _stream()), "clip_gradients")
+        return self.stats

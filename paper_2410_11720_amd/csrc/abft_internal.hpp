@@ -261,6 +261,9 @@ hipError_t lds_limit(size_t bytes) {
   return e;
 }
 
+// ABFT_OK where the current device is a gfx950 (looked up once per device).
+int check_device();
+
 // Threshold as the storage dtype represents it (round to nearest even).
 float stored_threshold(float t, int dtype);
 

@@ -34,6 +34,23 @@ float stored_threshold(float t, int dtype) {
   return r;
 }
 
+int check_device() {
+  static std::mutex mu;
+  static int cached[64];
+  static bool init[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return ABFT_ERR_HIP;
+  if (dev < 0 || dev >= 64) return ABFT_ERR_UNSUPPORTED;
+  std::lock_guard<std::mutex> lk(mu);
+  if (!init[dev]) {
+    hipDeviceProp_t p;
+    if (hipGetDeviceProperties(&p, dev) != hipSuccess) return ABFT_ERR_HIP;
+    cached[dev] = std::strncmp(p.gcnArchName, "gfx950", 6) == 0 ? ABFT_OK : ABFT_ERR_UNSUPPORTED;
+    init[dev] = true;
+  }
+  return cached[dev];
+}
+
 namespace {
 
 constexpr size_t ALIGN = 256;
@@ -238,23 +255,6 @@ int validate(const attn_abft_config* c, Dims* d) {
   if (!(c->t_near_inf >= 0.f) || !(c->t_correct >= 0.f) || !(c->e_rel >= 0.f))
     return ABFT_ERR_INVALID;
   return ABFT_OK;
-}
-
-int check_device() {
-  static std::mutex mu;
-  static int cached[64];
-  static bool init[64];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return ABFT_ERR_HIP;
-  if (dev < 0 || dev >= 64) return ABFT_ERR_UNSUPPORTED;
-  std::lock_guard<std::mutex> lk(mu);
-  if (!init[dev]) {
-    hipDeviceProp_t p;
-    if (hipGetDeviceProperties(&p, dev) != hipSuccess) return ABFT_ERR_HIP;
-    cached[dev] = std::strncmp(p.gcnArchName, "gfx950", 6) == 0 ? ABFT_OK : ABFT_ERR_UNSUPPORTED;
-    init[dev] = true;
-  }
-  return cached[dev];
 }
 
 struct Params {

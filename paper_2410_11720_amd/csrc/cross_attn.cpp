@@ -1,0 +1,268 @@
+// Host entry points of attention over keys of another length
+// (include/attn_abft.h): checks, workspace layout, choice of the form.
+#include <algorithm>
+#include <cmath>
+
+#include "cross_internal.hpp"
+
+namespace abft {
+namespace {
+
+constexpr size_t ALIGN = 256;
+constexpr int MAX_LEN = 1 << 29;             // positions and their differences fit 32 bits
+constexpr int64_t MAX_TOKEN_BYTES = 1 << 24; // a tile's rows fit the copies' 32-bit offsets
+
+size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+int es_of(const attn_cross_config* c) { return c->dtype == ABFT_FP32 ? 4 : 2; }
+
+// n^f >= e^(f - t) m^t for whole numbers, i.e. n >= e (m / e)^(t / f): exact.
+// Away from equality extended precision decides; next to it (a relative
+// distance below 1e-12, where rounding could) the prime exponents tell
+// whether both sides are equal.
+bool reaches(int n, int e, int m, int t, int f) {
+  const long double x = f * std::log((long double)n);
+  const long double y = (f - t) * std::log((long double)e) + t * std::log((long double)m);
+  if (std::fabs(x - y) > 1e-12L * (y + 1)) return x > y;
+  int a = n, b = e, c = m;
+  for (int p = 2; a > 1 || b > 1 || c > 1; ++p) {
+    int va = 0, vb = 0, vc = 0;
+    while (a % p == 0) { a /= p; ++va; }
+    while (b % p == 0) { b /= p; ++vb; }
+    while (c % p == 0) { c /= p; ++vc; }
+    if (f * va != (f - t) * vb + t * vc) return x > y;
+  }
+  return true;
+}
+
+bool make_bias(int buckets, int max_distance, int bidirectional, CrossBias* b) {
+  if (buckets > CROSS_MAX_BUCKETS || max_distance > CROSS_MAX_DISTANCE) return false;
+  if (bidirectional != 0 && bidirectional != 1) return false;
+  if (bidirectional && buckets % 2) return false;
+  b->buckets = buckets;
+  b->bidirectional = bidirectional;
+  b->side = bidirectional ? buckets / 2 : buckets;
+  if (b->side < 2) return false;
+  b->exact = b->side / 2;
+  if (max_distance <= b->exact) return false;
+  const int f = b->side - b->exact;
+  b->border[0] = uint16_t(b->exact);
+  int n = b->exact;
+  for (int t = 1; t < f; ++t) {
+    while (!reaches(n, b->exact, max_distance, t, f)) ++n;
+    b->border[t] = uint16_t(n);
+  }
+  b->lo = -int(b->border[f - 1]);
+  b->hi = bidirectional ? int(b->border[f - 1]) : 0;
+  return true;
+}
+
+int validate(const attn_cross_config* c, CrossBias* bias) {
+  if (!c || c->batch < 0 || c->q_len < 0 || c->k_len < 0 || c->heads < 1 || c->kv_heads < 1)
+    return ABFT_ERR_INVALID;
+  if (c->heads % c->kv_heads) return ABFT_ERR_INVALID;
+  if (c->causal != 0 && c->causal != 1) return ABFT_ERR_INVALID;
+  if (!std::isfinite(c->scale)) return ABFT_ERR_INVALID;
+  if (c->buckets < 0) return ABFT_ERR_INVALID;
+  if (c->dtype != ABFT_BF16 && c->dtype != ABFT_FP32) return ABFT_ERR_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128) return ABFT_ERR_UNSUPPORTED;
+  if (c->q_len > MAX_LEN || c->k_len > MAX_LEN) return ABFT_ERR_UNSUPPORTED;
+  const int64_t wgs = int64_t(c->batch) * c->heads;
+  if (wgs > (int64_t(1) << 24) ||
+      wgs * std::max(cross_tiles(c->q_len), cross_tiles(c->k_len)) > (int64_t(1) << 30))
+    return ABFT_ERR_UNSUPPORTED;
+  if (c->buckets && !make_bias(c->buckets, c->max_distance, c->bidirectional, bias))
+    return ABFT_ERR_INVALID;
+  return ABFT_OK;
+}
+
+// Whether the short form takes a forward, and its key splits. It runs the
+// queries of all heads that share a key head as tiles of 32 rows.
+bool short_form(const attn_cross_config* c, int* splits) {
+  *splits = 1;
+  if (c->q_len > 32) return false;
+  const int64_t rows = int64_t(c->q_len) * (c->heads / c->kv_heads);
+  const int64_t base = int64_t(c->batch) * c->kv_heads * ((rows + 31) / 32);
+  if (base == 0) return false;
+  const int64_t steps = (int64_t(c->k_len) + 127) / 128;
+  int64_t n = (512 + base - 1) / base;
+  n = std::min(n, steps / 2);
+  *splits = int(std::max<int64_t>(1, std::min<int64_t>(n, 64)));
+  return true;
+}
+
+struct Space {
+  size_t part_o = 0, part_ml = 0;        // forward, short form
+  size_t nlse = 0, ndelta = 0, dbias = 0;  // backward
+  size_t fwd = 0, bwd = 0;
+};
+
+Space make_space(const attn_cross_config* c) {
+  Space L;
+  int splits;
+  if (short_form(c, &splits) && splits > 1) {
+    const size_t n = size_t(c->batch) * c->heads * c->q_len * splits;
+    L.part_o = 0;
+    L.part_ml = align_up(n * c->head_dim * 4);
+    L.fwd = L.part_ml + align_up(n * 8);
+  }
+  const size_t rows = size_t(c->batch) * c->heads * cross_tiles(c->q_len) * CROSS_QT;
+  L.ndelta = align_up(rows * 4);
+  L.dbias = 2 * L.ndelta;
+  L.bwd = L.dbias + align_up(size_t(c->batch) * c->heads * cross_tiles(c->q_len) * c->buckets * 4);
+  return L;
+}
+
+// An operand as the kernels take it: n tokens of nh heads.
+int take(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh, bool out,
+         CrossTensor* r) {
+  if (!t) return ABFT_ERR_INVALID;
+  if (c->batch == 0 || n == 0) return ABFT_OK;  // no element: not looked at
+  const int es = es_of(c);
+  const int64_t st[3] = {t->batch_stride, t->token_stride, t->head_stride};
+  const int ext[3] = {c->batch, n, nh};
+  if (!t->data || reinterpret_cast<uintptr_t>(t->data) % 16) return ABFT_ERR_INVALID;
+  for (int k = 0; k < 3; ++k) {
+    if (ext[k] == 1) continue;                  // the stride is not used
+    if (st[k] < 0 || (st[k] * es) % 16) return ABFT_ERR_INVALID;
+    if (out && st[k] < c->head_dim) return ABFT_ERR_INVALID;  // rows written twice
+  }
+  if (n > 1 && st[1] * es > MAX_TOKEN_BYTES) return ABFT_ERR_UNSUPPORTED;
+  r->p = static_cast<char*>(const_cast<void*>(t->data));
+  r->b = c->batch > 1 ? st[0] * es : 0;
+  r->t = n > 1 ? uint32_t(st[1] * es) : 0;
+  r->h = nh > 1 ? st[2] * es : 0;
+  return ABFT_OK;
+}
+
+void common(const attn_cross_config* c, const float* bias, const int32_t* k_lens,
+            const int32_t* q_start, CrossArgs* a) {
+  a->B = c->batch;
+  a->Sq = c->q_len;
+  a->Sk = c->k_len;
+  a->nh = c->heads;
+  a->kvh = c->kv_heads;
+  a->group = c->heads / c->kv_heads;
+  a->causal = c->causal;
+  a->scale = c->scale > 0.f ? c->scale : 1.f / std::sqrt(float(c->head_dim));
+  a->k_lens = k_lens;
+  a->q_start = q_start;
+  a->bias.table = bias;
+}
+
+}  // namespace
+}  // namespace abft
+
+using namespace abft;
+
+#define TRY(x)                      \
+  do {                              \
+    const int st_ = (x);            \
+    if (st_ != ABFT_OK) return st_; \
+  } while (0)
+#define CK(x)                                       \
+  do {                                              \
+    if ((x) != hipSuccess) return ABFT_ERR_HIP;     \
+  } while (0)
+
+extern "C" {
+
+int attn_rel_bucket(int64_t relative, int32_t buckets, int32_t max_distance,
+                    int32_t bidirectional) {
+  CrossBias b;
+  if (buckets < 1 || !make_bias(buckets, max_distance, bidirectional, &b)) return ABFT_ERR_INVALID;
+  int base = 0;
+  int64_t n = relative < -CROSS_MAX_DISTANCE ? -CROSS_MAX_DISTANCE
+                                             : (relative > CROSS_MAX_DISTANCE ? CROSS_MAX_DISTANCE
+                                                                              : relative);
+  if (b.bidirectional) {
+    base = n > 0 ? b.side : 0;
+    n = n < 0 ? -n : n;
+  } else {
+    n = n < 0 ? -n : 0;
+  }
+  if (n < b.exact) return base + int(n);
+  int k = b.exact;
+  for (int i = 1; i < b.side - b.exact; ++i) k += n >= b.border[i] ? 1 : 0;
+  return base + k;
+}
+
+size_t attn_cross_workspace_bytes(const attn_cross_config* cfg) {
+  CrossBias b;
+  if (validate(cfg, &b) != ABFT_OK) return 0;
+  const Space L = make_space(cfg);
+  return std::max(std::max(L.fwd, L.bwd), ALIGN);
+}
+
+int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
+                       const attn_cross_tensor* K, const attn_cross_tensor* V, const float* bias,
+                       const int32_t* k_lens, const int32_t* q_start, const attn_cross_tensor* O,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  CrossArgs a;
+  TRY(validate(cfg, &a.bias));
+  if ((cfg->buckets > 0) != (bias != nullptr)) return ABFT_ERR_INVALID;
+  TRY(take(cfg, Q, cfg->q_len, cfg->heads, false, &a.q));
+  TRY(take(cfg, K, cfg->k_len, cfg->kv_heads, false, &a.k));
+  TRY(take(cfg, V, cfg->k_len, cfg->kv_heads, false, &a.v));
+  TRY(take(cfg, O, cfg->q_len, cfg->heads, true, &a.o));
+  const Space L = make_space(cfg);
+  if (L.fwd && !workspace) return ABFT_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16) return ABFT_ERR_INVALID;
+  if (workspace_bytes < L.fwd) return ABFT_ERR_WORKSPACE;
+  if (cfg->batch == 0 || cfg->q_len == 0) return ABFT_OK;
+  TRY(check_device());
+  common(cfg, bias, k_lens, q_start, &a);
+  a.lse = lse;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (short_form(cfg, &a.splits)) {
+    char* ws = static_cast<char*>(workspace);
+    a.part_o = reinterpret_cast<float*>(ws + L.part_o);
+    a.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
+    CK(launch_cross_short(a, cfg->dtype, cfg->head_dim, s));
+  } else {
+    CK(launch_cross_fwd(a, cfg->dtype, cfg->head_dim, s));
+  }
+  return ABFT_OK;
+}
+
+int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* dO,
+                        const attn_cross_tensor* Q, const attn_cross_tensor* K,
+                        const attn_cross_tensor* V, const attn_cross_tensor* O, const float* lse,
+                        const float* bias, const int32_t* k_lens, const int32_t* q_start,
+                        const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
+                        const attn_cross_tensor* dV, float* dbias, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  CrossArgs a;
+  TRY(validate(cfg, &a.bias));
+  if ((cfg->buckets > 0) != (bias != nullptr)) return ABFT_ERR_INVALID;
+  if ((cfg->buckets > 0) != (dbias != nullptr)) return ABFT_ERR_INVALID;
+  TRY(take(cfg, dO, cfg->q_len, cfg->heads, false, &a.dout));
+  TRY(take(cfg, Q, cfg->q_len, cfg->heads, false, &a.q));
+  TRY(take(cfg, K, cfg->k_len, cfg->kv_heads, false, &a.k));
+  TRY(take(cfg, V, cfg->k_len, cfg->kv_heads, false, &a.v));
+  TRY(take(cfg, O, cfg->q_len, cfg->heads, false, &a.o));
+  TRY(take(cfg, dQ, cfg->q_len, cfg->heads, true, &a.dq));
+  TRY(take(cfg, dK, cfg->k_len, cfg->kv_heads, true, &a.dk));
+  TRY(take(cfg, dV, cfg->k_len, cfg->kv_heads, true, &a.dv));
+  const bool any_q = cfg->batch > 0 && cfg->q_len > 0, any_k = cfg->batch > 0 && cfg->k_len > 0;
+  if (any_q && !lse) return ABFT_ERR_INVALID;
+  const Space L = make_space(cfg);
+  if (L.bwd && !workspace) return ABFT_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16) return ABFT_ERR_INVALID;
+  if (workspace_bytes < L.bwd) return ABFT_ERR_WORKSPACE;
+  TRY(check_device());
+  common(cfg, bias, k_lens, q_start, &a);
+  a.lse = const_cast<float*>(lse);
+  char* ws = static_cast<char*>(workspace);
+  a.q_pad = cross_tiles(cfg->q_len) * CROSS_QT;
+  a.nlse = reinterpret_cast<float*>(ws);
+  a.ndelta = reinterpret_cast<float*>(ws + L.ndelta);
+  a.dbias_part = reinterpret_cast<float*>(ws + L.dbias);
+  a.dbias = dbias;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (any_q) CK(launch_cross_bwd_q(a, cfg->dtype, cfg->head_dim, s));
+  if (any_k) CK(launch_cross_bwd_kv(a, cfg->dtype, cfg->head_dim, s));
+  if (cfg->buckets) CK(launch_cross_dbias(a, s));
+  return ABFT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,399 @@
+// Attention over keys of another length, backward, from the forward's lse.
+//
+//   P_ij = 2^(s_ij log2 e - lse_i),  D_i = dO_i . O_i,  dP_ij = dO_i . v_j,
+//   dS_ij = P_ij (dP_ij - D_i),
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,
+//   dv_j = sum_i P_ij dO_i,  dtable[t] = sum over pairs of bucket t of dS_ij,
+// with dk_j and dv_j summed over the query heads that share a key head.
+//
+// Two passes, each of which owns what it sums (no atomics on memory, so
+// results do not depend on the order of workgroups): the query pass owns 128
+// queries and runs over the keys (dq, dtable; it leaves -lse and -D for the
+// other), the key pass owns 128 keys and runs over the queries of all heads
+// that share them (dk, dv). The price is a second S and dP (14 d flops a pair
+// against 10 d in one pass).
+#include "cross_tile.hpp"
+
+namespace abft {
+namespace {
+
+template <typename T>
+constexpr int other_tile() { return sizeof(T) == 2 ? 64 : 32; }
+
+// ---- query pass -----------------------------------------------------------
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
+  using Tile = CrossTile<T, D>;
+  constexpr int KT = other_tile<T>(), NB = KT / 32;
+  constexpr int IMG = KT * Tile::ROWB;
+  extern __shared__ __align__(1024) char smem[];
+  float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
+  // sums of dS by t, one array for each wave and half: the lanes of a half
+  // hold 32 queries and one key, so an addition never meets another to the
+  // same entry and the order of every sum is fixed
+  const int span = BIAS ? bias_span(a.bias) : 0;
+  float* sums = tab + span;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
+  const int nbk = a.B * a.kvh, ntile = cross_tiles_d(a.Sq);
+  const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
+  const int b = bk / a.kvh, kv = bk % a.kvh, h = kv * a.group + y % a.group;
+  int tile = y / a.group;
+  if (a.causal) tile = ntile - 1 - tile;
+  const int q0 = tile * CROSS_QT;
+  const int len = seq_len(a, b), start = seq_start(a, b);
+  int kend = len;
+  if (a.causal) kend = min(kend, start + min(q0 + CROSS_QT, a.Sq));
+  kend = max(kend, 0);
+  const int nt = (kend + KT - 1) / KT;
+  const int w0 = q0 + 32 * wave, i = w0 + (lane & 31), ic = min(i, a.Sq - 1);
+  const bool valid = i < a.Sq;
+  int wend = len;
+  if (a.causal) wend = min(wend, start + min(w0 + 32, a.Sq));
+  if (w0 >= a.Sq) wend = 0;
+  const int limit = a.causal ? min(len, start + i + 1) : len;
+
+  const char* kp = a.k.p + b * a.k.b + kv * a.k.h;
+  const char* vp = a.v.p + b * a.v.b + kv * a.v.h;
+  const uint32_t lds0 = lds_addr(smem);
+  auto issue = [&](int t) {
+    const uint32_t to = lds0 + (t & 1) * 2 * IMG;
+    Tile::template issue<KT, 4>(kp + int64_t(t) * KT * a.k.t, a.k.t, len - t * KT, to, wave, lane);
+    Tile::template issue<KT, 4>(vp + int64_t(t) * KT * a.v.t, a.v.t, len - t * KT, to + IMG, wave,
+                                lane);
+  };
+  if (nt > 0) issue(0);
+
+  typename Tile::RowFrag q, g;
+  Tile::load_row(q, a.q.p + b * a.q.b + h * a.q.h + int64_t(ic) * a.q.t, half);
+  Tile::load_row(g, a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(ic) * a.dout.t, half);
+  float nl, nd;
+  {
+    typename Tile::RowFrag o;
+    Tile::load_row(o, a.o.p + b * a.o.b + h * a.o.h + int64_t(ic) * a.o.t, half);
+    nd = -half_sum(Tile::dot_row(g, o));
+    const float lse = a.lse[(int64_t(b) * a.nh + h) * a.Sq + ic];
+    // rows without keys and rows past the last query: P = 0
+    nl = valid && lse != NEG_INF ? -lse : NEG_INF;
+    if (!valid) {
+      nd = 0.f;
+      Tile::zero_row(g);
+    }
+    if (half == 0) {
+      const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i;
+      a.nlse[at] = nl;
+      a.ndelta[at] = nd;
+    }
+  }
+  if constexpr (BIAS) {
+    bias_spread(tab, a.bias, h, a.nh, tid, 256);
+    for (int x = tid; x < 8 * span; x += 256) sums[x] = 0.f;
+  }
+  float* mine = sums + (wave * 2 + half) * span;
+  float far_lo = 0.f, far_hi = 0.f;  // sums of the blocks in a constant side
+
+  floatx16 dq[Tile::ND];
+#pragma unroll
+  for (int d = 0; d < Tile::ND; ++d) dq[d] = floatx16{};
+  const float c = a.scale * LOG2E;
+  for (int t = 0; t < nt; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < nt) issue(t + 1);
+    const int k0 = t * KT;
+    if (k0 >= wend) continue;
+    const char* img = smem + (t & 1) * 2 * IMG;
+    const bool masked = k0 + KT > len || (a.causal && k0 + KT - 1 > start + w0);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      floatx16 s = floatx16{}, dp;
+      Tile::rows(s, img, 32 * n, q, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = nd;
+      Tile::rows(dp, img + IMG, 32 * n, g, lane);
+      float ce = c, off = nl;
+      int where = 0, at = 0;  // -1, 1: in a constant side
+      if constexpr (BIAS) {
+        const int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
+        if (tb + 31 <= a.bias.lo) {
+          where = -1;
+          off += tab[0];
+        } else if (tb - 31 >= a.bias.hi) {
+          where = 1;
+          off += tab[span - 1];
+        } else {
+          ce = 1.f;
+          at = tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[r] = fmaf(s[r], c, tab[at + 8 * (r >> 2) + (r & 3)]);
+        }
+      }
+      if (masked) {
+        const int lim = limit - k0 - 32 * n - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < lim ? s[r] : NEG_INF;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
+      if constexpr (BIAS) {
+        if (where == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            __hip_atomic_fetch_add(mine + at + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_WAVEFRONT);
+        } else {
+          float sum = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum += s[r];
+          if (where < 0)
+            far_lo += sum;
+          else
+            far_hi += sum;
+        }
+      }
+      typename Tile::Probs p;
+      Tile::pack(p, s);
+      Tile::cols(dq, img, 32 * n, p, lane);
+    }
+  }
+  Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid, half);
+
+  if constexpr (BIAS) {
+    // by t over the waves and halves, then by bucket: a side's buckets are
+    // runs of t, and a thread sums one bucket's run (or two: t = 0 belongs to
+    // the first of the lower side)
+    far_lo = group_sum<64>(far_lo);
+    far_hi = group_sum<64>(far_hi);
+    __syncthreads();
+    for (int x = tid; x < span; x += 256) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) v += sums[w * span + x];
+      tab[x] = v;
+    }
+    __syncthreads();
+    if (lane == 0) {
+      sums[2 * wave] = far_lo;
+      sums[2 * wave + 1] = far_hi;
+    }
+    __syncthreads();
+    const int lo = a.bias.lo, hi = a.bias.hi, side = a.bias.side;
+    for (int k = tid; k < a.bias.buckets; k += 256) {
+      float v = 0.f;
+      // distances [n0, n1) of the bucket; the last one of a side is open
+      const int u = k % side;
+      const bool ahead = k >= side, last = u == side - 1;
+      int n0 = u < a.bias.exact ? u : (u == a.bias.exact ? u : a.bias.border[u - a.bias.exact]);
+      int n1 = u < a.bias.exact ? u + 1
+                                : (last ? 0 : a.bias.border[u - a.bias.exact + 1]);
+      if (!ahead) {
+        // t from -(n1 - 1) to -n0, and for a one-sided table t >= 0 too
+        const int t1 = -n0, t0 = last ? lo - BIAS_PAD : -(n1 - 1);
+        for (int t = t0; t <= t1; ++t) v += tab[t - lo + BIAS_PAD];
+        if (last) v += (sums[0] + sums[2]) + (sums[4] + sums[6]);
+        if (!a.bias.bidirectional && u == 0) {
+          for (int t = 1; t <= hi + BIAS_PAD; ++t) v += tab[t - lo + BIAS_PAD];
+          v += (sums[1] + sums[3]) + (sums[5] + sums[7]);
+        }
+      } else {
+        const int t0 = max(n0, 1), t1 = last ? hi + BIAS_PAD : n1 - 1;
+        for (int t = t0; t <= t1; ++t) v += tab[t - lo + BIAS_PAD];
+        if (last) v += (sums[1] + sums[3]) + (sums[5] + sums[7]);
+      }
+      a.dbias_part[((int64_t(h) * a.B + b) * ntile + tile) * a.bias.buckets + k] = v;
+    }
+  }
+}
+
+// Sums the query pass's partial bias gradients of one head in a fixed order.
+__global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, float* dbias, int n,
+                                                          int buckets, int heads) {
+  __shared__ float sh[256];
+  const int h = blockIdx.x, lanes = 256 / buckets;  // partial sums of a bucket
+  const int k = threadIdx.x % buckets, j = threadIdx.x / buckets;
+  float v = 0.f;
+  if (j < lanes)
+    for (int x = j; x < n; x += lanes) v += part[(int64_t(h) * n + x) * buckets + k];
+  sh[threadIdx.x] = v;
+  __syncthreads();
+  if (threadIdx.x < buckets) {
+    for (int x = 1; x < lanes; ++x) v += sh[x * buckets + threadIdx.x];
+    dbias[int64_t(threadIdx.x) * heads + h] = v;
+  }
+}
+
+// ---- key pass ---------------------------------------------------------------
+// S = Q K^T, so that a lane holds the scores of one key (its mask is a bound on
+// the query) and P and dS are the second operands of dV^T = dO^T P and
+// dK^T = Q^T dS from registers.
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
+  using Tile = CrossTile<T, D>;
+  constexpr int QT = other_tile<T>(), NB = QT / 32;
+  constexpr int IMG = QT * Tile::ROWB;
+  constexpr int STAGE = 2 * IMG + 512;  // Q, dO, -lse and -D of a tile
+  extern __shared__ __align__(1024) char smem[];
+  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
+  const int nbk = a.B * a.kvh;
+  const int bk = blockIdx.x % nbk, tile = blockIdx.x / nbk;  // causal: heaviest first
+  const int b = bk / a.kvh, kv = bk % a.kvh;
+  const int len = seq_len(a, b), start = seq_start(a, b);
+  const int key0 = tile * CROSS_QT, w0 = key0 + 32 * wave, j = w0 + (lane & 31);
+  // query tiles that see the workgroup's keys, of each head of the group
+  int first = 0;
+  if (a.causal) first = max(0, key0 - start) / QT;
+  int per = max(0, (a.Sq + QT - 1) / QT - first);
+  if (key0 >= len) per = 0;
+  const int nt = per * a.group;
+
+  const uint32_t lds0 = lds_addr(smem);
+  auto issue = [&](int t) {
+    const int h = kv * a.group + t / per, i0 = (first + t % per) * QT;
+    const uint32_t to = lds0 + (t & 1) * STAGE;
+    Tile::template issue<QT, 4>(a.q.p + b * a.q.b + h * a.q.h + int64_t(i0) * a.q.t, a.q.t,
+                                a.Sq - i0, to, wave, lane);
+    Tile::template issue<QT, 4>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
+                                a.dout.t, a.Sq - i0, to + IMG, wave, lane);
+    const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i0;
+    if (wave < 2) {  // (64 values; a 32-row tile uses half of them)
+      const int n = min(64, a.q_pad - i0);
+      dma4(rsrc_of((wave == 0 ? a.nlse : a.ndelta) + at, 256), uni(to + 2 * IMG + wave * 256),
+           uint32_t(min(lane, n - 1) * 4), 0u);
+    }
+  };
+  if (nt > 0) issue(0);
+
+  typename Tile::RowFrag kf, vf;
+  const int jc = max(0, min(j, len - 1));
+  if (nt > 0) {
+    Tile::load_row(kf, a.k.p + b * a.k.b + kv * a.k.h + int64_t(jc) * a.k.t, half);
+    Tile::load_row(vf, a.v.p + b * a.v.b + kv * a.v.h + int64_t(jc) * a.v.t, half);
+  }
+  floatx16 dk[Tile::ND], dv[Tile::ND];
+#pragma unroll
+  for (int d = 0; d < Tile::ND; ++d) {
+    dk[d] = floatx16{};
+    dv[d] = floatx16{};
+  }
+  const float c = a.scale * LOG2E;
+  for (int t = 0; t < nt; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < nt) issue(t + 1);
+    if constexpr (BIAS) {
+      if (t % per == 0) {  // the next head's bias (every wave is past the last one's)
+        bias_spread(tab, a.bias, kv * a.group + t / per, a.nh, tid, 256);
+        __syncthreads();
+      }
+    }
+    const int i0 = (first + t % per) * QT;
+    if (w0 >= len || (a.causal && start + i0 + QT - 1 < w0)) continue;
+    const char* img = smem + (t & 1) * STAGE;
+    const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
+    const float* nds = nls + 64;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      floatx16 s = floatx16{}, dp, nl;
+      Tile::rows(s, img, 32 * n, kf, lane);
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int row = 32 * n + 2 * r + 4 * half;  // 8 (r / 4) + 4 half
+        const floatx4 x = *reinterpret_cast<const floatx4*>(nls + row);
+        const floatx4 d = *reinterpret_cast<const floatx4*>(nds + row);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          nl[r + e] = x[e];
+          dp[r + e] = d[e];
+        }
+      }
+      Tile::rows(dp, img + IMG, 32 * n, vf, lane);
+      float ce = c, off = 0.f;
+      if constexpr (BIAS) {
+        const int tb = w0 - start - i0 - 32 * n;  // the block spans [tb - 31, tb + 31]
+        if (tb + 31 <= a.bias.lo) {
+          off = tab[0];
+        } else if (tb - 31 >= a.bias.hi) {
+          off = tab[bias_span(a.bias) - 1];
+        } else {
+          ce = 1.f;
+          const float* p = tab + (tb + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[-(8 * (r >> 2) + (r & 3))]);
+        }
+      }
+      if (a.causal && start + i0 + 32 * n < w0 + 31) {
+        // query start + i0 + 32 n + row sees key j from row = j - start - i0 - 32 n on
+        const int from = j - start - i0 - 32 * n - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= from ? s[r] : NEG_INF;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, nl[r] + off));
+      typename Tile::Probs p;
+      Tile::pack(p, s);
+      Tile::cols(dv, img + IMG, 32 * n, p, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] *= dp[r];
+      Tile::pack(p, s);
+      Tile::cols(dk, img, 32 * n, p, lane);
+    }
+  }
+  // keys behind the sequence's length: zero
+  const bool valid = j < a.Sk;
+  if (j >= len) {
+#pragma unroll
+    for (int d = 0; d < Tile::ND; ++d) {
+      dk[d] = floatx16{};
+      dv[d] = floatx16{};
+    }
+  }
+  Tile::store_row(a.dk.p + b * a.dk.b + kv * a.dk.h + int64_t(j) * a.dk.t, dk, a.scale, valid, half);
+  Tile::store_row(a.dv.p + b * a.dv.b + kv * a.dv.h + int64_t(j) * a.dv.t, dv, 1.f, valid, half);
+}
+
+template <typename T, int D, bool BIAS>
+hipError_t run_q(const CrossArgs& a, hipStream_t s) {
+  const size_t lds = size_t(4) * other_tile<T>() * D * sizeof(T) +
+                     (BIAS ? size_t(9) * bias_span_h(a.bias) * 4 : 0);
+  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS>>(160 * 1024);
+  if (e != hipSuccess) return e;
+  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq);
+  cross_bwd_q_kernel<T, D, BIAS><<<dim3(uint32_t(grid)), 256, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool BIAS>
+hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
+  const size_t lds = 2 * (size_t(2) * other_tile<T>() * D * sizeof(T) + 512) +
+                     (BIAS ? size_t(bias_span_h(a.bias)) * 4 : 0);
+  hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS>>(160 * 1024);
+  if (e != hipSuccess) return e;
+  const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk);
+  cross_bwd_kv_kernel<T, D, BIAS><<<dim3(uint32_t(grid)), 256, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cross_bwd_q(const CrossArgs& a, int dtype, int D, hipStream_t s) {
+  return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
+    return run_q<typename decltype(t)::type, decltype(d)::value, decltype(bias)::value>(a, s);
+  });
+}
+
+hipError_t launch_cross_bwd_kv(const CrossArgs& a, int dtype, int D, hipStream_t s) {
+  return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
+    return run_kv<typename decltype(t)::type, decltype(d)::value, decltype(bias)::value>(a, s);
+  });
+}
+
+hipError_t launch_cross_dbias(const CrossArgs& a, hipStream_t s) {
+  cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
+      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sq), a.bias.buckets, a.nh);
+  return hipGetLastError();
+}
+
+}  // namespace abft

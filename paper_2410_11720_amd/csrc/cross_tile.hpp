@@ -1,0 +1,307 @@
+// Building blocks of the attention kernels over keys of another length
+// (cross_fwd.hip, cross_bwd.hip): operand tiles in LDS, their products on
+// the matrix cores, and the relative position bias.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "abft_device.hpp"
+#include "cross_internal.hpp"
+#include "direct_lds.hpp"
+
+namespace abft {
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float NEG_INF = -__builtin_inff();
+constexpr float LOG2E = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
+
+// x combined with the value of lane l ^ 32.
+__device__ __forceinline__ float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef float float2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const float2_t f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+}
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+__device__ __forceinline__ int cross_tiles_d(int n) { return (n + CROSS_QT - 1) / CROSS_QT; }
+
+// Keys of a sequence, and the position of its first query among them (values
+// that the host cannot check are brought into range here).
+__device__ __forceinline__ int seq_len(const CrossArgs& a, int b) {
+  return a.k_lens ? clampi(a.k_lens[b], 0, a.Sk) : a.Sk;
+}
+__device__ __forceinline__ int seq_start(const CrossArgs& a, int b) {
+  return a.q_start ? clampi(a.q_start[b], -(1 << 29), 1 << 29) : 0;
+}
+
+// 4 bytes per lane from the buffer to LDS [lds, lds + 256) in lane order.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma4(const u32x4& rs, uint32_t lds, uint32_t voff, uint32_t soff) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :
+               : "s"(lds), "v"(voff), "s"(rs), "s"(soff)
+               : "memory", "m0");
+#endif
+}
+#pragma clang diagnostic pop
+
+// A tile of rows of D elements in LDS, row-major, 16-byte chunk c of row r at
+// chunk c ^ swz(r). Both ways a tile is read are free of bank conflicts: the
+// 8 rows that a 16-byte read of one chunk serves together hit 8 chunks, and
+// the 4 rows that a transposing read serves together hit 4 pairs of chunks.
+//
+// Products (32 x 32 tiles, lane l: column l % 32, half = l / 32):
+//  rows  C[32 rows x 32] += tile rows . B, B's column the lane's own vector of
+//        D elements (RowFrag)
+//  cols  C[D x 32] += tile^T . P over 32 rows, P the 32 x 32 result of a
+//        `rows` product: register r of it holds row 8 (r / 4) + 4 half + r % 4,
+//        and the transposed operand is read in that order of rows, so P goes
+//        from one product to the next in registers.
+template <typename T, int D>
+struct CrossTile {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int ROWB = D * int(sizeof(T));  // bytes per row
+  static constexpr int CPR = ROWB / 16;            // chunks per row
+  static constexpr int RPR = 64 / CPR;             // rows per 1-KB run
+  static constexpr int NV = 8 / RPR;               // runs until the swizzle repeats
+  static constexpr int NF = D / (BF ? 16 : 8);     // fragments of a row vector
+  static constexpr int ND = D / 32;                // 32-row blocks of a transposed product
+
+  __device__ static __forceinline__ int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+  // the lane's share of a row vector: 16-byte chunks 2 f + half
+  struct RowFrag {
+    u32x4 f[NF];
+  };
+  __device__ static __forceinline__ void load_row(RowFrag& q, const char* row, int half) {
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      q.f[f] = *reinterpret_cast<const u32x4*>(row + (2 * f + half) * 16);
+  }
+  __device__ static __forceinline__ void zero_row(RowFrag& q) {
+#pragma unroll
+    for (int f = 0; f < NF; ++f) q.f[f] = u32x4{0u, 0u, 0u, 0u};
+  }
+  // this lane's part of the dot product of two row vectors
+  __device__ static __forceinline__ float dot_row(const RowFrag& a, const RowFrag& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (BF) {
+          s = fmaf(__uint_as_float(a.f[f][e] << 16), __uint_as_float(b.f[f][e] << 16), s);
+          s = fmaf(__uint_as_float(a.f[f][e] & 0xffff0000u),
+                   __uint_as_float(b.f[f][e] & 0xffff0000u), s);
+        } else {
+          s = fmaf(__uint_as_float(a.f[f][e]), __uint_as_float(b.f[f][e]), s);
+        }
+      }
+    return s;
+  }
+
+  // Copies ROWS rows starting at `src` (rows ldb bytes apart) to the image at
+  // `lds`, split over NW waves. Rows from `left` on repeat row left - 1, so
+  // nothing past a sequence's end is read: what they bring is masked or never
+  // stored. left >= 1.
+  template <int ROWS, int NW>
+  __device__ static __forceinline__ void issue(const char* src, uint32_t ldb, int left,
+                                               uint32_t lds, int wave, int lane) {
+    constexpr int PW = ROWS / RPR / NW;  // runs of this wave
+    static_assert(PW * RPR * NW == ROWS && PW % NV == 0, "whole runs a wave");
+    const u32x4 rs = rsrc_of(src, 0x7fffffffu);
+    const int r = lane / CPR, pos = lane % CPR;
+    if (left >= ROWS) {
+#pragma unroll
+      for (int j = 0; j < PW; ++j) {
+        const uint32_t vo = uint32_t(r) * ldb + uint32_t((pos ^ swz((j % NV) * RPR + r)) << 4);
+        const int i = wave * PW + j;
+        dma16(rs, uni(lds + i * 1024), vo, uni(uint32_t(i * RPR) * ldb));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < PW; ++j) {
+        const int i = wave * PW + j, row = i * RPR + r;
+        const uint32_t vo =
+            uint32_t(min(row, left - 1)) * ldb + uint32_t((pos ^ swz((j % NV) * RPR + r)) << 4);
+        dma16(rs, uni(lds + i * 1024), vo, 0u);
+      }
+    }
+  }
+
+  // C += rows [row0, row0 + 32) of the image times B
+  __device__ static __forceinline__ void rows(floatx16& c, const char* img, int row0,
+                                              const RowFrag& b, int lane) {
+    const int r = lane & 31, half = lane >> 5;
+    const char* p = img + (row0 + r) * ROWB;
+    const int sw = swz(r);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(p + (((2 * f + half) ^ sw) << 4));
+      if constexpr (BF) {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                    __builtin_bit_cast(bf16x8, b.f[f]), c, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]),
+                                                   __uint_as_float(b.f[f][e]), c, 0, 0, 0);
+      }
+    }
+  }
+
+  // P as the second operand of `cols`: bf16 rounds it (the products take
+  // bf16 operands and sum in fp32), fp32 keeps it
+  struct Probs {
+    float x[BF ? 1 : 16];
+    u32x4 b[BF ? 2 : 1];
+  };
+  __device__ static __forceinline__ void pack(Probs& p, const floatx16& s) {
+    if constexpr (BF) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        p.b[k] = u32x4{pack_bf16(s[8 * k], s[8 * k + 1]), pack_bf16(s[8 * k + 2], s[8 * k + 3]),
+                       pack_bf16(s[8 * k + 4], s[8 * k + 5]), pack_bf16(s[8 * k + 6], s[8 * k + 7])};
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p.x[r] = s[r];
+    }
+  }
+
+  // C[d] += (rows [row0, row0 + 32) of the image)^T P
+  __device__ static __forceinline__ void cols(floatx16 (&c)[ND], const char* img, int row0,
+                                              const Probs& p, int lane) {
+    const int half = lane >> 5;
+    if constexpr (BF) {
+      // lane l of a 16-lane group supplies 4 elements of row l / 4, columns
+      // 4 (l % 4); it receives column l of the 4 rows
+      const int s = lane & 15, k = 4 * half + (s >> 2);
+      const int ch = 2 * ((lane >> 4) & 1) + ((s >> 1) & 1);
+      const char* q = img + (row0 + k) * ROWB + (s & 1) * 8;
+      const int sw = swz(k);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const char* a0 = q + st * 16 * ROWB + (((4 * d + ch) ^ sw) << 4);
+          const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)a0);
+          const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a0 + 8 * ROWB));
+          typedef short short8_t __attribute__((ext_vector_type(8)));
+          const short8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          c[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v),
+                                                         __builtin_bit_cast(bf16x8, p.b[st]), c[d],
+                                                         0, 0, 0);
+        }
+    } else {
+      const int col = lane & 31;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int k = 8 * (r >> 2) + 4 * half + (r & 3);
+        const char* q = img + (row0 + k) * ROWB + (col & 3) * 4;
+        const int sw = swz(k);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const float a = *reinterpret_cast<const float*>(q + (((8 * d + (col >> 2)) ^ sw) << 4));
+          c[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.x[r], c[d], 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // Stores a transposed result (lane: column l % 32 = one output row, rows
+  // = its elements) times f to `row`. bf16: the halves exchange 4-element
+  // groups first, so a lane stores 16 bytes.
+  __device__ static __forceinline__ void store_row(char* row, const floatx16 (&c)[ND], float f,
+                                                   bool valid, int half) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      if constexpr (BF) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          u32x2 a = {pack_bf16(c[d][8 * k] * f, c[d][8 * k + 1] * f),
+                     pack_bf16(c[d][8 * k + 2] * f, c[d][8 * k + 3] * f)};
+          u32x2 b = {pack_bf16(c[d][8 * k + 4] * f, c[d][8 * k + 5] * f),
+                     pack_bf16(c[d][8 * k + 6] * f, c[d][8 * k + 7] * f)};
+          u32x4 o;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const auto x = __builtin_amdgcn_permlane32_swap(a[e], b[e], false, false);
+            o[e] = x[0];
+            o[2 + e] = x[1];
+          }
+          if (valid)
+            *reinterpret_cast<u32x4*>(row + (32 * d + 16 * k + 8 * half) * 2) = o;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (valid)
+            *reinterpret_cast<floatx4*>(row + (32 * d + 8 * k + 4 * half) * 4) =
+                floatx4{c[d][4 * k] * f, c[d][4 * k + 1] * f, c[d][4 * k + 2] * f,
+                        c[d][4 * k + 3] * f};
+      }
+    }
+  }
+};
+
+// ---- relative position bias ------------------------------------------------
+// The bias of a pair depends on t = key - query position alone, and is
+// constant for t <= lo and for t >= hi. A workgroup spreads its head's column of
+// the table over t once (times log2 e, as the scores enter exp2), 32 x 32
+// blocks inside a constant side add one value, the others read LDS.
+// (Reading the table through a bucket index costs a second LDS access an
+// element.)
+constexpr int BIAS_PAD = CROSS_BIAS_PAD;
+
+__device__ __forceinline__ int bias_bucket(const CrossBias& b, int t) {
+  int n, base = 0;
+  if (b.bidirectional) {
+    n = t < 0 ? -t : t;
+    base = t > 0 ? b.side : 0;
+  } else {
+    n = t < 0 ? -t : 0;
+  }
+  if (n < b.exact) return base + n;
+  int k = b.exact;
+  for (int i = 1; i < b.side - b.exact; ++i) k += n >= b.border[i] ? 1 : 0;
+  return base + k;
+}
+
+// entries of the spread table
+__device__ __forceinline__ int bias_span(const CrossBias& b) { return b.hi - b.lo + 1 + 2 * BIAS_PAD; }
+
+// a table entry as it enters exp2; entries below -1e30 mask
+__device__ __forceinline__ float bias_entry(float x) {
+  return x < -1e30f ? NEG_INF : x * LOG2E;
+}
+
+// the spread table of one head: tab[t - lo + BIAS_PAD]
+__device__ __forceinline__ void bias_spread(float* tab, const CrossBias& b, int head, int heads,
+                                            int tid, int nthreads) {
+  const int n = bias_span(b);
+  for (int i = tid; i < n; i += nthreads)
+    tab[i] = bias_entry(b.table[int64_t(bias_bucket(b, i + b.lo - BIAS_PAD)) * heads + head]);
+}
+
+}  // namespace
+}  // namespace abft
