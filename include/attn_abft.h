@@ -394,19 +394,24 @@ size_t attn_cross_workspace_bytes(const attn_cross_config* cfg /* host */);
  *     (a decoded token's is its sequence's length - 1), NULL: 0
  *   lse (device) [batch][heads][q_len] fp32: log2 of the row's sum of
  *     2^(S log2 e), -INF for a row without keys; what the backward takes. May be
- *     NULL. */
+ *     NULL.
+ *   rest (device) [batch][heads][q_len][head_dim] bf16, 16-byte aligned: what
+ *     rounding to bf16 took off O, for the backward. May be NULL; not written in
+ *     fp32. */
 int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
                        const attn_cross_tensor* K, const attn_cross_tensor* V, const float* bias,
                        const int32_t* k_lens, const int32_t* q_start, const attn_cross_tensor* O,
-                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+                       float* lse, void* rest, void* workspace, size_t workspace_bytes,
+                       void* stream);
 
 /* Backward: dQ, dK, dV (as Q, K, V; zero behind a sequence's keys) and dbias
  * [buckets][heads] fp32 (NULL when buckets == 0) from dO, the forward's inputs,
- * its O and lse. */
+ * its O, lse and rest. Without rest (NULL) a row's dO . O is formed for dQ from
+ * the rounded O: an error of 2^-8 |dO| . |O| in every dS of the row. */
 int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* dO,
                         const attn_cross_tensor* Q, const attn_cross_tensor* K,
                         const attn_cross_tensor* V, const attn_cross_tensor* O, const float* lse,
-                        const float* bias, const int32_t* k_lens, const int32_t* q_start,
+                        const void* rest, const float* bias, const int32_t* k_lens, const int32_t* q_start,
                         const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
                         const attn_cross_tensor* dV, float* dbias, void* workspace,
                         size_t workspace_bytes, void* stream);

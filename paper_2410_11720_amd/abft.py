@@ -122,10 +122,10 @@ _sig = {
     "attn_abft_sections_for_step": (_u32, [_vp, _i64]),
     "attn_rel_bucket": (ctypes.c_int, [_i64, _i32, _i32, _i32]),
     "attn_cross_workspace_bytes": (_sz, [_CP]),
-    "attn_cross_forward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _vp, _vp, _vp, _TP, _vp, _vp, _sz,
-                                          _vp]),
-    "attn_cross_backward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _TP, _TP, _vp, _vp, _vp, _vp, _TP,
-                                           _TP, _TP, _vp, _vp, _sz, _vp]),
+    "attn_cross_forward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _vp, _vp, _vp, _TP, _vp, _vp, _vp,
+                                          _sz, _vp]),
+    "attn_cross_backward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _TP, _TP, _vp, _vp, _vp, _vp, _vp,
+                                           _TP, _TP, _TP, _vp, _vp, _sz, _vp]),
     "clip_gradients_workspace_bytes": (_sz, [_i32]),
     "global_grad_norm": (ctypes.c_int, [_vp, _i32, _vp, _vp, _sz, _vp]),
     "clip_gradients": (ctypes.c_int, [_vp, _i32, ctypes.c_double, _vp, _vp, _sz, _vp]),
@@ -478,6 +478,10 @@ def attn_cross_workspace_bytes(cfg: CrossConfig) -> int:
     return n
 
 
+def _data(t):
+    return None if t is None else t.data_ptr()
+
+
 class _on_device:
     """Makes a tensor's device the current one for a call (most calls are on
     it already)."""
@@ -498,23 +502,29 @@ class _on_device:
 
 class CrossAttention:
     """Attention of q_len queries over k_len keys a sequence: owns the
-    workspace of one shape and the row statistics that the forward leaves for the
-    backward (`lse`), as ProtectedAttention does for its layer. Calls run on
-    the current stream of the tensors' device.
+    workspace of one shape and what the forward leaves for the backward (the row
+    statistics `lse`, and `rest`, what rounding took off O), as
+    ProtectedAttention does for its layer; with training=False neither is
+    kept. Calls run on the current stream of the tensors' device.
 
     Q, O, dO, dQ [batch, q_len, heads, head_dim]; K, V, dK, dV [batch, k_len,
     kv_heads, head_dim]; any strides with whole rows at multiples of 16 bytes
     (views of packed projections, of a cache). bias, dbias [buckets, heads]
     fp32; k_lens, q_start [batch] int32."""
 
-    def __init__(self, cfg: CrossConfig, device="cuda"):
+    def __init__(self, cfg: CrossConfig, device="cuda", training=True):
         self.cfg = cfg
         self.device = torch.empty(0, device=device).device
         self._c = cfg.to_c()
         self.workspace = torch.empty(attn_cross_workspace_bytes(cfg), dtype=torch.uint8,
                                      device=self.device)
-        self.lse = torch.empty((cfg.batch, cfg.heads, cfg.q_len), dtype=torch.float32,
-                               device=self.device)
+        self.lse = self.rest = None
+        rows = (cfg.batch, cfg.heads, cfg.q_len)
+        if training:
+            self.lse = torch.empty(rows, dtype=torch.float32, device=self.device)
+        if training and cfg.dtype != "f32":
+            self.rest = torch.empty((*rows, cfg.head_dim), dtype=torch.bfloat16,
+                                    device=self.device)
         kvh = cfg.kv_heads or cfg.heads
         self._q_shape = (cfg.batch, cfg.q_len, cfg.heads, cfg.head_dim)
         self._k_shape = (cfg.batch, cfg.k_len, kvh, cfg.head_dim)
@@ -550,14 +560,16 @@ class CrossAttention:
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
         with _on_device(self.device):
             _check(_lib.attn_cross_forward(self._c, q, k, v, bias, k_lens, q_start, o,
-                                           self.lse.data_ptr(), self.workspace.data_ptr(),
-                                           self.workspace.numel(), _stream()),
-                   "attn_cross_forward")
+                                           _data(self.lse), _data(self.rest),
+                                           self.workspace.data_ptr(), self.workspace.numel(),
+                                           _stream()), "attn_cross_forward")
         return O
 
     def backward(self, dO, Q, K, V, O, bias=None, k_lens=None, q_start=None, dQ=None, dK=None,
                  dV=None, dbias=None):
         c = self.cfg
+        if self.lse is None:
+            raise AbftError("backward: made with training=False")
 
         def new(t, shape):
             return t if t is not None else torch.empty(shape, dtype=c.torch_dtype,
@@ -573,10 +585,10 @@ class CrossAttention:
         db = self._vector(dbias, "dbias", (c.buckets, c.heads), torch.float32)
         with _on_device(self.device):
             _check(_lib.attn_cross_backward(self._c, qs[0], qs[1], ks[0], ks[1], qs[2],
-                                            self.lse.data_ptr(), bias, k_lens, q_start, qs[3],
-                                            ks[2], ks[3], db, self.workspace.data_ptr(),
-                                            self.workspace.numel(), _stream()),
-                   "attn_cross_backward")
+                                            _data(self.lse), _data(self.rest), bias, k_lens,
+                                            q_start, qs[3], ks[2], ks[3], db,
+                                            self.workspace.data_ptr(), self.workspace.numel(),
+                                            _stream()), "attn_cross_backward")
         return dQ, dK, dV, dbias
 
 

@@ -108,7 +108,7 @@ Space make_space(const attn_cross_config* c) {
   const size_t rows = size_t(c->batch) * c->heads * cross_tiles(c->q_len) * CROSS_QT;
   L.ndelta = align_up(rows * 4);
   L.dbias = 2 * L.ndelta;
-  L.bwd = L.dbias + align_up(size_t(c->batch) * c->heads * cross_tiles(c->q_len) * c->buckets * 4);
+  L.bwd = L.dbias + align_up(size_t(c->batch) * c->heads * cross_tiles(c->k_len) * c->buckets * 4);
   return L;
 }
 
@@ -196,7 +196,8 @@ size_t attn_cross_workspace_bytes(const attn_cross_config* cfg) {
 int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
                        const attn_cross_tensor* K, const attn_cross_tensor* V, const float* bias,
                        const int32_t* k_lens, const int32_t* q_start, const attn_cross_tensor* O,
-                       float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+                       float* lse, void* rest, void* workspace, size_t workspace_bytes,
+                       void* stream) {
   CrossArgs a;
   TRY(validate(cfg, &a.bias));
   if ((cfg->buckets > 0) != (bias != nullptr)) return ABFT_ERR_INVALID;
@@ -206,12 +207,14 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
   TRY(take(cfg, O, cfg->q_len, cfg->heads, true, &a.o));
   const Space L = make_space(cfg);
   if (L.fwd && !workspace) return ABFT_ERR_INVALID;
-  if (reinterpret_cast<uintptr_t>(workspace) % 16) return ABFT_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 || reinterpret_cast<uintptr_t>(rest) % 16)
+    return ABFT_ERR_INVALID;
   if (workspace_bytes < L.fwd) return ABFT_ERR_WORKSPACE;
   if (cfg->batch == 0 || cfg->q_len == 0) return ABFT_OK;
   TRY(check_device());
   common(cfg, bias, k_lens, q_start, &a);
   a.lse = lse;
+  a.rest = static_cast<char*>(rest);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (short_form(cfg, &a.splits)) {
     char* ws = static_cast<char*>(workspace);
@@ -227,7 +230,7 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
 int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* dO,
                         const attn_cross_tensor* Q, const attn_cross_tensor* K,
                         const attn_cross_tensor* V, const attn_cross_tensor* O, const float* lse,
-                        const float* bias, const int32_t* k_lens, const int32_t* q_start,
+                        const void* rest, const float* bias, const int32_t* k_lens, const int32_t* q_start,
                         const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
                         const attn_cross_tensor* dV, float* dbias, void* workspace,
                         size_t workspace_bytes, void* stream) {
@@ -247,11 +250,13 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
   if (any_q && !lse) return ABFT_ERR_INVALID;
   const Space L = make_space(cfg);
   if (L.bwd && !workspace) return ABFT_ERR_INVALID;
-  if (reinterpret_cast<uintptr_t>(workspace) % 16) return ABFT_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 || reinterpret_cast<uintptr_t>(rest) % 16)
+    return ABFT_ERR_INVALID;
   if (workspace_bytes < L.bwd) return ABFT_ERR_WORKSPACE;
   TRY(check_device());
   common(cfg, bias, k_lens, q_start, &a);
   a.lse = const_cast<float*>(lse);
+  a.rest = static_cast<char*>(const_cast<void*>(rest));
   char* ws = static_cast<char*>(workspace);
   a.q_pad = cross_tiles(cfg->q_len) * CROSS_QT;
   a.nlse = reinterpret_cast<float*>(ws);

@@ -8,9 +8,9 @@
 //
 // Two passes, each of which owns what it sums (no atomics on memory, so
 // results do not depend on the order of workgroups): the query pass owns 128
-// queries and runs over the keys (dq, dtable; it leaves -lse and -D for the
-// other), the key pass owns 128 keys and runs over the queries of all heads
-// that share them (dk, dv). The price is a second S and dP (14 d flops a pair
+// queries and runs over the keys (dq; it leaves -lse and -D for the other),
+// the key pass owns 128 keys and runs over the queries of all heads that share
+// them (dk, dv, dtable). The price is a second S and dP (14 d flops a pair
 // against 10 d in one pass).
 #include "cross_tile.hpp"
 
@@ -28,11 +28,6 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
   constexpr int IMG = KT * Tile::ROWB;
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
-  // sums of dS by t, one array for each wave and half: the lanes of a half
-  // hold 32 queries and one key, so an addition never meets another to the
-  // same entry and the order of every sum is fixed
-  const int span = BIAS ? bias_span(a.bias) : 0;
-  float* sums = tab + span;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
   const int nbk = a.B * a.kvh, ntile = cross_tiles_d(a.Sq);
@@ -71,7 +66,13 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
   {
     typename Tile::RowFrag o;
     Tile::load_row(o, a.o.p + b * a.o.b + h * a.o.h + int64_t(ic) * a.o.t, half);
-    nd = -half_sum(Tile::dot_row(g, o));
+    nd = Tile::dot_row(g, o);
+    if (sizeof(T) == 2 && a.rest != nullptr) {
+      // dP - D cancels, so D is formed from O before its rounding
+      Tile::load_row(o, a.rest + ((int64_t(b) * a.nh + h) * a.Sq + ic) * Tile::ROWB, half);
+      nd += Tile::dot_row(g, o);
+    }
+    nd = -half_sum(nd);
     const float lse = a.lse[(int64_t(b) * a.nh + h) * a.Sq + ic];
     // rows without keys and rows past the last query: P = 0
     nl = valid && lse != NEG_INF ? -lse : NEG_INF;
@@ -79,18 +80,9 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
       nd = 0.f;
       Tile::zero_row(g);
     }
-    if (half == 0) {
-      const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i;
-      a.nlse[at] = nl;
-      a.ndelta[at] = nd;
-    }
   }
-  if constexpr (BIAS) {
-    bias_spread(tab, a.bias, h, a.nh, tid, 256);
-    for (int x = tid; x < 8 * span; x += 256) sums[x] = 0.f;
-  }
-  float* mine = sums + (wave * 2 + half) * span;
-  float far_lo = 0.f, far_hi = 0.f;  // sums of the blocks in a constant side
+  if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 256);
+  float sum = 0.f;  // of the row's dS
 
   floatx16 dq[Tile::ND];
 #pragma unroll
@@ -112,21 +104,17 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
       for (int r = 0; r < 16; ++r) dp[r] = nd;
       Tile::rows(dp, img + IMG, 32 * n, g, lane);
       float ce = c, off = nl;
-      int where = 0, at = 0;  // -1, 1: in a constant side
       if constexpr (BIAS) {
         const int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
         if (tb + 31 <= a.bias.lo) {
-          where = -1;
           off += tab[0];
         } else if (tb - 31 >= a.bias.hi) {
-          where = 1;
-          off += tab[span - 1];
+          off += tab[bias_span(a.bias) - 1];
         } else {
           ce = 1.f;
-          at = tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD;
+          const float* p = tab + (tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD);
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s[r] = fmaf(s[r], c, tab[at + 8 * (r >> 2) + (r & 3)]);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[8 * (r >> 2) + (r & 3)]);
         }
       }
       if (masked) {
@@ -135,22 +123,9 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
         for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < lim ? s[r] : NEG_INF;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
-      if constexpr (BIAS) {
-        if (where == 0) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            __hip_atomic_fetch_add(mine + at + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_WAVEFRONT);
-        } else {
-          float sum = 0.f;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sum += s[r];
-          if (where < 0)
-            far_lo += sum;
-          else
-            far_hi += sum;
-        }
+      for (int r = 0; r < 16; ++r) {
+        s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
+        sum += s[r];
       }
       typename Tile::Probs p;
       Tile::pack(p, s);
@@ -159,54 +134,18 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
   }
   Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid, half);
 
-  if constexpr (BIAS) {
-    // by t over the waves and halves, then by bucket: a side's buckets are
-    // runs of t, and a thread sums one bucket's run (or two: t = 0 belongs to
-    // the first of the lower side)
-    far_lo = group_sum<64>(far_lo);
-    far_hi = group_sum<64>(far_hi);
-    __syncthreads();
-    for (int x = tid; x < span; x += 256) {
-      float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) v += sums[w * span + x];
-      tab[x] = v;
-    }
-    __syncthreads();
-    if (lane == 0) {
-      sums[2 * wave] = far_lo;
-      sums[2 * wave + 1] = far_hi;
-    }
-    __syncthreads();
-    const int lo = a.bias.lo, hi = a.bias.hi, side = a.bias.side;
-    for (int k = tid; k < a.bias.buckets; k += 256) {
-      float v = 0.f;
-      // distances [n0, n1) of the bucket; the last one of a side is open
-      const int u = k % side;
-      const bool ahead = k >= side, last = u == side - 1;
-      int n0 = u < a.bias.exact ? u : (u == a.bias.exact ? u : a.bias.border[u - a.bias.exact]);
-      int n1 = u < a.bias.exact ? u + 1
-                                : (last ? 0 : a.bias.border[u - a.bias.exact + 1]);
-      if (!ahead) {
-        // t from -(n1 - 1) to -n0, and for a one-sided table t >= 0 too
-        const int t1 = -n0, t0 = last ? lo - BIAS_PAD : -(n1 - 1);
-        for (int t = t0; t <= t1; ++t) v += tab[t - lo + BIAS_PAD];
-        if (last) v += (sums[0] + sums[2]) + (sums[4] + sums[6]);
-        if (!a.bias.bidirectional && u == 0) {
-          for (int t = 1; t <= hi + BIAS_PAD; ++t) v += tab[t - lo + BIAS_PAD];
-          v += (sums[1] + sums[3]) + (sums[5] + sums[7]);
-        }
-      } else {
-        const int t0 = max(n0, 1), t1 = last ? hi + BIAS_PAD : n1 - 1;
-        for (int t = t0; t <= t1; ++t) v += tab[t - lo + BIAS_PAD];
-        if (last) v += (sums[1] + sums[3]) + (sums[5] + sums[7]);
-      }
-      a.dbias_part[((int64_t(h) * a.B + b) * ntile + tile) * a.bias.buckets + k] = v;
-    }
+  // For the key pass: -lse, and D so that the row's dS sum to zero as they must.
+  // (O was formed from P rounded to bf16, which moves D by 2^-9 of its terms;
+  // a bias gradient, the sum of many dS of either sign, was off by 0.1%.)
+  nd -= half_sum(sum);
+  if (half == 0) {
+    const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i;
+    a.nlse[at] = nl;
+    a.ndelta[at] = nd;
   }
 }
 
-// Sums the query pass's partial bias gradients of one head in a fixed order.
+// Sums the key pass's partial bias gradients of one head in a fixed order.
 __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, float* dbias, int n,
                                                           int buckets, int heads) {
   __shared__ float sh[256];
@@ -235,6 +174,7 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
   constexpr int STAGE = 2 * IMG + 512;  // Q, dO, -lse and -D of a tile
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 2 * STAGE);
+  BiasSums sums;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
   const int nbk = a.B * a.kvh;
@@ -278,14 +218,28 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
     dk[d] = floatx16{};
     dv[d] = floatx16{};
   }
+  // the bias gradient's part of this workgroup's keys and head h
+  auto part = [&](int h) {
+    return a.dbias_part + ((int64_t(h) * a.B + b) * cross_tiles_d(a.Sk) + tile) * a.bias.buckets;
+  };
+  if constexpr (BIAS) {
+    sums.init(tab + bias_span(a.bias), a.bias, wave, half);
+    if (nt == 0)
+      for (int x = tid; x < a.group * a.bias.buckets; x += 256)
+        part(kv * a.group + x / a.bias.buckets)[x % a.bias.buckets] = 0.f;
+  }
   const float c = a.scale * LOG2E;
   for (int t = 0; t < nt; ++t) {
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < nt) issue(t + 1);
     if constexpr (BIAS) {
-      if (t % per == 0) {  // the next head's bias (every wave is past the last one's)
-        bias_spread(tab, a.bias, kv * a.group + t / per, a.nh, tid, 256);
+      if (t % per == 0) {  // the next head (every wave is past the last one's tiles)
+        const int h = kv * a.group + t / per;
+        if (t > 0) sums.flush(a.bias, part(h - 1), tid, lane, wave);
+        bias_spread(tab, a.bias, h, a.nh, tid, 256);
+        __syncthreads();
+        sums.clear(tid);
         __syncthreads();
       }
     }
@@ -311,17 +265,20 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
       }
       Tile::rows(dp, img + IMG, 32 * n, vf, lane);
       float ce = c, off = 0.f;
+      int side = 0, at = 0;  // -1, 1: in a constant side of the bias
       if constexpr (BIAS) {
         const int tb = w0 - start - i0 - 32 * n;  // the block spans [tb - 31, tb + 31]
         if (tb + 31 <= a.bias.lo) {
           off = tab[0];
+          side = -1;
         } else if (tb - 31 >= a.bias.hi) {
           off = tab[bias_span(a.bias) - 1];
+          side = 1;
         } else {
           ce = 1.f;
-          const float* p = tab + (tb + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD);
+          at = tb + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[-(8 * (r >> 2) + (r & 3))]);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, tab[at - (8 * (r >> 2) + (r & 3))]);
         }
       }
       if (a.causal && start + i0 + 32 * n < w0 + 31) {
@@ -337,9 +294,30 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
       Tile::cols(dv, img + IMG, 32 * n, p, lane);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] *= dp[r];
+      if constexpr (BIAS) {
+        // (a lane behind the sequence's keys holds what it read there)
+        if (j >= len) s = floatx16{};
+        if (side == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            __hip_atomic_fetch_add(sums.mine + at - (8 * (r >> 2) + (r & 3)), s[r],
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+        } else {
+          float x = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x += s[r];
+          if (side < 0)
+            sums.lo += x;
+          else
+            sums.hi += x;
+        }
+      }
       Tile::pack(p, s);
       Tile::cols(dk, img, 32 * n, p, lane);
     }
+  }
+  if constexpr (BIAS) {
+    if (nt > 0) sums.flush(a.bias, part(kv * a.group + a.group - 1), tid, lane, wave);
   }
   // keys behind the sequence's length: zero
   const bool valid = j < a.Sk;
@@ -357,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
 template <typename T, int D, bool BIAS>
 hipError_t run_q(const CrossArgs& a, hipStream_t s) {
   const size_t lds = size_t(4) * other_tile<T>() * D * sizeof(T) +
-                     (BIAS ? size_t(9) * bias_span_h(a.bias) * 4 : 0);
+                     (BIAS ? size_t(bias_span_h(a.bias)) * 4 : 0);
   hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS>>(160 * 1024);
   if (e != hipSuccess) return e;
   const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq);
@@ -368,7 +346,7 @@ hipError_t run_q(const CrossArgs& a, hipStream_t s) {
 template <typename T, int D, bool BIAS>
 hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
   const size_t lds = 2 * (size_t(2) * other_tile<T>() * D * sizeof(T) + 512) +
-                     (BIAS ? size_t(bias_span_h(a.bias)) * 4 : 0);
+                     (BIAS ? size_t(9) * bias_span_h(a.bias) * 4 : 0);
   hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS>>(160 * 1024);
   if (e != hipSuccess) return e;
   const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk);
@@ -392,7 +370,7 @@ hipError_t launch_cross_bwd_kv(const CrossArgs& a, int dtype, int D, hipStream_t
 
 hipError_t launch_cross_dbias(const CrossArgs& a, hipStream_t s) {
   cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
-      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sq), a.bias.buckets, a.nh);
+      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk), a.bias.buckets, a.nh);
   return hipGetLastError();
 }
 

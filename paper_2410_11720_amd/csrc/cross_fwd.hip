@@ -82,6 +82,13 @@ __device__ __forceinline__ void add_bias(floatx16& s, float c, const float* p) {
   for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[8 * (r >> 2) + (r & 3)]);
 }
 
+// Where the rest of an output row goes (null: nowhere; fp32 has none).
+template <typename T, int D>
+__device__ __forceinline__ char* rest_row(const CrossArgs& a, int b, int h, int i) {
+  if (sizeof(T) == 4 || a.rest == nullptr) return nullptr;
+  return a.rest + ((int64_t(b) * a.nh + h) * a.Sq + i) * D * 2;
+}
+
 template <typename T>
 constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
 
@@ -177,7 +184,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(CrossArgs a) {
   const float l = half_sum(on.l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
   char* op = a.o.p + b * a.o.b + h * a.o.h + int64_t(i) * a.o.t;
-  Tile::store_row(op, on.o, inv, valid, half);
+  Tile::store_row(op, on.o, inv, valid, half, rest_row<T, D>(a, b, h, i));
   if (a.lse && valid && half == 0)
     a.lse[(int64_t(b) * a.nh + h) * a.Sq + i] = l == 0.f ? NEG_INF : on.m + log2_hw(l);
 }
@@ -328,15 +335,19 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
     const int oi = out_row / a.group, oh = kv * a.group + out_row % a.group;
     const float inv = lt == 0.f ? 0.f : 1.f / lt;
     char* op = a.o.p + b * a.o.b + oh * a.o.h + int64_t(oi) * a.o.t + j0 * int(sizeof(T));
+    char* rp = rest_row<T, D>(a, b, oh, oi);
 #pragma unroll
     for (int e = 0; e < PER; e += 4) {
-      if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<u32x2*>(op + e * 2) =
-            u32x2{pack_bf16(acc[e] * inv, acc[e + 1] * inv),
-                  pack_bf16(acc[e + 2] * inv, acc[e + 3] * inv)};
-      else
-        *reinterpret_cast<floatx4*>(op + e * 4) = floatx4{
-            acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
+      const floatx4 x = {acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x2*>(op + e * 2) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        if (rp != nullptr)
+          *reinterpret_cast<u32x2*>(rp + (j0 + e) * 2) =
+              u32x2{pack_bf16(rounding_rest(x[0]), rounding_rest(x[1])),
+                    pack_bf16(rounding_rest(x[2]), rounding_rest(x[3]))};
+      } else {
+        *reinterpret_cast<floatx4*>(op + e * 4) = x;
+      }
     }
     if (a.lse && j0 == 0)
       a.lse[(int64_t(b) * a.nh + oh) * a.Sq + oi] = lt == 0.f ? NEG_INF : mm + log2_hw(lt);
@@ -381,8 +392,12 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   const int b = bk / a.kvh, h = (bk % a.kvh) * a.group + row % a.group, i = row / a.group;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* op = reinterpret_cast<T*>(a.o.p + b * a.o.b + h * a.o.h + int64_t(i) * a.o.t) + lane * PER;
+  T* rp = reinterpret_cast<T*>(rest_row<T, D>(a, b, h, i));
 #pragma unroll
-  for (int e = 0; e < PER; ++e) op[e] = Storage<T>::store(acc[e] * inv);
+  for (int e = 0; e < PER; ++e) {
+    op[e] = Storage<T>::store(acc[e] * inv);
+    if (rp != nullptr) rp[lane * PER + e] = Storage<T>::store(rounding_rest(acc[e] * inv));
+  }
   if (a.lse && lane == 0)
     a.lse[(int64_t(b) * a.nh + h) * a.Sq + i] = l == 0.f ? NEG_INF : m + log2_hw(l);
 }

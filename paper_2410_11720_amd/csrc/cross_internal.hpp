@@ -41,6 +41,7 @@ struct CrossArgs {
   const int32_t* k_lens = nullptr;         // [B] or null
   const int32_t* q_start = nullptr;        // [B] or null
   float* lse = nullptr;                    // [B][nh][Sq], base 2; may be null forward
+  char* rest = nullptr;                    // [B][nh][Sq][D]: what rounding took off O; may be null
   // short form: key splits and their partial results
   int splits = 1;
   float* part_o = nullptr;                 // [B][kvh][rows][splits][D]
@@ -48,8 +49,8 @@ struct CrossArgs {
   // backward
   int q_pad = 0;                           // Sq rounded up to the query tile
   float* nlse = nullptr;                   // [B][nh][q_pad]: -lse (-inf: no key)
-  float* ndelta = nullptr;                 // [B][nh][q_pad]: -dO . O
-  float* dbias_part = nullptr;             // [nh][B * query tiles][buckets]
+  float* ndelta = nullptr;                 // [B][nh][q_pad]: -D
+  float* dbias_part = nullptr;             // [nh][B * key tiles][buckets]
   float* dbias = nullptr;                  // [buckets][nh]
   CrossBias bias;
 };

@@ -52,6 +52,12 @@ __device__ __forceinline__ int seq_start(const CrossArgs& a, int b) {
   return a.q_start ? clampi(a.q_start[b], -(1 << 29), 1 << 29) : 0;
 }
 
+// x - bf16(x) (0 where that is not a number: x INF or NaN)
+__device__ __forceinline__ float rounding_rest(float x) {
+  const float r = x - bf2f(f2bf(x));
+  return r == r ? r : 0.f;
+}
+
 // 4 bytes per lane from the buffer to LDS [lds, lds + 256) in lane order.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
@@ -229,28 +235,26 @@ struct CrossTile {
   }
 
   // Stores a transposed result (lane: column l % 32 = one output row, rows
-  // = its elements) times f to `row`. bf16: the halves exchange 4-element
-  // groups first, so a lane stores 16 bytes.
+  // = its elements) times f to `row`, and what its rounding took off to `rest`
+  // if that is given. bf16: the halves exchange 4-element groups first, so a
+  // lane stores 16 bytes.
   __device__ static __forceinline__ void store_row(char* row, const floatx16 (&c)[ND], float f,
-                                                   bool valid, int half) {
+                                                   bool valid, int half, char* rest = nullptr) {
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       if constexpr (BF) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          u32x2 a = {pack_bf16(c[d][8 * k] * f, c[d][8 * k + 1] * f),
-                     pack_bf16(c[d][8 * k + 2] * f, c[d][8 * k + 3] * f)};
-          u32x2 b = {pack_bf16(c[d][8 * k + 4] * f, c[d][8 * k + 5] * f),
-                     pack_bf16(c[d][8 * k + 6] * f, c[d][8 * k + 7] * f)};
-          u32x4 o;
+          float x[8];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const auto x = __builtin_amdgcn_permlane32_swap(a[e], b[e], false, false);
-            o[e] = x[0];
-            o[2 + e] = x[1];
+          for (int e = 0; e < 8; ++e) x[e] = c[d][8 * k + e] * f;
+          const int at = (32 * d + 16 * k + 8 * half) * 2;
+          store8(row + at, x, valid);
+          if (rest != nullptr) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = rounding_rest(x[e]);
+            store8(rest + at, x, valid);
           }
-          if (valid)
-            *reinterpret_cast<u32x4*>(row + (32 * d + 16 * k + 8 * half) * 2) = o;
         }
       } else {
 #pragma unroll
@@ -261,6 +265,19 @@ struct CrossTile {
                         c[d][4 * k + 3] * f};
       }
     }
+  }
+  // 8 elements of a row from both halves' groups of 4
+  __device__ static __forceinline__ void store8(char* p, const float (&x)[8], bool valid) {
+    const u32x2 a = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    const u32x2 b = {pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+    u32x4 o;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const auto y = __builtin_amdgcn_permlane32_swap(a[e], b[e], false, false);
+      o[e] = y[0];
+      o[2 + e] = y[1];
+    }
+    if (valid) *reinterpret_cast<u32x4*>(p) = o;
   }
 };
 
@@ -302,6 +319,73 @@ __device__ __forceinline__ void bias_spread(float* tab, const CrossBias& b, int 
   for (int i = tid; i < n; i += nthreads)
     tab[i] = bias_entry(b.table[int64_t(bias_bucket(b, i + b.lo - BIAS_PAD)) * heads + head]);
 }
+
+// Sums of dS by t for the bias gradient: 8 arrays of bias_span entries, one for
+// each wave and half. The lanes of a half hold 32 keys and one query at a time,
+// so an addition never meets another one to the same entry, and the order of every
+// sum is fixed. What falls in a constant side is summed in registers.
+struct BiasSums {
+  float* arrays;
+  float* mine;
+  int span;
+  float lo, hi;
+
+  __device__ __forceinline__ void init(float* at, const CrossBias& b, int wave, int half) {
+    arrays = at;
+    span = bias_span(b);
+    mine = at + (2 * wave + half) * span;
+    lo = hi = 0.f;
+  }
+  __device__ __forceinline__ void clear(int tid) {
+    for (int x = tid; x < 8 * span; x += 256) arrays[x] = 0.f;
+    lo = hi = 0.f;
+  }
+  // Joins the arrays by t and writes the sum of every bucket. Called by the whole
+  // workgroup, whose arrays are then free (behind a barrier). A side's buckets are
+  // runs of t; a thread sums one bucket's run.
+  __device__ __forceinline__ void flush(const CrossBias& b, float* out, int tid, int lane,
+                                        int wave) {
+    lo = group_sum<64>(lo);
+    hi = group_sum<64>(hi);
+    __syncthreads();
+    for (int x = tid; x < span; x += 256) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) v += arrays[w * span + x];
+      arrays[x] = v;
+    }
+    __syncthreads();
+    float* ends = arrays + span;  // [4 waves][2]
+    if (lane == 0) {
+      ends[2 * wave] = lo;
+      ends[2 * wave + 1] = hi;
+    }
+    __syncthreads();
+    const float* tab = arrays + BIAS_PAD - b.lo;  // by t
+    for (int k = tid; k < b.buckets; k += 256) {
+      // distances [n0, n1) of the bucket; the last one of a side is open
+      const int u = k % b.side;
+      const bool ahead = k >= b.side, last = u == b.side - 1;
+      const int n0 = u <= b.exact ? u : b.border[u - b.exact];
+      const int n1 = last ? 0 : (u < b.exact ? u + 1 : b.border[u - b.exact + 1]);
+      float v = 0.f;
+      if (!ahead) {
+        const int t0 = last ? b.lo - BIAS_PAD : 1 - n1;
+        for (int t = t0; t <= -n0; ++t) v += tab[t];
+        if (last) v += (ends[0] + ends[2]) + (ends[4] + ends[6]);
+        if (!b.bidirectional && u == 0) {  // keys ahead share the bucket of t = 0
+          for (int t = 1; t <= b.hi + BIAS_PAD; ++t) v += tab[t];
+          v += (ends[1] + ends[3]) + (ends[5] + ends[7]);
+        }
+      } else {
+        const int t1 = last ? b.hi + BIAS_PAD : n1 - 1;
+        for (int t = max(n0, 1); t <= t1; ++t) v += tab[t];
+        if (last) v += (ends[1] + ends[3]) + (ends[5] + ends[7]);
+      }
+      out[k] = v;
+    }
+  }
+};
 
 }  // namespace
 }  // namespace abft

@@ -76,7 +76,7 @@ def _forward_status(cfg, q=None, k=None, o=None, bias=0, ws=1 << 20, ws_ptr=4096
     q, k = q or _c_tensor(4096, qs), k or _c_tensor(8192, ks)
     o = o or _c_tensor(4096, qs)
     return abft._lib.attn_cross_forward(c, q, k, _c_tensor(8192, ks), bias or None, None, None, o,
-                                        None, ws_ptr, ws, None)
+                                        None, None, ws_ptr, ws, None)
 
 
 def test_forward_refuses_before_any_launch():
