@@ -96,40 +96,50 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
     if (k0 >= wend) continue;
     const char* img = smem + (t & 1) * 2 * IMG;
     const bool masked = k0 + KT > len || (a.causal && k0 + KT - 1 > start + w0);
+    // rows of few keys (one tile) sum their dS first and correct D by it: there
+    // the rounding of single P shows in dq
+    for (int sweep = wend <= KT ? 0 : 1; sweep < 2; ++sweep) {
+      asm volatile("" ::: "memory");  // (reads of the image stay in the loop: they need registers)
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      floatx16 s = floatx16{}, dp;
-      Tile::rows(s, img, 32 * n, q, lane);
+      for (int n = 0; n < NB; ++n) {
+        floatx16 s = floatx16{}, dp;
+        Tile::rows(s, img, 32 * n, q, lane);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = nd;
-      Tile::rows(dp, img + IMG, 32 * n, g, lane);
-      float ce = c, off = nl;
-      if constexpr (BIAS) {
-        const int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
-        if (tb + 31 <= a.bias.lo) {
-          off += tab[0];
-        } else if (tb - 31 >= a.bias.hi) {
-          off += tab[bias_span(a.bias) - 1];
-        } else {
-          ce = 1.f;
-          const float* p = tab + (tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD);
+        for (int r = 0; r < 16; ++r) dp[r] = nd;
+        Tile::rows(dp, img + IMG, 32 * n, g, lane);
+        float ce = c, off = nl;
+        if constexpr (BIAS) {
+          const int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
+          if (tb + 31 <= a.bias.lo) {
+            off += tab[0];
+          } else if (tb - 31 >= a.bias.hi) {
+            off += tab[bias_span(a.bias) - 1];
+          } else {
+            ce = 1.f;
+            const float* p = tab + (tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[8 * (r >> 2) + (r & 3)]);
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[8 * (r >> 2) + (r & 3)]);
+          }
         }
-      }
-      if (masked) {
-        const int lim = limit - k0 - 32 * n - 4 * half;
+        if (masked) {
+          const int lim = limit - k0 - 32 * n - 4 * half;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < lim ? s[r] : NEG_INF;
-      }
+          for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < lim ? s[r] : NEG_INF;
+        }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
-        sum += s[r];
+        for (int r = 0; r < 16; ++r) {
+          s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
+          sum += s[r];
+        }
+        if (sweep == 0) continue;
+        typename Tile::Probs p;
+        Tile::pack(p, s);
+        Tile::cols(dq, img, 32 * n, p, lane);
       }
-      typename Tile::Probs p;
-      Tile::pack(p, s);
-      Tile::cols(dq, img, 32 * n, p, lane);
+      if (sweep == 0) {
+        nd -= half_sum(sum);
+        sum = 0.f;
+      }
     }
   }
   Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid, half);
@@ -166,14 +176,29 @@ __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, flo
 // S = Q K^T, so that a lane holds the scores of one key (its mask is a bound on
 // the query) and P and dS are the second operands of dV^T = dO^T P and
 // dK^T = Q^T dS from registers.
+// At head dim 128 the accumulators of both gradients and the keys' and values' own
+// fragments do not fit 256 registers beside the scores (36 spilled: the pass of
+// 4 x 2048 queries over 1024 keys, 32 heads on 8, 720 us). In bf16 the values' are
+// read from LDS and query tiles have 32 rows, so that two workgroups still share a
+// CU (410 us; one wave per SIMD with everything in registers: 420 us, and 25%
+// slower under a causal mask). fp32 runs one wave per SIMD.
+template <typename T, int D>
+constexpr bool v_in_lds() { return D == 128 && sizeof(T) == 2; }
+template <typename T, int D>
+constexpr int kv_tile() { return D * sizeof(T) == 128 ? 64 : 32; }
+template <typename T, int D>
+constexpr int kv_waves() { return D * sizeof(T) == 512 ? 1 : 2; }
+
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
+__global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int QT = other_tile<T>(), NB = QT / 32;
+  constexpr int QT = kv_tile<T, D>(), NB = QT / 32;
   constexpr int IMG = QT * Tile::ROWB;
   constexpr int STAGE = 2 * IMG + 512;  // Q, dO, -lse and -D of a tile
+  constexpr bool VLDS = v_in_lds<T, D>();
   extern __shared__ __align__(1024) char smem[];
-  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE);
+  const char* vimg = smem + 2 * STAGE;
+  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS ? CROSS_QT * Tile::ROWB : 0));
   BiasSums sums;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
@@ -204,13 +229,18 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
            uint32_t(min(lane, n - 1) * 4), 0u);
     }
   };
-  if (nt > 0) issue(0);
+  if (nt > 0) {
+    issue(0);
+    if constexpr (VLDS)
+      Tile::template issue<CROSS_QT, 4>(a.v.p + b * a.v.b + kv * a.v.h + int64_t(key0) * a.v.t,
+                                        a.v.t, len - key0, lds0 + 2 * STAGE, wave, lane);
+  }
 
   typename Tile::RowFrag kf, vf;
   const int jc = max(0, min(j, len - 1));
   if (nt > 0) {
     Tile::load_row(kf, a.k.p + b * a.k.b + kv * a.k.h + int64_t(jc) * a.k.t, half);
-    Tile::load_row(vf, a.v.p + b * a.v.b + kv * a.v.h + int64_t(jc) * a.v.t, half);
+    if constexpr (!VLDS) Tile::load_row(vf, a.v.p + b * a.v.b + kv * a.v.h + int64_t(jc) * a.v.t, half);
   }
   floatx16 dk[Tile::ND], dv[Tile::ND];
 #pragma unroll
@@ -223,7 +253,7 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
     return a.dbias_part + ((int64_t(h) * a.B + b) * cross_tiles_d(a.Sk) + tile) * a.bias.buckets;
   };
   if constexpr (BIAS) {
-    sums.init(tab + bias_span(a.bias), a.bias, wave, half);
+    sums.init(tab + bias_span(a.bias), a.bias, wave);
     if (nt == 0)
       for (int x = tid; x < a.group * a.bias.buckets; x += 256)
         part(kv * a.group + x / a.bias.buckets)[x % a.bias.buckets] = 0.f;
@@ -263,7 +293,10 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
           dp[r + e] = d[e];
         }
       }
-      Tile::rows(dp, img + IMG, 32 * n, vf, lane);
+      if constexpr (VLDS)
+        Tile::rows(dp, img + IMG, 32 * n, vimg, 32 * wave, lane);
+      else
+        Tile::rows(dp, img + IMG, 32 * n, vf, lane);
       float ce = c, off = 0.f;
       int side = 0, at = 0;  // -1, 1: in a constant side of the bias
       if constexpr (BIAS) {
@@ -276,9 +309,10 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
           side = 1;
         } else {
           ce = 1.f;
-          at = tb + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD;
+          at = tb;
+          const float* p = tab + (tb + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, tab[at - (8 * (r >> 2) + (r & 3))]);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[-(8 * (r >> 2) + (r & 3))]);
         }
       }
       if (a.causal && start + i0 + 32 * n < w0 + 31) {
@@ -298,10 +332,7 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_kv_kernel(CrossArgs a) {
         // (a lane behind the sequence's keys holds what it read there)
         if (j >= len) s = floatx16{};
         if (side == 0) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            __hip_atomic_fetch_add(sums.mine + at - (8 * (r >> 2) + (r & 3)), s[r],
-                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+          sums.add(a.bias, s, at, lane);
         } else {
           float x = 0.f;
 #pragma unroll
@@ -345,8 +376,9 @@ hipError_t run_q(const CrossArgs& a, hipStream_t s) {
 
 template <typename T, int D, bool BIAS>
 hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
-  const size_t lds = 2 * (size_t(2) * other_tile<T>() * D * sizeof(T) + 512) +
-                     (BIAS ? size_t(9) * bias_span_h(a.bias) * 4 : 0);
+  const size_t lds = 2 * (size_t(2) * kv_tile<T, D>() * D * sizeof(T) + 512) +
+                     (v_in_lds<T, D>() ? size_t(CROSS_QT) * D * sizeof(T) : 0) +
+                     (BIAS ? size_t(5) * bias_span_h(a.bias) * 4 : 0);
   hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS>>(160 * 1024);
   if (e != hipSuccess) return e;
   const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk);

@@ -176,6 +176,30 @@ struct CrossTile {
     }
   }
 
+  // The same with B's columns the rows [at, at + 32) of an image.
+  __device__ static __forceinline__ void rows(floatx16& c, const char* img, int row0,
+                                              const char* own, int at, int lane) {
+    const int r = lane & 31, half = lane >> 5;
+    const char* p = img + (row0 + r) * ROWB;
+    const char* q = own + (at + r) * ROWB;
+    const int sw = swz(r);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      const int ch = ((2 * f + half) ^ sw) << 4;
+      const u32x4 a = *reinterpret_cast<const u32x4*>(p + ch);
+      const u32x4 b = *reinterpret_cast<const u32x4*>(q + ch);
+      if constexpr (BF) {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c,
+                                                   0, 0, 0);
+      }
+    }
+  }
+
   // P as the second operand of `cols`: bf16 rounds it (the products take
   // bf16 operands and sum in fp32), fp32 keeps it
   struct Probs {
@@ -320,25 +344,96 @@ __device__ __forceinline__ void bias_spread(float* tab, const CrossBias& b, int 
     tab[i] = bias_entry(b.table[int64_t(bias_bucket(b, i + b.lo - BIAS_PAD)) * heads + head]);
 }
 
-// Sums of dS by t for the bias gradient: 8 arrays of bias_span entries, one for
-// each wave and half. The lanes of a half hold 32 keys and one query at a time,
-// so an addition never meets another one to the same entry, and the order of every
-// sum is fixed. What falls in a constant side is summed in registers.
+// x of the lane n to the right (left) in its row of 16 lanes, 0 past the end.
+template <int N>
+__device__ __forceinline__ float row_left(float x) {
+  if constexpr (N == 0) return x;
+  else return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+      0, __builtin_bit_cast(int, x), 0x100 + N, 0xf, 0xf, true));
+}
+template <int N>
+__device__ __forceinline__ float row_right(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+      0, __builtin_bit_cast(int, x), 0x110 + N, 0xf, 0xf, true));
+}
+
+// Sums of a 32 x 32 block (lane: column l % 32, register r: row 8 (r / 4) +
+// 4 half + r % 4) along its diagonals: lane u gets the sum of all elements with
+// column - row = u - 32. A row is shifted onto the first one inside each 16
+// lanes, what falls off goes to the next 16 diagonals down; then the halves (4
+// rows apart) and the 16-column groups are joined. About 50 vector
+// instructions; adding each element to its sum in LDS took 16 LDS atomics of
+// some 250 cycles.
+template <int R>
+__device__ __forceinline__ void diag_row(float (&x)[3], float s) {
+  constexpr int M = R / 16, N = R % 16;
+  x[M] += row_left<N>(s);
+  if constexpr (N > 0) x[M + 1] += row_right<16 - N>(s);
+}
+__device__ __forceinline__ float diagonal_sums(const floatx16& s, int lane) {
+  float x[3] = {0.f, 0.f, 0.f};
+  diag_row<0>(x, s[0]);
+  diag_row<1>(x, s[1]);
+  diag_row<2>(x, s[2]);
+  diag_row<3>(x, s[3]);
+  diag_row<8>(x, s[4]);
+  diag_row<9>(x, s[5]);
+  diag_row<10>(x, s[6]);
+  diag_row<11>(x, s[7]);
+  diag_row<16>(x, s[8]);
+  diag_row<17>(x, s[9]);
+  diag_row<18>(x, s[10]);
+  diag_row<19>(x, s[11]);
+  diag_row<24>(x, s[12]);
+  diag_row<25>(x, s[13]);
+  diag_row<26>(x, s[14]);
+  diag_row<27>(x, s[15]);
+  // x[m] of half h and column group g: diagonal 16 g + lane % 16 - 16 m - 4 h
+  float y[3], fall = 0.f;
+#pragma unroll
+  for (int m = 0; m < 3; ++m) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[m]), __float_as_uint(x[m]),
+                                                    false, false);
+    const float up = __uint_as_float(r[1]);
+    y[m] = __uint_as_float(r[0]) + row_left<4>(up) + fall;
+    fall = row_right<12>(up);
+  }
+  const int G = lane >> 4;
+  float v = 0.f;
+#pragma unroll
+  for (int m = 0; m < 3; ++m) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(y[m]), __float_as_uint(y[m]),
+                                                    false, false);
+    v += G == 2 - m ? __uint_as_float(r[0]) : 0.f;
+    v += G == 3 - m ? __uint_as_float(r[1]) : 0.f;
+  }
+  return v;
+}
+
+// Sums of dS by t for the bias gradient, an array of bias_span entries for each
+// wave: every sum's order is fixed. What falls in a constant side is summed in
+// registers.
 struct BiasSums {
   float* arrays;
   float* mine;
   int span;
   float lo, hi;
 
-  __device__ __forceinline__ void init(float* at, const CrossBias& b, int wave, int half) {
+  __device__ __forceinline__ void init(float* at, const CrossBias& b, int wave) {
     arrays = at;
     span = bias_span(b);
-    mine = at + (2 * wave + half) * span;
+    mine = at + wave * span;
     lo = hi = 0.f;
   }
   __device__ __forceinline__ void clear(int tid) {
-    for (int x = tid; x < 8 * span; x += 256) arrays[x] = 0.f;
+    for (int x = tid; x < 4 * span; x += 256) arrays[x] = 0.f;
     lo = hi = 0.f;
+  }
+  // Adds a block (lane: key, registers: queries) whose corner (first key, first
+  // query) has t = tb, inside (lo - 31, hi + 31).
+  __device__ __forceinline__ void add(const CrossBias& b, const floatx16& s, int tb, int lane) {
+    const float v = diagonal_sums(s, lane);
+    if (lane > 0) mine[tb - 32 + lane - b.lo + BIAS_PAD] += v;
   }
   // Joins the arrays by t and writes the sum of every bucket. Called by the whole
   // workgroup, whose arrays are then free (behind a barrier). A side's buckets are
@@ -351,7 +446,7 @@ struct BiasSums {
     for (int x = tid; x < span; x += 256) {
       float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) v += arrays[w * span + x];
+      for (int w = 0; w < 4; ++w) v += arrays[w * span + x];
       arrays[x] = v;
     }
     __syncthreads();
