@@ -68,7 +68,7 @@ int validate(const attn_cross_config* c, CrossBias* bias) {
   if (c->q_len > MAX_LEN || c->k_len > MAX_LEN) return ABFT_ERR_UNSUPPORTED;
   const int64_t wgs = int64_t(c->batch) * c->heads;
   if (wgs > (int64_t(1) << 24) ||
-      wgs * std::max(cross_tiles(c->q_len), cross_tiles(c->k_len)) > (int64_t(1) << 30))
+      wgs * cross_tiles(std::max(c->q_len, c->k_len), CROSS_QMIN) > (int64_t(1) << 30))
     return ABFT_ERR_UNSUPPORTED;
   if (c->buckets && !make_bias(c->buckets, c->max_distance, c->bidirectional, bias))
     return ABFT_ERR_INVALID;
@@ -105,10 +105,11 @@ Space make_space(const attn_cross_config* c) {
     L.part_ml = align_up(n * c->head_dim * 4);
     L.fwd = L.part_ml + align_up(n * 8);
   }
-  const size_t rows = size_t(c->batch) * c->heads * cross_tiles(c->q_len) * CROSS_QT;
+  const size_t rows = size_t(c->batch) * c->heads * cross_tiles(c->q_len, CROSS_QT) * CROSS_QT;
   L.ndelta = align_up(rows * 4);
   L.dbias = 2 * L.ndelta;
-  L.bwd = L.dbias + align_up(size_t(c->batch) * c->heads * cross_tiles(c->k_len) * c->buckets * 4);
+  L.bwd = L.dbias + align_up(size_t(c->batch) * c->heads *
+                              cross_tiles(c->k_len, CROSS_QMIN) * c->buckets * 4);
   return L;
 }
 
@@ -258,15 +259,17 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
   a.lse = const_cast<float*>(lse);
   a.rest = static_cast<char*>(const_cast<void*>(rest));
   char* ws = static_cast<char*>(workspace);
-  a.q_pad = cross_tiles(cfg->q_len) * CROSS_QT;
+  a.q_pad = cross_tiles(cfg->q_len, CROSS_QT) * CROSS_QT;
   a.nlse = reinterpret_cast<float*>(ws);
   a.ndelta = reinterpret_cast<float*>(ws + L.ndelta);
   a.dbias_part = reinterpret_cast<float*>(ws + L.dbias);
   a.dbias = dbias;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (any_q) CK(launch_cross_bwd_q(a, cfg->dtype, cfg->head_dim, s));
-  if (any_k) CK(launch_cross_bwd_kv(a, cfg->dtype, cfg->head_dim, s));
-  if (cfg->buckets) CK(launch_cross_dbias(a, s));
+  if (any_k)
+    CK(launch_cross_bwd_kv(a, cfg->dtype, cfg->head_dim, s));
+  else if (cfg->buckets)
+    CK(launch_cross_no_keys(a, s));
   return ABFT_OK;
 }
 

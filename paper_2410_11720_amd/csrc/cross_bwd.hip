@@ -8,8 +8,8 @@
 //
 // Two passes, each of which owns what it sums (no atomics on memory, so
 // results do not depend on the order of workgroups): the query pass owns 128
-// queries and runs over the keys (dq; it leaves -lse and -D for the other),
-// the key pass owns 128 keys and runs over the queries of all heads that share
+// queries (or 64) and runs over the keys (dq; it leaves -lse and -D for the other),
+// the key pass owns 128 keys (or 64) and runs over the queries of all heads that share
 // them (dk, dv, dtable). The price is a second S and dP (14 d flops a pair
 // against 10 d in one pass).
 #include "cross_tile.hpp"
@@ -21,8 +21,8 @@ template <typename T>
 constexpr int other_tile() { return sizeof(T) == 2 ? 64 : 32; }
 
 // ---- query pass -----------------------------------------------------------
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
+template <typename T, int D, bool BIAS, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void cross_bwd_q_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
   constexpr int KT = other_tile<T>(), NB = KT / 32;
   constexpr int IMG = KT * Tile::ROWB;
@@ -30,15 +30,15 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
-  const int nbk = a.B * a.kvh, ntile = cross_tiles_d(a.Sq);
+  const int nbk = a.B * a.kvh, ntile = cross_tiles(a.Sq, 32 * NW);
   const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
   const int b = bk / a.kvh, kv = bk % a.kvh, h = kv * a.group + y % a.group;
   int tile = y / a.group;
   if (a.causal) tile = ntile - 1 - tile;
-  const int q0 = tile * CROSS_QT;
+  const int q0 = tile * 32 * NW;
   const int len = seq_len(a, b), start = seq_start(a, b);
   int kend = len;
-  if (a.causal) kend = min(kend, start + min(q0 + CROSS_QT, a.Sq));
+  if (a.causal) kend = min(kend, start + min(q0 + 32 * NW, a.Sq));
   kend = max(kend, 0);
   const int nt = (kend + KT - 1) / KT;
   const int w0 = q0 + 32 * wave, i = w0 + (lane & 31), ic = min(i, a.Sq - 1);
@@ -53,8 +53,8 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
   const uint32_t lds0 = lds_addr(smem);
   auto issue = [&](int t) {
     const uint32_t to = lds0 + (t & 1) * 2 * IMG;
-    Tile::template issue<KT, 4>(kp + int64_t(t) * KT * a.k.t, a.k.t, len - t * KT, to, wave, lane);
-    Tile::template issue<KT, 4>(vp + int64_t(t) * KT * a.v.t, a.v.t, len - t * KT, to + IMG, wave,
+    Tile::template issue<KT, NW>(kp + int64_t(t) * KT * a.k.t, a.k.t, len - t * KT, to, wave, lane);
+    Tile::template issue<KT, NW>(vp + int64_t(t) * KT * a.v.t, a.v.t, len - t * KT, to + IMG, wave,
                                 lane);
   };
   if (nt > 0) issue(0);
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, 2) void cross_bwd_q_kernel(CrossArgs a) {
       Tile::zero_row(g);
     }
   }
-  if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 256);
+  if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
   float sum = 0.f;  // of the row's dS
 
   floatx16 dq[Tile::ND];
@@ -176,37 +176,45 @@ __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, flo
 // S = Q K^T, so that a lane holds the scores of one key (its mask is a bound on
 // the query) and P and dS are the second operands of dV^T = dO^T P and
 // dK^T = Q^T dS from registers.
+// A workgroup has KW x QH waves: KW times 32 keys, and QH waves on the same keys
+// that take the 32-row blocks of a query tile in turn and join their sums at
+// the end.
 // At head dim 128 the accumulators of both gradients and the keys' and values' own
 // fragments do not fit 256 registers beside the scores (36 spilled: the pass of
 // 4 x 2048 queries over 1024 keys, 32 heads on 8, 720 us). In bf16 the values' are
-// read from LDS and query tiles have 32 rows, so that two workgroups still share a
-// CU (410 us; one wave per SIMD with everything in registers: 420 us, and 25%
-// slower under a causal mask). fp32 runs one wave per SIMD.
+// read from LDS, and there is one workgroup of 8 waves a CU. fp32 runs one wave per
+// SIMD.
 template <typename T, int D>
-constexpr bool v_in_lds() { return D == 128 && sizeof(T) == 2; }
-template <typename T, int D>
-constexpr int kv_tile() { return D * sizeof(T) == 128 ? 64 : 32; }
-template <typename T, int D>
-constexpr int kv_waves() { return D * sizeof(T) == 512 ? 1 : 2; }
+struct KvShape {
+  static constexpr bool WIDE = D * int(sizeof(T)) == 256 && sizeof(T) == 2;
+  static constexpr int QH = WIDE ? 2 : 1;
+  static constexpr int QT = sizeof(T) == 2 ? 64 : 32;  // rows of a query tile
+  static constexpr int NB = QT / 32 / QH;              // blocks of it a wave takes
+  static constexpr bool VLDS = WIDE;
+  static constexpr int PER_SIMD = D * int(sizeof(T)) == 512 ? 1 : 2;
+};
 
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(CrossArgs a) {
+template <typename T, int D, bool BIAS, int KW>
+__global__ __launch_bounds__((64 * KW * KvShape<T, D>::QH), (KvShape<T, D>::PER_SIMD)) void
+cross_bwd_kv_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int QT = kv_tile<T, D>(), NB = QT / 32;
+  using Shape = KvShape<T, D>;
+  constexpr int QT = Shape::QT, NB = Shape::NB, QH = Shape::QH, NW = KW * QH, KEYS = 32 * KW;
   constexpr int IMG = QT * Tile::ROWB;
   constexpr int STAGE = 2 * IMG + 512;  // Q, dO, -lse and -D of a tile
-  constexpr bool VLDS = v_in_lds<T, D>();
+  constexpr bool VLDS = Shape::VLDS;
   extern __shared__ __align__(1024) char smem[];
   const char* vimg = smem + 2 * STAGE;
-  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS ? CROSS_QT * Tile::ROWB : 0));
-  BiasSums sums;
+  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS ? KEYS * Tile::ROWB : 0));
+  BiasSums<NW> sums;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
   const int nbk = a.B * a.kvh;
   const int bk = blockIdx.x % nbk, tile = blockIdx.x / nbk;  // causal: heaviest first
   const int b = bk / a.kvh, kv = bk % a.kvh;
   const int len = seq_len(a, b), start = seq_start(a, b);
-  const int key0 = tile * CROSS_QT, w0 = key0 + 32 * wave, j = w0 + (lane & 31);
+  const int kw = wave % KW, qh = wave / KW;
+  const int key0 = tile * KEYS, w0 = key0 + 32 * kw, j = w0 + (lane & 31);
   // query tiles that see the workgroup's keys, of each head of the group
   int first = 0;
   if (a.causal) first = max(0, key0 - start) / QT;
@@ -218,9 +226,9 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
   auto issue = [&](int t) {
     const int h = kv * a.group + t / per, i0 = (first + t % per) * QT;
     const uint32_t to = lds0 + (t & 1) * STAGE;
-    Tile::template issue<QT, 4>(a.q.p + b * a.q.b + h * a.q.h + int64_t(i0) * a.q.t, a.q.t,
+    Tile::template issue<QT, NW>(a.q.p + b * a.q.b + h * a.q.h + int64_t(i0) * a.q.t, a.q.t,
                                 a.Sq - i0, to, wave, lane);
-    Tile::template issue<QT, 4>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
+    Tile::template issue<QT, NW>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
                                 a.dout.t, a.Sq - i0, to + IMG, wave, lane);
     const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i0;
     if (wave < 2) {  // (64 values; a 32-row tile uses half of them)
@@ -232,7 +240,7 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
   if (nt > 0) {
     issue(0);
     if constexpr (VLDS)
-      Tile::template issue<CROSS_QT, 4>(a.v.p + b * a.v.b + kv * a.v.h + int64_t(key0) * a.v.t,
+      Tile::template issue<KEYS, NW>(a.v.p + b * a.v.b + kv * a.v.h + int64_t(key0) * a.v.t,
                                         a.v.t, len - key0, lds0 + 2 * STAGE, wave, lane);
   }
 
@@ -250,12 +258,12 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
   }
   // the bias gradient's part of this workgroup's keys and head h
   auto part = [&](int h) {
-    return a.dbias_part + ((int64_t(h) * a.B + b) * cross_tiles_d(a.Sk) + tile) * a.bias.buckets;
+    return a.dbias_part + ((int64_t(h) * a.B + b) * cross_tiles(a.Sk, KEYS) + tile) * a.bias.buckets;
   };
   if constexpr (BIAS) {
     sums.init(tab + bias_span(a.bias), a.bias, wave);
     if (nt == 0)
-      for (int x = tid; x < a.group * a.bias.buckets; x += 256)
+      for (int x = tid; x < a.group * a.bias.buckets; x += 64 * NW)
         part(kv * a.group + x / a.bias.buckets)[x % a.bias.buckets] = 0.f;
   }
   const float c = a.scale * LOG2E;
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
       if (t % per == 0) {  // the next head (every wave is past the last one's tiles)
         const int h = kv * a.group + t / per;
         if (t > 0) sums.flush(a.bias, part(h - 1), tid, lane, wave);
-        bias_spread(tab, a.bias, h, a.nh, tid, 256);
+        bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
         __syncthreads();
         sums.clear(tid);
         __syncthreads();
@@ -279,7 +287,8 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
     const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
     const float* nds = nls + 64;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
+    for (int m = 0; m < NB; ++m) {
+      const int n = m * QH + qh;
       floatx16 s = floatx16{}, dp, nl;
       Tile::rows(s, img, 32 * n, kf, lane);
 #pragma unroll
@@ -294,7 +303,7 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
         }
       }
       if constexpr (VLDS)
-        Tile::rows(dp, img + IMG, 32 * n, vimg, 32 * wave, lane);
+        Tile::rows(dp, img + IMG, 32 * n, vimg, 32 * kw, lane);
       else
         Tile::rows(dp, img + IMG, 32 * n, vf, lane);
       float ce = c, off = 0.f;
@@ -350,6 +359,26 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
   if constexpr (BIAS) {
     if (nt > 0) sums.flush(a.bias, part(kv * a.group + a.group - 1), tid, lane, wave);
   }
+  if constexpr (QH == 2) {
+    // the second half's sums to the first, one gradient after the other
+    float* box = reinterpret_cast<float*>(smem) + kw * 64 * 16 * Tile::ND + lane;
+    static_assert(KW * 64 * 16 * Tile::ND * 4 <= 2 * STAGE, "the tiles' space holds a gradient");
+    auto join = [&](floatx16(&x)[Tile::ND]) {
+      __syncthreads();
+      if (qh == 1) {
+#pragma unroll
+        for (int e = 0; e < 16 * Tile::ND; ++e) box[64 * e] = x[e / 16][e % 16];
+      }
+      __syncthreads();
+      if (qh == 0) {
+#pragma unroll
+        for (int e = 0; e < 16 * Tile::ND; ++e) x[e / 16][e % 16] += box[64 * e];
+      }
+    };
+    join(dk);
+    join(dv);
+    if (qh == 1) return;
+  }
   // keys behind the sequence's length: zero
   const bool valid = j < a.Sk;
   if (j >= len) {
@@ -363,26 +392,37 @@ __global__ __launch_bounds__(256, (kv_waves<T, D>())) void cross_bwd_kv_kernel(C
   Tile::store_row(a.dv.p + b * a.dv.b + kv * a.dv.h + int64_t(j) * a.dv.t, dv, 1.f, valid, half);
 }
 
-template <typename T, int D, bool BIAS>
+template <typename T, int D, bool BIAS, int NW>
 hipError_t run_q(const CrossArgs& a, hipStream_t s) {
   const size_t lds = size_t(4) * other_tile<T>() * D * sizeof(T) +
                      (BIAS ? size_t(bias_span_h(a.bias)) * 4 : 0);
-  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS>>(160 * 1024);
+  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS, NW>>(160 * 1024);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq);
-  cross_bwd_q_kernel<T, D, BIAS><<<dim3(uint32_t(grid)), 256, lds, s>>>(a);
+  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NW);
+  cross_bwd_q_kernel<T, D, BIAS, NW><<<dim3(uint32_t(grid)), 64 * NW, lds, s>>>(a);
   return hipGetLastError();
 }
 
-template <typename T, int D, bool BIAS>
+// Keys a workgroup of the key pass owns, in 32s.
+template <typename T, int D>
+int kv_waves(const CrossArgs& a) {
+  return KvShape<T, D>::QH == 2 ? 4 : cross_waves(int64_t(a.B) * a.kvh, a.Sk);
+}
+
+template <typename T, int D, bool BIAS, int KW>
 hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
-  const size_t lds = 2 * (size_t(2) * kv_tile<T, D>() * D * sizeof(T) + 512) +
-                     (v_in_lds<T, D>() ? size_t(CROSS_QT) * D * sizeof(T) : 0) +
-                     (BIAS ? size_t(5) * bias_span_h(a.bias) * 4 : 0);
-  hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS>>(160 * 1024);
+  using Shape = KvShape<T, D>;
+  const size_t lds = 2 * (size_t(2) * Shape::QT * D * sizeof(T) + 512) +
+                     (Shape::VLDS ? size_t(32) * KW * D * sizeof(T) : 0) +
+                     (BIAS ? size_t(KW * Shape::QH + 1) * bias_span_h(a.bias) * 4 : 0);
+  hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS, KW>>(160 * 1024);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk);
-  cross_bwd_kv_kernel<T, D, BIAS><<<dim3(uint32_t(grid)), 256, lds, s>>>(a);
+  const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk, 32 * KW);
+  cross_bwd_kv_kernel<T, D, BIAS, KW>
+      <<<dim3(uint32_t(grid)), 64 * KW * Shape::QH, lds, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || !BIAS) return e;
+  cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
+      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk, 32 * KW), a.bias.buckets, a.nh);
   return hipGetLastError();
 }
 
@@ -390,19 +430,29 @@ hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
 
 hipError_t launch_cross_bwd_q(const CrossArgs& a, int dtype, int D, hipStream_t s) {
   return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
-    return run_q<typename decltype(t)::type, decltype(d)::value, decltype(bias)::value>(a, s);
+    using T = typename decltype(t)::type;
+    constexpr int DD = decltype(d)::value;
+    constexpr bool BIAS = decltype(bias)::value;
+    return cross_waves(int64_t(a.B) * a.nh, a.Sq) == 2 ? run_q<T, DD, BIAS, 2>(a, s)
+                                                       : run_q<T, DD, BIAS, 4>(a, s);
   });
 }
 
 hipError_t launch_cross_bwd_kv(const CrossArgs& a, int dtype, int D, hipStream_t s) {
   return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
-    return run_kv<typename decltype(t)::type, decltype(d)::value, decltype(bias)::value>(a, s);
+    using T = typename decltype(t)::type;
+    constexpr int DD = decltype(d)::value;
+    constexpr bool BIAS = decltype(bias)::value;
+    if constexpr (KvShape<T, DD>::QH == 2)
+      return run_kv<T, DD, BIAS, 4>(a, s);
+    else
+      return kv_waves<T, DD>(a) == 2 ? run_kv<T, DD, BIAS, 2>(a, s) : run_kv<T, DD, BIAS, 4>(a, s);
   });
 }
 
-hipError_t launch_cross_dbias(const CrossArgs& a, hipStream_t s) {
-  cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
-      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk), a.bias.buckets, a.nh);
+hipError_t launch_cross_no_keys(const CrossArgs& a, hipStream_t s) {
+  cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(a.dbias_part, a.dbias, 0, a.bias.buckets,
+                                                          a.nh);
   return hipGetLastError();
 }
 

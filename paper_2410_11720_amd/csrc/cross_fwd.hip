@@ -92,11 +92,11 @@ __device__ __forceinline__ char* rest_row(const CrossArgs& a, int b, int h, int 
 template <typename T>
 constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
 
-// Tiled form: a workgroup owns 128 queries of one head, a wave 32 of them; key
+// Tiled form: a workgroup owns 32 NW queries of one head, a wave 32 of them; key
 // tiles of 64 (fp32: 32) pass through LDS in two stages, the next one copied
 // while this one is worked on.
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void cross_fwd_kernel(CrossArgs a) {
+template <typename T, int D, bool BIAS, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void cross_fwd_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
   constexpr int KT = key_tile<T>(), NB = KT / 32;
   constexpr int IMG = KT * Tile::ROWB;
@@ -110,11 +110,11 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(CrossArgs a) {
   const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
   const int b = bk / a.kvh, kv = bk % a.kvh, h = kv * a.group + y % a.group;
   int tile = y / a.group;
-  if (a.causal) tile = cross_tiles_d(a.Sq) - 1 - tile;
-  const int q0 = tile * CROSS_QT;
+  if (a.causal) tile = cross_tiles(a.Sq, 32 * NW) - 1 - tile;
+  const int q0 = tile * 32 * NW;
   const int len = seq_len(a, b), start = seq_start(a, b);
   int kend = len;
-  if (a.causal) kend = min(kend, start + min(q0 + CROSS_QT, a.Sq));
+  if (a.causal) kend = min(kend, start + min(q0 + 32 * NW, a.Sq));
   kend = max(kend, 0);
   const int nt = (kend + KT - 1) / KT;
 
@@ -131,15 +131,15 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(CrossArgs a) {
   const uint32_t lds0 = lds_addr(smem);
   auto issue = [&](int t) {
     const uint32_t to = lds0 + (t & 1) * 2 * IMG;
-    Tile::template issue<KT, 4>(kp + int64_t(t) * KT * a.k.t, a.k.t, len - t * KT, to, wave, lane);
-    Tile::template issue<KT, 4>(vp + int64_t(t) * KT * a.v.t, a.v.t, len - t * KT, to + IMG, wave,
+    Tile::template issue<KT, NW>(kp + int64_t(t) * KT * a.k.t, a.k.t, len - t * KT, to, wave, lane);
+    Tile::template issue<KT, NW>(vp + int64_t(t) * KT * a.v.t, a.v.t, len - t * KT, to + IMG, wave,
                                 lane);
   };
   if (nt > 0) issue(0);
 
   typename Tile::RowFrag q;
   Tile::load_row(q, a.q.p + b * a.q.b + h * a.q.h + int64_t(min(i, a.Sq - 1)) * a.q.t, half);
-  if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 256);
+  if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
 
   Online<T, D> on;
   on.init();
@@ -402,14 +402,14 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
     a.lse[(int64_t(b) * a.nh + h) * a.Sq + i] = l == 0.f ? NEG_INF : m + log2_hw(l);
 }
 
-template <typename T, int D, bool BIAS>
+template <typename T, int D, bool BIAS, int NW>
 hipError_t run_fwd(const CrossArgs& a, hipStream_t s) {
   constexpr int KT = key_tile<T>();
   const size_t lds = size_t(4) * KT * D * sizeof(T) + (BIAS ? bias_span_h(a.bias) * 4 : 0);
-  hipError_t e = lds_limit<cross_fwd_kernel<T, D, BIAS>>(160 * 1024);
+  hipError_t e = lds_limit<cross_fwd_kernel<T, D, BIAS, NW>>(160 * 1024);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq);
-  cross_fwd_kernel<T, D, BIAS><<<dim3(uint32_t(grid)), 256, lds, s>>>(a);
+  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NW);
+  cross_fwd_kernel<T, D, BIAS, NW><<<dim3(uint32_t(grid)), 64 * NW, lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -432,7 +432,11 @@ hipError_t run_short(const CrossArgs& a, hipStream_t s) {
 
 hipError_t launch_cross_fwd(const CrossArgs& a, int dtype, int D, hipStream_t s) {
   return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
-    return run_fwd<typename decltype(t)::type, decltype(d)::value, decltype(bias)::value>(a, s);
+    using T = typename decltype(t)::type;
+    constexpr int D = decltype(d)::value;
+    constexpr bool BIAS = decltype(bias)::value;
+    return cross_waves(int64_t(a.B) * a.nh, a.Sq) == 2 ? run_fwd<T, D, BIAS, 2>(a, s)
+                                                       : run_fwd<T, D, BIAS, 4>(a, s);
   });
 }
 

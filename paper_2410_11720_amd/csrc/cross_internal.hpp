@@ -55,9 +55,19 @@ struct CrossArgs {
   CrossBias bias;
 };
 
-constexpr int CROSS_QT = 128;  // queries (keys) a workgroup owns in the tiled kernels
+constexpr int CROSS_QT = 128;  // queries (keys) a workgroup owns at most in the tiled kernels
+constexpr int CROSS_QMIN = 64;  // and at least
 
-inline int cross_tiles(int n) { return (n + CROSS_QT - 1) / CROSS_QT; }
+constexpr int cross_tiles(int n, int tile) { return (n + tile - 1) / tile; }
+
+// Waves of 32 queries (keys) a workgroup has, 4 or 2, for n of them and `heads`
+// (batch, head) pairs: those that leave the fullest CU with fewer waves. (96
+// heads x 512 queries in fours are 384 workgroups, two on every other CU; in
+// twos they are three everywhere.) In fours a tile's copies serve more queries.
+inline int cross_waves(int64_t heads, int n) {
+  auto load = [&](int w) { return (heads * cross_tiles(n, 32 * w) + 255) / 256 * w; };
+  return load(2) < load(4) ? 2 : 4;
+}
 
 // Entries of the spread bias table in LDS.
 constexpr int CROSS_BIAS_PAD = 63;
@@ -82,6 +92,6 @@ hipError_t launch_cross_fwd(const CrossArgs& a, int dtype, int D, hipStream_t s)
 hipError_t launch_cross_short(const CrossArgs& a, int dtype, int D, hipStream_t s);
 hipError_t launch_cross_bwd_q(const CrossArgs& a, int dtype, int D, hipStream_t s);
 hipError_t launch_cross_bwd_kv(const CrossArgs& a, int dtype, int D, hipStream_t s);
-hipError_t launch_cross_dbias(const CrossArgs& a, hipStream_t s);
+hipError_t launch_cross_no_keys(const CrossArgs& a, hipStream_t s);  // a bias gradient of zeros
 
 }  // namespace abft

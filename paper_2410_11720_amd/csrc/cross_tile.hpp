@@ -41,7 +41,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
-__device__ __forceinline__ int cross_tiles_d(int n) { return (n + CROSS_QT - 1) / CROSS_QT; }
 
 // Keys of a sequence, and the position of its first query among them (values
 // that the host cannot check are brought into range here).
@@ -72,9 +71,12 @@ __device__ __forceinline__ void dma4(const u32x4& rs, uint32_t lds, uint32_t vof
 #pragma clang diagnostic pop
 
 // A tile of rows of D elements in LDS, row-major, 16-byte chunk c of row r at
-// chunk c ^ swz(r). Both ways a tile is read are free of bank conflicts: the
-// 8 rows that a 16-byte read of one chunk serves together hit 8 chunks, and
-// the 4 rows that a transposing read serves together hit 4 pairs of chunks.
+// chunk c ^ swz(r). LDS serves 256 bytes, a run of 16 chunks, at a time: the 16
+// rows that share a step of a 16-byte read of one chunk lie at 16 places of
+// it in bf16, and so do the 4 rows x 4 chunks of a transposing read. (With the 8
+// places that a swizzle of three bits reaches, half of all LDS cycles were
+// conflicts. fp32 keeps to three bits: its products take 16 times as long as their
+// reads, and longer periods cost registers.)
 //
 // Products (32 x 32 tiles, lane l: column l % 32, half = l / 32):
 //  rows  C[32 rows x 32] += tile rows . B, B's column the lane's own vector of
@@ -89,11 +91,15 @@ struct CrossTile {
   static constexpr int ROWB = D * int(sizeof(T));  // bytes per row
   static constexpr int CPR = ROWB / 16;            // chunks per row
   static constexpr int RPR = 64 / CPR;             // rows per 1-KB run
-  static constexpr int NV = 8 / RPR;               // runs until the swizzle repeats
+  static constexpr int NV = (BF ? 16 : 8) / RPR;   // runs until the swizzle repeats
   static constexpr int NF = D / (BF ? 16 : 8);     // fragments of a row vector
   static constexpr int ND = D / 32;                // 32-row blocks of a transposed product
 
-  __device__ static __forceinline__ int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+  __device__ static __forceinline__ int swz(int r) {
+    if constexpr (!BF) return ((r & 3) << 1) | ((r >> 2) & 1);
+    else if constexpr (CPR == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    else return ((r & 3) << 2) | ((r >> 2) & 3);
+  }
 
   // the lane's share of a row vector: 16-byte chunks 2 f + half
   struct RowFrag {
@@ -134,14 +140,15 @@ struct CrossTile {
   __device__ static __forceinline__ void issue(const char* src, uint32_t ldb, int left,
                                                uint32_t lds, int wave, int lane) {
     constexpr int PW = ROWS / RPR / NW;  // runs of this wave
-    static_assert(PW * RPR * NW == ROWS && PW % NV == 0, "whole runs a wave");
+    static_assert(PW * RPR * NW == ROWS, "whole runs a wave");
     const u32x4 rs = rsrc_of(src, 0x7fffffffu);
     const int r = lane / CPR, pos = lane % CPR;
     if (left >= ROWS) {
 #pragma unroll
       for (int j = 0; j < PW; ++j) {
-        const uint32_t vo = uint32_t(r) * ldb + uint32_t((pos ^ swz((j % NV) * RPR + r)) << 4);
         const int i = wave * PW + j;
+        const int rr = (PW % NV == 0 ? j : i) * RPR + r;  // the row, modulo the swizzle's period
+        const uint32_t vo = uint32_t(r) * ldb + uint32_t((pos ^ swz(rr)) << 4);
         dma16(rs, uni(lds + i * 1024), vo, uni(uint32_t(i * RPR) * ldb));
       }
     } else {
@@ -149,7 +156,7 @@ struct CrossTile {
       for (int j = 0; j < PW; ++j) {
         const int i = wave * PW + j, row = i * RPR + r;
         const uint32_t vo =
-            uint32_t(min(row, left - 1)) * ldb + uint32_t((pos ^ swz((j % NV) * RPR + r)) << 4);
+            uint32_t(min(row, left - 1)) * ldb + uint32_t((pos ^ swz(row)) << 4);
         dma16(rs, uni(lds + i * 1024), vo, 0u);
       }
     }
@@ -228,14 +235,15 @@ struct CrossTile {
       const int s = lane & 15, k = 4 * half + (s >> 2);
       const int ch = 2 * ((lane >> 4) & 1) + ((s >> 1) & 1);
       const char* q = img + (row0 + k) * ROWB + (s & 1) * 8;
-      const int sw = swz(k);
+      const int sw = swz(k), sw8 = swz(k + 8);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
           const char* a0 = q + st * 16 * ROWB + (((4 * d + ch) ^ sw) << 4);
+          const char* a1 = q + (st * 16 + 8) * ROWB + (((4 * d + ch) ^ sw8) << 4);
           const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)a0);
-          const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a0 + 8 * ROWB));
+          const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)a1);
           typedef short short8_t __attribute__((ext_vector_type(8)));
           const short8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
           c[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v),
@@ -413,6 +421,7 @@ __device__ __forceinline__ float diagonal_sums(const floatx16& s, int lane) {
 // Sums of dS by t for the bias gradient, an array of bias_span entries for each
 // wave: every sum's order is fixed. What falls in a constant side is summed in
 // registers.
+template <int NW>
 struct BiasSums {
   float* arrays;
   float* mine;
@@ -426,7 +435,7 @@ struct BiasSums {
     lo = hi = 0.f;
   }
   __device__ __forceinline__ void clear(int tid) {
-    for (int x = tid; x < 4 * span; x += 256) arrays[x] = 0.f;
+    for (int x = tid; x < NW * span; x += 64 * NW) arrays[x] = 0.f;
     lo = hi = 0.f;
   }
   // Adds a block (lane: key, registers: queries) whose corner (first key, first
@@ -443,21 +452,27 @@ struct BiasSums {
     lo = group_sum<64>(lo);
     hi = group_sum<64>(hi);
     __syncthreads();
-    for (int x = tid; x < span; x += 256) {
+    for (int x = tid; x < span; x += 64 * NW) {
       float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) v += arrays[w * span + x];
+      for (int w = 0; w < NW; ++w) v += arrays[w * span + x];
       arrays[x] = v;
     }
     __syncthreads();
-    float* ends = arrays + span;  // [4 waves][2]
+    float* ends = arrays + span;  // [NW][2]
     if (lane == 0) {
       ends[2 * wave] = lo;
       ends[2 * wave + 1] = hi;
     }
     __syncthreads();
     const float* tab = arrays + BIAS_PAD - b.lo;  // by t
-    for (int k = tid; k < b.buckets; k += 256) {
+    float below = 0.f, above = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      below += ends[2 * w];
+      above += ends[2 * w + 1];
+    }
+    for (int k = tid; k < b.buckets; k += 64 * NW) {
       // distances [n0, n1) of the bucket; the last one of a side is open
       const int u = k % b.side;
       const bool ahead = k >= b.side, last = u == b.side - 1;
@@ -467,15 +482,15 @@ struct BiasSums {
       if (!ahead) {
         const int t0 = last ? b.lo - BIAS_PAD : 1 - n1;
         for (int t = t0; t <= -n0; ++t) v += tab[t];
-        if (last) v += (ends[0] + ends[2]) + (ends[4] + ends[6]);
+        if (last) v += below;
         if (!b.bidirectional && u == 0) {  // keys ahead share the bucket of t = 0
           for (int t = 1; t <= b.hi + BIAS_PAD; ++t) v += tab[t];
-          v += (ends[1] + ends[3]) + (ends[5] + ends[7]);
+          v += above;
         }
       } else {
         const int t1 = last ? b.hi + BIAS_PAD : n1 - 1;
         for (int t = max(n0, 1); t <= t1; ++t) v += tab[t];
-        if (last) v += (ends[1] + ends[3]) + (ends[5] + ends[7]);
+        if (last) v += above;
       }
       out[k] = v;
     }
