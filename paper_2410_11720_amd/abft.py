@@ -7,6 +7,7 @@ library is missing, importing this module raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import dataclasses
 import os
@@ -482,22 +483,13 @@ def _data(t):
     return None if t is None else t.data_ptr()
 
 
-class _on_device:
-    """Makes a tensor's device the current one for a call (most calls are on
-    it already)."""
-
-    def __init__(self, device):
-        self.guard = None
-        if device.index is not None and device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(fn, device, *args):
+    """fn(*args, current stream of the device) with that device current."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
 
 
 class CrossAttention:
@@ -558,11 +550,9 @@ class CrossAttention:
         q, o = self._tensor(Q, "Q", self._q_shape), self._tensor(O, "O", self._q_shape)
         k, v = self._tensor(K, "K", self._k_shape), self._tensor(V, "V", self._k_shape)
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
-        with _on_device(self.device):
-            _check(_lib.attn_cross_forward(self._c, q, k, v, bias, k_lens, q_start, o,
-                                           _data(self.lse), _data(self.rest),
-                                           self.workspace.data_ptr(), self.workspace.numel(),
-                                           _stream()), "attn_cross_forward")
+        _check(_call(_lib.attn_cross_forward, self.device, self._c, q, k, v, bias, k_lens, q_start,
+                     o, _data(self.lse), _data(self.rest), self.workspace.data_ptr(),
+                     self.workspace.numel()), "attn_cross_forward")
         return O
 
     def backward(self, dO, Q, K, V, O, bias=None, k_lens=None, q_start=None, dQ=None, dK=None,
@@ -583,16 +573,17 @@ class CrossAttention:
                                                              (dV, "dV"))]
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
         db = self._vector(dbias, "dbias", (c.buckets, c.heads), torch.float32)
-        with _on_device(self.device):
-            _check(_lib.attn_cross_backward(self._c, qs[0], qs[1], ks[0], ks[1], qs[2],
-                                            _data(self.lse), _data(self.rest), bias, k_lens,
-                                            q_start, qs[3], ks[2], ks[3], db,
-                                            self.workspace.data_ptr(), self.workspace.numel(),
-                                            _stream()), "attn_cross_backward")
+        _check(_call(_lib.attn_cross_backward, self.device, self._c, qs[0], qs[1], ks[0], ks[1],
+                     qs[2], _data(self.lse), _data(self.rest), bias, k_lens, q_start, qs[3], ks[2],
+                     ks[3], db, self.workspace.data_ptr(), self.workspace.numel()),
+               "attn_cross_backward")
         return dQ, dK, dV, dbias
 
 
 # ---- norm and clipping of gradients -------------------------------------------
+
+_GRAD_DTYPES = {torch.float32: FP32, torch.bfloat16: BF16}
+
 
 class GradStats:
     """Views of the device statistics that global_grad_norm and clip_gradients
@@ -623,39 +614,44 @@ class GradientClip:
             raise AbftError(f"{n} gradients, made for {self._n}")
         if len(out) != n:
             raise AbftError(f"{n} gradients, {len(out)} outputs")
-        arr = (Grad * max(1, n))()
-        for i in range(n):
-            g, o = grads[i], out[i]
-            if g.dtype is torch.float32:
-                dt = FP32
-            elif g.dtype is torch.bfloat16:
-                dt = BF16
-            else:
-                raise AbftError(f"gradient {i}: {g.dtype}")
-            if g.device != self.device or not g.is_contiguous():
-                raise AbftError(f"gradient {i}: expected contiguous on {self.device}")
-            if o is not g and (o.dtype != g.dtype or o.device != g.device or
-                               o.shape != g.shape or not o.is_contiguous()):
-                raise AbftError(f"output {i}: expected contiguous, as the gradient")
-            a = arr[i]
-            a.grad, a.out, a.numel, a.dtype = g.data_ptr(), o.data_ptr(), g.numel(), dt
-        return arr, n
+        # checked and read a field at a time (a tensor at a time takes twice as
+        # long, more than clipping 28 M elements does)
+        dtypes = [_GRAD_DTYPES.get(g.dtype) for g in grads]
+        numel = self._plain(grads, "gradient")
+        if None in dtypes:
+            i = dtypes.index(None)
+            raise AbftError(f"gradient {i}: {grads[i].dtype}")
+        grad_ptrs = out_ptrs = list(map(torch.Tensor.data_ptr, grads))
+        if out is not grads:
+            if (self._plain(out, "output") != numel
+                    or [_GRAD_DTYPES.get(o.dtype) for o in out] != dtypes):
+                raise AbftError("outputs: expected the gradients' types and sizes")
+            out_ptrs = list(map(torch.Tensor.data_ptr, out))
+        fields = [0] * (4 * n)   # abft_grad, dtype and reserved as one
+        fields[0::4], fields[1::4], fields[2::4], fields[3::4] = grad_ptrs, out_ptrs, numel, dtypes
+        return array.array("q", fields), n
+
+    def _plain(self, tensors, name):
+        """Sizes of contiguous tensors on the device (else raises)."""
+        index = self.device.index
+        if (not all(map(torch.Tensor.is_contiguous, tensors))
+                or any(d != index for d in map(torch.Tensor.get_device, tensors))):
+            raise AbftError(f"{name}s: expected contiguous tensors on {self.device}")
+        return list(map(torch.Tensor.numel, tensors))
 
     def norm(self, grads):
         """Leaves the norm in `stats`, which it returns."""
         arr, n = self._list(grads, grads)
-        with _on_device(self.device):
-            _check(_lib.global_grad_norm(arr, n, self.stats.raw.data_ptr(),
-                                         self.workspace.data_ptr(), self.workspace.numel(),
-                                         _stream()), "global_grad_norm")
+        _check(_call(_lib.global_grad_norm, self.device, arr.buffer_info()[0], n,
+                     self.stats.raw.data_ptr(), self.workspace.data_ptr(),
+                     self.workspace.numel()), "global_grad_norm")
         return self.stats
 
     def clip(self, grads, max_norm, out=None):
         """Scales the gradients to a global norm of at most max_norm, in place
         or into `out`; leaves norm, coef and nonfinite in `stats`."""
         arr, n = self._list(grads, grads if out is None else out)
-        with _on_device(self.device):
-            _check(_lib.clip_gradients(arr, n, float(max_norm), self.stats.raw.data_ptr(),
-                                       self.workspace.data_ptr(), self.workspace.numel(),
-                                       _stream()), "clip_gradients")
+        _check(_call(_lib.clip_gradients, self.device, arr.buffer_info()[0], n, float(max_norm),
+                     self.stats.raw.data_ptr(), self.workspace.data_ptr(),
+                     self.workspace.numel()), "clip_gradients")
         return self.stats

@@ -15,23 +15,25 @@ constexpr int64_t MAX_TOKEN_BYTES = 1 << 24; // a tile's rows fit the copies' 32
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 int es_of(const attn_cross_config* c) { return c->dtype == ABFT_FP32 ? 4 : 2; }
 
-// n^f >= e^(f - t) m^t for whole numbers, i.e. n >= e (m / e)^(t / f): exact.
-// Away from equality extended precision decides; next to it (a relative
-// distance below 1e-12, where rounding could) the prime exponents tell
-// whether both sides are equal.
-bool reaches(int n, int e, int m, int t, int f) {
-  const long double x = f * std::log((long double)n);
-  const long double y = (f - t) * std::log((long double)e) + t * std::log((long double)m);
-  if (std::fabs(x - y) > 1e-12L * (y + 1)) return x > y;
-  int a = n, b = e, c = m;
+// Least whole n with n >= e (m / e)^(t / f), i.e. n^f >= e^(f - t) m^t: exact.
+// Where the right side lies within 1e-9 of a whole number, that number's prime
+// exponents tell whether both sides are equal; else extended precision decides.
+int border(int e, int m, int t, int f) {
+  const double x = e * std::pow(double(m) / e, double(t) / f);
+  const double near = std::round(x);
+  if (std::fabs(x - near) > 1e-9 * x) return int(std::ceil(x));
+  int a = int(near), b = e, c = m;
+  bool equal = true;
   for (int p = 2; a > 1 || b > 1 || c > 1; ++p) {
     int va = 0, vb = 0, vc = 0;
     while (a % p == 0) { a /= p; ++va; }
     while (b % p == 0) { b /= p; ++vb; }
     while (c % p == 0) { c /= p; ++vc; }
-    if (f * va != (f - t) * vb + t * vc) return x > y;
+    equal = equal && f * va == (f - t) * vb + t * vc;
   }
-  return true;
+  const long double l = f * std::log((long double)near), r = (f - t) * std::log((long double)e) +
+                                                             t * std::log((long double)m);
+  return int(near) + (equal || l > r ? 0 : 1);
 }
 
 bool make_bias(int buckets, int max_distance, int bidirectional, CrossBias* b) {
@@ -45,14 +47,10 @@ bool make_bias(int buckets, int max_distance, int bidirectional, CrossBias* b) {
   b->exact = b->side / 2;
   if (max_distance <= b->exact) return false;
   const int f = b->side - b->exact;
-  b->border[0] = uint16_t(b->exact);
-  int n = b->exact;
-  for (int t = 1; t < f; ++t) {
-    while (!reaches(n, b->exact, max_distance, t, f)) ++n;
-    b->border[t] = uint16_t(n);
-  }
-  b->lo = -int(b->border[f - 1]);
-  b->hi = bidirectional ? int(b->border[f - 1]) : 0;
+  b->border[0] = b->exact;
+  for (int t = 1; t < f; ++t) b->border[t] = border(b->exact, max_distance, t, f);
+  b->lo = -b->border[f - 1];
+  b->hi = bidirectional ? b->border[f - 1] : 0;
   return true;
 }
 

@@ -17,31 +17,37 @@
 namespace abft {
 namespace {
 
-template <typename T>
-constexpr int other_tile() { return sizeof(T) == 2 ? 64 : 32; }
+// Whether a product's fragments are read ahead of the work in front of it: where
+// the registers last (head dim 64 in bf16; cross attention of 8 x 512 over 1000,
+// 12 heads: 73 -> 68 us).
+template <typename T, int D>
+constexpr bool read_ahead() { return D * sizeof(T) == 128; }
 
 // ---- query pass -----------------------------------------------------------
-template <typename T, int D, bool BIAS, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void cross_bwd_q_kernel(CrossArgs a) {
+template <typename T, int D, bool BIAS, int NQ, int KS>
+__global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void cross_bwd_q_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int KT = other_tile<T>(), NB = KT / 32;
+  constexpr int NW = NQ * KS, KT = cross_rows<T>(KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
+  constexpr bool AHEAD = read_ahead<T, D>();
+  __shared__ float row_sum[KS > 1 ? NW * 64 : 1];
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
-  const int nbk = a.B * a.kvh, ntile = cross_tiles(a.Sq, 32 * NW);
+  const int nbk = a.B * a.kvh, ntile = cross_tiles(a.Sq, 32 * NQ);
   const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
   const int b = bk / a.kvh, kv = bk % a.kvh, h = kv * a.group + y % a.group;
   int tile = y / a.group;
   if (a.causal) tile = ntile - 1 - tile;
-  const int q0 = tile * 32 * NW;
+  const int q0 = tile * 32 * NQ;
   const int len = seq_len(a, b), start = seq_start(a, b);
   int kend = len;
-  if (a.causal) kend = min(kend, start + min(q0 + 32 * NW, a.Sq));
+  if (a.causal) kend = min(kend, start + min(q0 + 32 * NQ, a.Sq));
   kend = max(kend, 0);
   const int nt = (kend + KT - 1) / KT;
-  const int w0 = q0 + 32 * wave, i = w0 + (lane & 31), ic = min(i, a.Sq - 1);
+  const int qw = wave % NQ, ks = wave / NQ;
+  const int w0 = q0 + 32 * qw, i = w0 + (lane & 31), ic = min(i, a.Sq - 1);
   const bool valid = i < a.Sq;
   int wend = len;
   if (a.causal) wend = min(wend, start + min(w0 + 32, a.Sq));
@@ -84,6 +90,28 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_bwd_q_kernel(CrossArgs a) {
   if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
   float sum = 0.f;  // of the row's dS
 
+  // rows between the last query and the end of the key pass's tiles: P = 0
+  if (q0 + 32 * NQ >= a.Sq)
+    for (int x = q0 + 32 * NQ + tid; x < a.q_pad; x += 64 * NW) {
+      const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + x;
+      a.nlse[at] = NEG_INF;
+      a.ndelta[at] = 0.f;
+    }
+  // a row's sum over its KS waves (all call it together, behind the last use of
+  // the sums before)
+  auto join_sum = [&](float x) {
+    x = half_sum(x);
+    if constexpr (KS > 1) {
+      row_sum[wave * 64 + lane] = x;
+      __syncthreads();
+      x = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) x += row_sum[(qw + k * NQ) * 64 + lane];
+      __syncthreads();
+    }
+    return x;
+  };
+
   floatx16 dq[Tile::ND];
 #pragma unroll
   for (int d = 0; d < Tile::ND; ++d) dq[d] = floatx16{};
@@ -92,21 +120,28 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_bwd_q_kernel(CrossArgs a) {
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < nt) issue(t + 1);
-    const int k0 = t * KT;
-    if (k0 >= wend) continue;
-    const char* img = smem + (t & 1) * 2 * IMG;
-    const bool masked = k0 + KT > len || (a.causal && k0 + KT - 1 > start + w0);
+    const int k0 = t * KT + 32 * NB * ks;  // the wave's keys of the tile
+    const char* img = smem + (t & 1) * 2 * IMG + 32 * NB * ks * Tile::ROWB;
+    const bool masked = k0 + 32 * NB > len || (a.causal && k0 + 32 * NB - 1 > start + w0);
     // rows of few keys (one tile) sum their dS first and correct D by it: there
     // the rounding of single P shows in dq
-    for (int sweep = wend <= KT ? 0 : 1; sweep < 2; ++sweep) {
+    for (int sweep = (KS > 1 ? nt == 1 : wend <= KT) ? 0 : 1; sweep < 2; ++sweep) {
       asm volatile("" ::: "memory");  // (reads of the image stay in the loop: they need registers)
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
+        if (k0 >= wend) continue;
         floatx16 s = floatx16{}, dp;
-        Tile::rows(s, img, 32 * n, q, lane);
+        typename Tile::RowFrag kf, vf;
+        Tile::load_rows(kf, img, 32 * n, lane);
+        Tile::load_rows(vf, img + IMG, 32 * n, lane);
+        issue_loads<AHEAD>();
+        Tile::rows(s, kf, q);
 #pragma unroll
         for (int r = 0; r < 16; ++r) dp[r] = nd;
-        Tile::rows(dp, img + IMG, 32 * n, g, lane);
+        Tile::rows(dp, vf, g);
+        typename Tile::ColFrag kc;
+        if constexpr (AHEAD) Tile::load_cols(kc, img, 32 * n, lane);
+        issue_loads<AHEAD>();
         float ce = c, off = nl;
         if constexpr (BIAS) {
           const int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
@@ -134,20 +169,41 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_bwd_q_kernel(CrossArgs a) {
         if (sweep == 0) continue;
         typename Tile::Probs p;
         Tile::pack(p, s);
-        Tile::cols(dq, img, 32 * n, p, lane);
+        if constexpr (!AHEAD) Tile::load_cols(kc, img, 32 * n, lane);
+        Tile::cols(dq, kc, p, lane);
       }
       if (sweep == 0) {
-        nd -= half_sum(sum);
+        nd -= join_sum(sum);
         sum = 0.f;
       }
     }
+  }
+  if constexpr (KS > 1) {
+    float* box = reinterpret_cast<float*>(smem) + lane;
+    constexpr int BOX = 64 * 16 * Tile::ND;
+    static_assert(NQ * (KS - 1) * BOX * 4 <= 4 * IMG, "the tiles' space holds the boxes");
+    sum = join_sum(sum);  // (a barrier: the tiles are no longer read)
+    if (ks > 0) {
+#pragma unroll
+      for (int e = 0; e < 16 * Tile::ND; ++e)
+        box[(wave - NQ) * BOX + 64 * e] = dq[e / 16][e % 16];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int k = 1; k < KS; ++k)
+#pragma unroll
+      for (int e = 0; e < 16 * Tile::ND; ++e)
+        dq[e / 16][e % 16] += box[(wave + (k - 1) * NQ) * BOX + 64 * e];
+  } else {
+    sum = half_sum(sum);
   }
   Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid, half);
 
   // For the key pass: -lse, and D so that the row's dS sum to zero as they must.
   // (O was formed from P rounded to bf16, which moves D by 2^-9 of its terms;
   // a bias gradient, the sum of many dS of either sign, was off by 0.1%.)
-  nd -= half_sum(sum);
+  nd -= sum;
   if (half == 0) {
     const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i;
     a.nlse[at] = nl;
@@ -176,33 +232,34 @@ __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, flo
 // S = Q K^T, so that a lane holds the scores of one key (its mask is a bound on
 // the query) and P and dS are the second operands of dV^T = dO^T P and
 // dK^T = Q^T dS from registers.
-// A workgroup has KW x QH waves: KW times 32 keys, and QH waves on the same keys
-// that take the 32-row blocks of a query tile in turn and join their sums at
-// the end.
+// A workgroup has KW x QH waves: 32 KW keys, and QH waves on the same 32 that
+// take different rows of a query tile and join their sums at the end.
 // At head dim 128 the accumulators of both gradients and the keys' and values' own
 // fragments do not fit 256 registers beside the scores (36 spilled: the pass of
 // 4 x 2048 queries over 1024 keys, 32 heads on 8, 720 us). In bf16 the values' are
-// read from LDS, and there is one workgroup of 8 waves a CU. fp32 runs one wave per
-// SIMD.
+// read from LDS, which leaves room for one workgroup a CU, of 8 waves (260 us;
+// of 4 waves 345 us). fp32 runs one wave per SIMD.
 template <typename T, int D>
 struct KvShape {
-  static constexpr bool WIDE = D * int(sizeof(T)) == 256 && sizeof(T) == 2;
-  static constexpr int QH = WIDE ? 2 : 1;
-  static constexpr int QT = sizeof(T) == 2 ? 64 : 32;  // rows of a query tile
-  static constexpr int NB = QT / 32 / QH;              // blocks of it a wave takes
-  static constexpr bool VLDS = WIDE;
+  static constexpr bool VLDS = D * int(sizeof(T)) == 256 && sizeof(T) == 2;
   static constexpr int PER_SIMD = D * int(sizeof(T)) == 512 ? 1 : 2;
 };
+template <typename T, int D, int KW, int QH>
+constexpr size_t kv_lds(int span) {
+  return 2 * (size_t(2) * cross_rows<T>(QH) * D * sizeof(T) + 8 * cross_stats(cross_rows<T>(QH))) +
+         (KvShape<T, D>::VLDS ? size_t(32) * KW * D * sizeof(T) : 0) +
+         (span ? size_t(KW * QH + 1) * span * 4 : 0);
+}
 
-template <typename T, int D, bool BIAS, int KW>
-__global__ __launch_bounds__((64 * KW * KvShape<T, D>::QH), (KvShape<T, D>::PER_SIMD)) void
+template <typename T, int D, bool BIAS, int KW, int QH>
+__global__ __launch_bounds__(64 * KW * QH, (KvShape<T, D>::PER_SIMD)) void
 cross_bwd_kv_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  using Shape = KvShape<T, D>;
-  constexpr int QT = Shape::QT, NB = Shape::NB, QH = Shape::QH, NW = KW * QH, KEYS = 32 * KW;
+  constexpr int QT = cross_rows<T>(QH), NB = QT / 32 / QH, NW = KW * QH, KEYS = 32 * KW;
   constexpr int IMG = QT * Tile::ROWB;
-  constexpr int STAGE = 2 * IMG + 512;  // Q, dO, -lse and -D of a tile
-  constexpr bool VLDS = Shape::VLDS;
+  constexpr int NS = cross_stats(QT);
+  constexpr int STAGE = 2 * IMG + 8 * NS;  // Q, dO, -lse and -D of a tile
+  constexpr bool VLDS = KvShape<T, D>::VLDS, AHEAD = read_ahead<T, D>();
   extern __shared__ __align__(1024) char smem[];
   const char* vimg = smem + 2 * STAGE;
   float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS ? KEYS * Tile::ROWB : 0));
@@ -231,10 +288,14 @@ cross_bwd_kv_kernel(CrossArgs a) {
     Tile::template issue<QT, NW>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
                                 a.dout.t, a.Sq - i0, to + IMG, wave, lane);
     const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i0;
-    if (wave < 2) {  // (64 values; a 32-row tile uses half of them)
-      const int n = min(64, a.q_pad - i0);
-      dma4(rsrc_of((wave == 0 ? a.nlse : a.ndelta) + at, 256), uni(to + 2 * IMG + wave * 256),
-           uint32_t(min(lane, n - 1) * 4), 0u);
+    if (wave < 2) {  // (64 at a time; a 32-row tile uses half of them)
+#pragma unroll
+      for (int x = 0; x < NS; x += 64) {
+        const int n = min(64, a.q_pad - i0 - x);  // the end of the rows: the last one again
+        if (n > 0)
+          dma4(rsrc_of((wave == 0 ? a.nlse : a.ndelta) + at + x, 256),
+               uni(to + 2 * IMG + wave * 4 * NS + 4 * x), uint32_t(min(lane, n - 1) * 4), 0u);
+      }
     }
   };
   if (nt > 0) {
@@ -282,15 +343,19 @@ cross_bwd_kv_kernel(CrossArgs a) {
       }
     }
     const int i0 = (first + t % per) * QT;
-    if (w0 >= len || (a.causal && start + i0 + QT - 1 < w0)) continue;
+    if (w0 >= len || (a.causal && start + i0 + 32 * NB * (qh + 1) - 1 < w0)) continue;
     const char* img = smem + (t & 1) * STAGE;
     const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
-    const float* nds = nls + 64;
+    const float* nds = nls + NS;
 #pragma unroll
     for (int m = 0; m < NB; ++m) {
-      const int n = m * QH + qh;
+      const int n = qh * NB + m;
       floatx16 s = floatx16{}, dp, nl;
-      Tile::rows(s, img, 32 * n, kf, lane);
+      typename Tile::RowFrag af;
+      Tile::load_rows(af, img, 32 * n, lane);
+      issue_loads<AHEAD>();
+      Tile::rows(s, af, kf);
+      if constexpr (!VLDS) Tile::load_rows(af, img + IMG, 32 * n, lane);
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const int row = 32 * n + 2 * r + 4 * half;  // 8 (r / 4) + 4 half
@@ -302,10 +367,14 @@ cross_bwd_kv_kernel(CrossArgs a) {
           dp[r + e] = d[e];
         }
       }
+      issue_loads<AHEAD>();
       if constexpr (VLDS)
         Tile::rows(dp, img + IMG, 32 * n, vimg, 32 * kw, lane);
       else
-        Tile::rows(dp, img + IMG, 32 * n, vf, lane);
+        Tile::rows(dp, af, vf);
+      typename Tile::ColFrag cf;
+      if constexpr (AHEAD) Tile::load_cols(cf, img + IMG, 32 * n, lane);
+      issue_loads<AHEAD>();
       float ce = c, off = 0.f;
       int side = 0, at = 0;  // -1, 1: in a constant side of the bias
       if constexpr (BIAS) {
@@ -334,7 +403,10 @@ cross_bwd_kv_kernel(CrossArgs a) {
       for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, nl[r] + off));
       typename Tile::Probs p;
       Tile::pack(p, s);
-      Tile::cols(dv, img + IMG, 32 * n, p, lane);
+      typename Tile::ColFrag qf;
+      if constexpr (AHEAD) Tile::load_cols(qf, img, 32 * n, lane);
+      if constexpr (!AHEAD) Tile::load_cols(cf, img + IMG, 32 * n, lane);
+      Tile::cols(dv, cf, p, lane);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] *= dp[r];
       if constexpr (BIAS) {
@@ -353,31 +425,36 @@ cross_bwd_kv_kernel(CrossArgs a) {
         }
       }
       Tile::pack(p, s);
-      Tile::cols(dk, img, 32 * n, p, lane);
+      if constexpr (!AHEAD) Tile::load_cols(qf, img, 32 * n, lane);
+      Tile::cols(dk, qf, p, lane);
     }
   }
   if constexpr (BIAS) {
     if (nt > 0) sums.flush(a.bias, part(kv * a.group + a.group - 1), tid, lane, wave);
   }
-  if constexpr (QH == 2) {
-    // the second half's sums to the first, one gradient after the other
-    float* box = reinterpret_cast<float*>(smem) + kw * 64 * 16 * Tile::ND + lane;
-    static_assert(KW * 64 * 16 * Tile::ND * 4 <= 2 * STAGE, "the tiles' space holds a gradient");
+  if constexpr (QH > 1) {
+    // the others' sums to the first wave of the keys, one gradient after the other
+    constexpr int BOX = 64 * 16 * Tile::ND;
+    float* box = reinterpret_cast<float*>(smem) + lane;
+    static_assert(KW * (QH - 1) * BOX * 4 <= 2 * STAGE, "the tiles' space holds a gradient");
     auto join = [&](floatx16(&x)[Tile::ND]) {
       __syncthreads();
-      if (qh == 1) {
+      if (qh > 0) {
 #pragma unroll
-        for (int e = 0; e < 16 * Tile::ND; ++e) box[64 * e] = x[e / 16][e % 16];
+        for (int e = 0; e < 16 * Tile::ND; ++e) box[(wave - KW) * BOX + 64 * e] = x[e / 16][e % 16];
       }
       __syncthreads();
       if (qh == 0) {
 #pragma unroll
-        for (int e = 0; e < 16 * Tile::ND; ++e) x[e / 16][e % 16] += box[64 * e];
+        for (int k = 1; k < QH; ++k)
+#pragma unroll
+          for (int e = 0; e < 16 * Tile::ND; ++e)
+            x[e / 16][e % 16] += box[(wave + (k - 1) * KW) * BOX + 64 * e];
       }
     };
     join(dk);
     join(dv);
-    if (qh == 1) return;
+    if (qh > 0) return;
   }
   // keys behind the sequence's length: zero
   const bool valid = j < a.Sk;
@@ -392,34 +469,29 @@ cross_bwd_kv_kernel(CrossArgs a) {
   Tile::store_row(a.dv.p + b * a.dv.b + kv * a.dv.h + int64_t(j) * a.dv.t, dv, 1.f, valid, half);
 }
 
-template <typename T, int D, bool BIAS, int NW>
+template <typename T, int D>
+size_t q_lds(const CrossArgs& a, int KS) {
+  return size_t(4) * cross_rows<T>(KS) * D * sizeof(T) +
+         (a.bias.buckets ? size_t(bias_span_h(a.bias)) * 4 : 0);
+}
+
+template <typename T, int D, bool BIAS, int NQ, int KS>
 hipError_t run_q(const CrossArgs& a, hipStream_t s) {
-  const size_t lds = size_t(4) * other_tile<T>() * D * sizeof(T) +
-                     (BIAS ? size_t(bias_span_h(a.bias)) * 4 : 0);
-  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS, NW>>(160 * 1024);
+  const size_t lds = q_lds<T, D>(a, KS);
+  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS, NQ, KS>>(CROSS_LDS - 2048);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NW);
-  cross_bwd_q_kernel<T, D, BIAS, NW><<<dim3(uint32_t(grid)), 64 * NW, lds, s>>>(a);
+  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NQ);
+  cross_bwd_q_kernel<T, D, BIAS, NQ, KS><<<dim3(uint32_t(grid)), 64 * NQ * KS, lds, s>>>(a);
   return hipGetLastError();
 }
 
-// Keys a workgroup of the key pass owns, in 32s.
-template <typename T, int D>
-int kv_waves(const CrossArgs& a) {
-  return KvShape<T, D>::QH == 2 ? 4 : cross_waves(int64_t(a.B) * a.kvh, a.Sk);
-}
-
-template <typename T, int D, bool BIAS, int KW>
+template <typename T, int D, bool BIAS, int KW, int QH>
 hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
-  using Shape = KvShape<T, D>;
-  const size_t lds = 2 * (size_t(2) * Shape::QT * D * sizeof(T) + 512) +
-                     (Shape::VLDS ? size_t(32) * KW * D * sizeof(T) : 0) +
-                     (BIAS ? size_t(KW * Shape::QH + 1) * bias_span_h(a.bias) * 4 : 0);
-  hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS, KW>>(160 * 1024);
+  hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS, KW, QH>>(CROSS_LDS);
   if (e != hipSuccess) return e;
+  const size_t lds = kv_lds<T, D, KW, QH>(BIAS ? bias_span_h(a.bias) : 0);
   const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk, 32 * KW);
-  cross_bwd_kv_kernel<T, D, BIAS, KW>
-      <<<dim3(uint32_t(grid)), 64 * KW * Shape::QH, lds, s>>>(a);
+  cross_bwd_kv_kernel<T, D, BIAS, KW, QH><<<dim3(uint32_t(grid)), 64 * KW * QH, lds, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || !BIAS) return e;
   cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
       a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk, 32 * KW), a.bias.buckets, a.nh);
@@ -433,8 +505,13 @@ hipError_t launch_cross_bwd_q(const CrossArgs& a, int dtype, int D, hipStream_t 
     using T = typename decltype(t)::type;
     constexpr int DD = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
-    return cross_waves(int64_t(a.B) * a.nh, a.Sq) == 2 ? run_q<T, DD, BIAS, 2>(a, s)
-                                                       : run_q<T, DD, BIAS, 4>(a, s);
+    const int64_t heads = int64_t(a.B) * a.nh, blocks = cross_tiles(a.Sk, 32);
+    if constexpr (DD * sizeof(T) < 512)  // (four 32-row tiles of 512 bytes do not fit LDS)
+      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), q_lds<T, DD>(a, 4), 2, blocks))
+        return run_q<T, DD, BIAS, 1, 4>(a, s);
+    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), q_lds<T, DD>(a, 2), 2, blocks))
+      return run_q<T, DD, BIAS, 2, 2>(a, s);
+    return run_q<T, DD, BIAS, 4, 1>(a, s);
   });
 }
 
@@ -443,10 +520,24 @@ hipError_t launch_cross_bwd_kv(const CrossArgs& a, int dtype, int D, hipStream_t
     using T = typename decltype(t)::type;
     constexpr int DD = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
-    if constexpr (KvShape<T, DD>::QH == 2)
-      return run_kv<T, DD, BIAS, 4>(a, s);
-    else
-      return kv_waves<T, DD>(a) == 2 ? run_kv<T, DD, BIAS, 2>(a, s) : run_kv<T, DD, BIAS, 4>(a, s);
+    const int64_t heads = int64_t(a.B) * a.kvh;
+    const int64_t blocks = int64_t(a.group) * cross_tiles(a.Sq, 32);
+    const int64_t one = heads * cross_tiles(a.Sk, 32), two = heads * cross_tiles(a.Sk, 64);
+    const int span = BIAS ? bias_span_h(a.bias) : 0;
+    if constexpr (KvShape<T, DD>::VLDS) {
+      // (8 waves a workgroup, and a CU; the sums of a wide bias leave room for 4)
+      if (cross_split_pays(4, two, kv_lds<T, DD, 2, 4>(span), 1, blocks))
+        return run_kv<T, DD, BIAS, 2, 4>(a, s);
+      if (kv_lds<T, DD, 4, 2>(span) <= CROSS_LDS) return run_kv<T, DD, BIAS, 4, 2>(a, s);
+      return run_kv<T, DD, BIAS, 2, 2>(a, s);
+    } else {
+      if constexpr (DD * sizeof(T) < 512)
+        if (cross_split_pays(4, one, kv_lds<T, DD, 1, 4>(span), 2, blocks))
+          return run_kv<T, DD, BIAS, 1, 4>(a, s);
+      if (cross_split_pays(2, two, kv_lds<T, DD, 2, 2>(span), 2, blocks))
+        return run_kv<T, DD, BIAS, 2, 2>(a, s);
+      return run_kv<T, DD, BIAS, 4, 1>(a, s);
+    }
   });
 }
 

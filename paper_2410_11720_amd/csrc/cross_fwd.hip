@@ -37,7 +37,10 @@ struct Online {
   // values in the image v.
   template <int NB>
   __device__ __forceinline__ void add(floatx16 (&s)[NB], float ce, float off, const char* v,
-                                      int row0, int lane) {
+                                      int lane) {
+    typename Tile::ColFrag vf;
+    Tile::load_cols(vf, v, 0, lane);
+    issue_loads<sizeof(T) == 2>();
     float mt = s[0][0];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -62,7 +65,10 @@ struct Online {
       }
       typename Tile::Probs p;
       Tile::pack(p, s[b]);
-      Tile::cols(o, v, row0 + 32 * b, p, lane);
+      typename Tile::ColFrag next;
+      if (b + 1 < NB) Tile::load_cols(next, v, 32 * (b + 1), lane);
+        Tile::cols(o, vf, p, lane);
+        if (b + 1 < NB) vf = next;
     }
   }
 };
@@ -89,16 +95,14 @@ __device__ __forceinline__ char* rest_row(const CrossArgs& a, int b, int h, int 
   return a.rest + ((int64_t(b) * a.nh + h) * a.Sq + i) * D * 2;
 }
 
-template <typename T>
-constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
-
-// Tiled form: a workgroup owns 32 NW queries of one head, a wave 32 of them; key
-// tiles of 64 (fp32: 32) pass through LDS in two stages, the next one copied
-// while this one is worked on.
-template <typename T, int D, bool BIAS, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void cross_fwd_kernel(CrossArgs a) {
+// Tiled form: a workgroup owns 32 NQ queries of one head, KS waves for each 32 of
+// them; key tiles pass through LDS in two stages, the next one copied while this
+// one is worked on. The KS waves take different keys of a tile and join their
+// sums at the end.
+template <typename T, int D, bool BIAS, int NQ, int KS>
+__global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int KT = key_tile<T>(), NB = KT / 32;
+  constexpr int NW = NQ * KS, KT = cross_rows<T>(KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
@@ -110,15 +114,16 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd_kernel(CrossArgs a) {
   const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
   const int b = bk / a.kvh, kv = bk % a.kvh, h = kv * a.group + y % a.group;
   int tile = y / a.group;
-  if (a.causal) tile = cross_tiles(a.Sq, 32 * NW) - 1 - tile;
-  const int q0 = tile * 32 * NW;
+  if (a.causal) tile = cross_tiles(a.Sq, 32 * NQ) - 1 - tile;
+  const int q0 = tile * 32 * NQ;
   const int len = seq_len(a, b), start = seq_start(a, b);
   int kend = len;
-  if (a.causal) kend = min(kend, start + min(q0 + 32 * NW, a.Sq));
+  if (a.causal) kend = min(kend, start + min(q0 + 32 * NQ, a.Sq));
   kend = max(kend, 0);
   const int nt = (kend + KT - 1) / KT;
 
-  const int w0 = q0 + 32 * wave;             // the wave's first query
+  const int qw = wave % NQ, ks = wave / NQ;
+  const int w0 = q0 + 32 * qw;               // the wave's first query
   const int i = w0 + (lane & 31);            // the lane's
   const bool valid = i < a.Sq;
   int wend = len;                            // keys of the wave
@@ -148,19 +153,24 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd_kernel(CrossArgs a) {
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < nt) issue(t + 1);
-    const int k0 = t * KT;
+    const int k0 = t * KT + 32 * NB * ks;    // the wave's keys of the tile
     if (k0 >= wend) continue;
-    const char* img = smem + (t & 1) * 2 * IMG;
+    const char* img = smem + (t & 1) * 2 * IMG + 32 * NB * ks * Tile::ROWB;
     floatx16 s[NB];
+    typename Tile::RowFrag kf[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) Tile::load_rows(kf[n], img, 32 * n, lane);
+    issue_loads<sizeof(T) == 2>();
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       s[n] = floatx16{};
-      Tile::rows(s[n], img, 32 * n, q, lane);
+      Tile::rows(s[n], kf[n], q);
     }
     float ce = c, off = 0.f;
     if constexpr (BIAS) {
-      const int t0 = k0 - start - w0;  // t of the corner; the tile spans [t0 - 31, t0 + KT - 1]
-      if (t0 + KT - 1 <= a.bias.lo) {
+      // t of the corner; the wave's keys span [t0 - 31, t0 + 32 NB - 1]
+      const int t0 = k0 - start - w0;
+      if (t0 + 32 * NB - 1 <= a.bias.lo) {
         off = tab[0];
       } else if (t0 - 31 >= a.bias.hi) {
         off = tab[bias_span(a.bias) - 1];
@@ -175,11 +185,40 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd_kernel(CrossArgs a) {
         }
       }
     }
-    if (k0 + KT > len || (a.causal && k0 + KT - 1 > start + w0)) {
+    if (k0 + 32 * NB > len || (a.causal && k0 + 32 * NB - 1 > start + w0)) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) mask_scores(s[n], limit - k0 - 32 * n, lane);
     }
-    on.template add<NB>(s, ce, off, img + IMG, 0, lane);
+    on.template add<NB>(s, ce, off, img + IMG, lane);
+  }
+  if constexpr (KS > 1) {
+    // the others' maximum, sum and output to the first wave of the queries
+    constexpr int BOX = 64 * (16 * Tile::ND + 2);
+    float* box = reinterpret_cast<float*>(smem) + lane;
+    static_assert(NQ * (KS - 1) * BOX * 4 <= 4 * IMG, "the tiles' space holds the boxes");
+    __syncthreads();
+    if (ks > 0) {
+      float* p = box + (wave - NQ) * BOX;
+      p[0] = on.m;
+      p[64] = on.l;
+#pragma unroll
+      for (int e = 0; e < 16 * Tile::ND; ++e) p[64 * (e + 2)] = on.o[e / 16][e % 16];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int k = 1; k < KS; ++k) {
+      const float* p = box + (wave + (k - 1) * NQ) * BOX;
+      const float mk = p[0], mn = fmaxf(on.m, mk);
+      if (!__any(mn != NEG_INF)) continue;
+      const float f = mn == NEG_INF ? 1.f : exp2_hw(on.m - mn);
+      const float g = mn == NEG_INF ? 0.f : exp2_hw(mk - mn);
+      on.m = mn;
+      on.l = fmaf(on.l, f, p[64] * g);
+#pragma unroll
+      for (int e = 0; e < 16 * Tile::ND; ++e)
+        on.o[e / 16][e % 16] = fmaf(on.o[e / 16][e % 16], f, p[64 * (e + 2)] * g);
+    }
   }
   const float l = half_sum(on.l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -270,7 +309,10 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
     const int k0 = ks + 32 * wave + 128 * t;
     const char* img = mine + (t % NS) * 2 * IMG;
     floatx16 s[1] = {floatx16{}};
-    Tile::rows(s[0], img, 0, q, lane);
+    typename Tile::RowFrag kf;
+    Tile::load_rows(kf, img, 0, lane);
+    issue_loads<sizeof(T) == 2>();
+    Tile::rows(s[0], kf, q);
     float ce = c, off = 0.f;
     if constexpr (BIAS) {
       const int lo = a.bias.lo, hi = a.bias.hi;
@@ -288,7 +330,7 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
       }
     }
     if (k0 + 32 > len || a.causal) mask_scores(s[0], limit - k0, lane);
-    on.template add<1>(s, ce, off, img + IMG, 0, lane);
+    on.template add<1>(s, ce, off, img + IMG, lane);
     if (t + NS < nt) {
       lds_wait_all();  // the stage has been read
       issue(t + NS);
@@ -402,14 +444,19 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
     a.lse[(int64_t(b) * a.nh + h) * a.Sq + i] = l == 0.f ? NEG_INF : m + log2_hw(l);
 }
 
-template <typename T, int D, bool BIAS, int NW>
+template <typename T, int D>
+size_t fwd_lds(const CrossArgs& a, int KS) {
+  return size_t(4) * cross_rows<T>(KS) * D * sizeof(T) +
+         (a.bias.buckets ? size_t(bias_span_h(a.bias)) * 4 : 0);
+}
+
+template <typename T, int D, bool BIAS, int NQ, int KS>
 hipError_t run_fwd(const CrossArgs& a, hipStream_t s) {
-  constexpr int KT = key_tile<T>();
-  const size_t lds = size_t(4) * KT * D * sizeof(T) + (BIAS ? bias_span_h(a.bias) * 4 : 0);
-  hipError_t e = lds_limit<cross_fwd_kernel<T, D, BIAS, NW>>(160 * 1024);
+  const size_t lds = fwd_lds<T, D>(a, KS);
+  hipError_t e = lds_limit<cross_fwd_kernel<T, D, BIAS, NQ, KS>>(CROSS_LDS);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NW);
-  cross_fwd_kernel<T, D, BIAS, NW><<<dim3(uint32_t(grid)), 64 * NW, lds, s>>>(a);
+  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NQ);
+  cross_fwd_kernel<T, D, BIAS, NQ, KS><<<dim3(uint32_t(grid)), 64 * NQ * KS, lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -435,8 +482,14 @@ hipError_t launch_cross_fwd(const CrossArgs& a, int dtype, int D, hipStream_t s)
     using T = typename decltype(t)::type;
     constexpr int D = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
-    return cross_waves(int64_t(a.B) * a.nh, a.Sq) == 2 ? run_fwd<T, D, BIAS, 2>(a, s)
-                                                       : run_fwd<T, D, BIAS, 4>(a, s);
+    const int64_t heads = int64_t(a.B) * a.nh, blocks = cross_tiles(a.Sk, 32);
+    const int most = sizeof(T) * D == 128 ? 3 : 2;
+    if constexpr (D * sizeof(T) < 512)  // (four 32-row tiles of 512 bytes do not fit LDS)
+      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), fwd_lds<T, D>(a, 4), most, blocks))
+        return run_fwd<T, D, BIAS, 1, 4>(a, s);
+    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), fwd_lds<T, D>(a, 2), most, blocks))
+      return run_fwd<T, D, BIAS, 2, 2>(a, s);
+    return run_fwd<T, D, BIAS, 4, 1>(a, s);
   });
 }
 

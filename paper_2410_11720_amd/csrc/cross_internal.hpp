@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "abft_internal.hpp"
@@ -29,7 +30,7 @@ struct CrossBias {
   int side = 0;   // buckets of one side
   int exact = 0;  // of them, distances with a bucket of their own
   int lo = 0, hi = 0;
-  uint16_t border[CROSS_MAX_BUCKETS];  // [i], i >= 1: least distance of bucket exact + i
+  int32_t border[CROSS_MAX_BUCKETS];  // [i], i >= 1: least distance of bucket exact + i
 };
 
 struct CrossArgs {
@@ -56,17 +57,22 @@ struct CrossArgs {
 };
 
 constexpr int CROSS_QT = 128;  // queries (keys) a workgroup owns at most in the tiled kernels
-constexpr int CROSS_QMIN = 64;  // and at least
+constexpr int CROSS_QMIN = 32;  // and at least
 
 constexpr int cross_tiles(int n, int tile) { return (n + tile - 1) / tile; }
 
-// Waves of 32 queries (keys) a workgroup has, 4 or 2, for n of them and `heads`
-// (batch, head) pairs: those that leave the fullest CU with fewer waves. (96
-// heads x 512 queries in fours are 384 workgroups, two on every other CU; in
-// twos they are three everywhere.) In fours a tile's copies serve more queries.
-inline int cross_waves(int64_t heads, int n) {
-  auto load = [&](int w) { return (heads * cross_tiles(n, 32 * w) + 255) / 256 * w; };
-  return load(2) < load(4) ? 2 : 4;
+constexpr size_t CROSS_LDS = 160 * 1024;
+
+// Whether `split` waves (2 or 4) share the work of 32 queries (keys), each a part
+// of the other axis: where all workgroups of that shape are on the chip at once. A wave's tiles follow each other, and fewer than two waves a
+// SIMD leave its waits uncovered, so a grid that does not fill the chip gains
+// (8 heads, 1024 queries and keys: 67 -> 35 us by 4; fp32 374 -> 121 us); one that
+// does loses what the smaller tiles read twice (16 heads x 4096: 345 -> 449 us).
+// wgs: workgroups of the shape; lds: bytes each takes; most: that a CU's
+// registers hold; blocks: 32s along the split axis.
+inline bool cross_split_pays(int split, int64_t wgs, size_t lds, int most, int64_t blocks) {
+  if (lds > CROSS_LDS || blocks < 2 * split) return false;
+  return wgs <= 256 * std::min<int64_t>(most, int64_t(CROSS_LDS / lds));
 }
 
 // Entries of the spread bias table in LDS.

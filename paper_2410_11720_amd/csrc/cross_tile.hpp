@@ -40,6 +40,22 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
 }
 
+// Keeps the loads before it in front of what follows.
+template <bool ON>
+__device__ __forceinline__ void issue_loads() {
+  if constexpr (ON) __builtin_amdgcn_sched_barrier(0);
+}
+
+// Rows of a tile of the other axis, for S waves that share it.
+template <typename T>
+constexpr int cross_rows(int S) {
+  const int least = sizeof(T) == 2 ? 64 : 32;
+  return least > 32 * S ? least : 32 * S;
+}
+
+// Entries of a tile's row statistics in LDS (copied 64 at a time).
+constexpr int cross_stats(int rows) { return rows < 64 ? 64 : rows; }
+
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 // Keys of a sequence, and the position of its first query among them (values
@@ -162,28 +178,37 @@ struct CrossTile {
     }
   }
 
-  // C += rows [row0, row0 + 32) of the image times B
-  __device__ static __forceinline__ void rows(floatx16& c, const char* img, int row0,
-                                              const RowFrag& b, int lane) {
+  // Fragments of 32 rows of an image as the first operand of a `rows` product.
+  // Products are written as a load and a multiply, so that a kernel can issue
+  // the loads of a product before the work in front of it: left to itself the
+  // compiler reads every fragment right before its instruction and waits.
+  __device__ static __forceinline__ void load_rows(RowFrag& a, const char* img, int row0,
+                                                   int lane) {
     const int r = lane & 31, half = lane >> 5;
     const char* p = img + (row0 + r) * ROWB;
     const int sw = swz(r);
 #pragma unroll
+    for (int f = 0; f < NF; ++f)
+      a.f[f] = *reinterpret_cast<const u32x4*>(p + (((2 * f + half) ^ sw) << 4));
+  }
+  // C += A B
+  __device__ static __forceinline__ void rows(floatx16& c, const RowFrag& a, const RowFrag& b) {
+#pragma unroll
     for (int f = 0; f < NF; ++f) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(p + (((2 * f + half) ^ sw) << 4));
       if constexpr (BF) {
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.f[f]),
                                                     __builtin_bit_cast(bf16x8, b.f[f]), c, 0, 0, 0);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]),
+          c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.f[f][e]),
                                                    __uint_as_float(b.f[f][e]), c, 0, 0, 0);
       }
     }
   }
 
-  // The same with B's columns the rows [at, at + 32) of an image.
+  // C += (rows [row0, row0 + 32) of the image) B, B's columns the rows [at, at +
+  // 32) of another image: fragment by fragment, for few registers.
   __device__ static __forceinline__ void rows(floatx16& c, const char* img, int row0,
                                               const char* own, int at, int lane) {
     const int r = lane & 31, half = lane >> 5;
@@ -195,15 +220,8 @@ struct CrossTile {
       const int ch = ((2 * f + half) ^ sw) << 4;
       const u32x4 a = *reinterpret_cast<const u32x4*>(p + ch);
       const u32x4 b = *reinterpret_cast<const u32x4*>(q + ch);
-      if constexpr (BF) {
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c,
-                                                   0, 0, 0);
-      }
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
   }
 
@@ -225,14 +243,18 @@ struct CrossTile {
     }
   }
 
-  // C[d] += (rows [row0, row0 + 32) of the image)^T P
-  __device__ static __forceinline__ void cols(floatx16 (&c)[ND], const char* img, int row0,
-                                              const Probs& p, int lane) {
-    const int half = lane >> 5;
+  // 32 rows of an image, transposed, as the first operand of a `cols` product
+  // (fp32 reads its elements in the product).
+  struct ColFrag {
+    u32x4 f[BF ? 2 * ND : 1];
+    const char* at;
+  };
+  __device__ static __forceinline__ void load_cols(ColFrag& a, const char* img, int row0,
+                                                   int lane) {
     if constexpr (BF) {
       // lane l of a 16-lane group supplies 4 elements of row l / 4, columns
       // 4 (l % 4); it receives column l of the 4 rows
-      const int s = lane & 15, k = 4 * half + (s >> 2);
+      const int s = lane & 15, k = 4 * (lane >> 5) + (s >> 2);
       const int ch = 2 * ((lane >> 4) & 1) + ((s >> 1) & 1);
       const char* q = img + (row0 + k) * ROWB + (s & 1) * 8;
       const int sw = swz(k), sw8 = swz(k + 8);
@@ -246,21 +268,34 @@ struct CrossTile {
           const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)a1);
           typedef short short8_t __attribute__((ext_vector_type(8)));
           const short8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          c[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v),
-                                                         __builtin_bit_cast(bf16x8, p.b[st]), c[d],
-                                                         0, 0, 0);
+          a.f[st * ND + d] = __builtin_bit_cast(u32x4, v);
         }
     } else {
-      const int col = lane & 31;
+      a.at = img + row0 * ROWB;
+    }
+  }
+  // C[d] += A^T P
+  __device__ static __forceinline__ void cols(floatx16 (&c)[ND], const ColFrag& a, const Probs& p,
+                                              int lane) {
+    if constexpr (BF) {
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+          c[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              __builtin_bit_cast(bf16x8, a.f[st * ND + d]), __builtin_bit_cast(bf16x8, p.b[st]),
+              c[d], 0, 0, 0);
+    } else {
+      const int half = lane >> 5, col = lane & 31;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int k = 8 * (r >> 2) + 4 * half + (r & 3);
-        const char* q = img + (row0 + k) * ROWB + (col & 3) * 4;
+        const char* q = a.at + k * ROWB + (col & 3) * 4;
         const int sw = swz(k);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          const float a = *reinterpret_cast<const float*>(q + (((8 * d + (col >> 2)) ^ sw) << 4));
-          c[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.x[r], c[d], 0, 0, 0);
+          const float x = *reinterpret_cast<const float*>(q + (((8 * d + (col >> 2)) ^ sw) << 4));
+          c[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p.x[r], c[d], 0, 0, 0);
         }
       }
     }
@@ -332,7 +367,9 @@ __device__ __forceinline__ int bias_bucket(const CrossBias& b, int t) {
   }
   if (n < b.exact) return base + n;
   int k = b.exact;
-  for (int i = 1; i < b.side - b.exact; ++i) k += n >= b.border[i] ? 1 : 0;
+  const int f = b.side - b.exact;
+#pragma unroll 8
+  for (int i = 1; i < f; ++i) k += n >= b.border[i] ? 1 : 0;
   return base + k;
 }
 

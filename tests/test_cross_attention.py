@@ -178,6 +178,18 @@ GRID = [
     (C(2, 65, 140, 4, 128, kv_heads=2, dtype="f32"), [140, 33], None),
     (C(2, 150, 150, 2, 64, dtype="f32", causal=True, buckets=32, bidirectional=False), None, None),
     (C(1, 100, 300, 2, 128, dtype="f32", buckets=32), None, None),
+    # few heads over long axes (waves that share queries or keys), many heads
+    (C(1, 330, 700, 2, 64, buckets=32), [650], None),
+    (C(1, 500, 500, 4, 128, causal=True, buckets=32, bidirectional=False), None, None),
+    (C(2, 260, 300, 2, 128, kv_heads=1), [300, 40], None),
+    (C(2, 250, 340, 2, 64, dtype="f32", causal=True), [340, 100], [90, -30]),
+    (C(1, 130, 500, 4, 128, dtype="f32", buckets=32), None, None),
+    (C(4, 64, 90, 100, 64, buckets=32), [90, 64, 33, 0], None),
+    (C(3, 70, 150, 60, 128, causal=True, buckets=32), [150, 129, 2], [80, 59, 0]),
+    (C(4, 45, 40, 90, 64, dtype="f32"), [40, 33, 32, 1], None),
+    (C(1, 96, 800, 2, 128, buckets=128, max_distance=1024), None, None),
+    (C(1, 96, 800, 2, 128, dtype="f32", buckets=128, max_distance=1024), None, None),
+    (C(1, 96, 800, 2, 64, dtype="f32", buckets=128, max_distance=1024), None, None),
     # another scale
     (C(1, 50, 60, 2, 64, scale=0.3), None, None),
 ]
