@@ -94,7 +94,7 @@ assert ctypes.sizeof(Event) == 40 and ctypes.sizeof(Fault) == 28
 _vp, _sz, _i32, _i64, _f32, _u32 = (ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32,
                                    ctypes.c_int64, ctypes.c_float, ctypes.c_uint32)
 _P = ctypes.POINTER(Config)
-_CP, _TP = ctypes.POINTER(CrossConfigC), ctypes.POINTER(CrossTensor)
+_CP = ctypes.POINTER(CrossConfigC)
 _sig = {
     "attn_abft_workspace_bytes": (_sz, [_P]),
     "attn_abft_report_bytes": (_sz, [_i32]),
@@ -123,10 +123,10 @@ _sig = {
     "attn_abft_sections_for_step": (_u32, [_vp, _i64]),
     "attn_rel_bucket": (ctypes.c_int, [_i64, _i32, _i32, _i32]),
     "attn_cross_workspace_bytes": (_sz, [_CP]),
-    "attn_cross_forward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _vp, _vp, _vp, _TP, _vp, _vp, _vp,
+    "attn_cross_forward": (ctypes.c_int, [_CP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                           _sz, _vp]),
-    "attn_cross_backward": (ctypes.c_int, [_CP, _TP, _TP, _TP, _TP, _TP, _vp, _vp, _vp, _vp, _vp,
-                                           _TP, _TP, _TP, _vp, _vp, _sz, _vp]),
+    "attn_cross_backward": (ctypes.c_int, [_CP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                           _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "clip_gradients_workspace_bytes": (_sz, [_i32]),
     "global_grad_norm": (ctypes.c_int, [_vp, _i32, _vp, _vp, _sz, _vp]),
     "clip_gradients": (ctypes.c_int, [_vp, _i32, ctypes.c_double, _vp, _vp, _sz, _vp]),
@@ -521,14 +521,20 @@ class CrossAttention:
         self._q_shape = (cfg.batch, cfg.q_len, cfg.heads, cfg.head_dim)
         self._k_shape = (cfg.batch, cfg.k_len, kvh, cfg.head_dim)
 
-    def _tensor(self, t, name, shape):
-        if t.device != self.device or t.dtype != self.cfg.torch_dtype or t.shape != shape:
-            raise AbftError(f"{name}: expected {shape} {self.cfg.torch_dtype} on {self.device}, got "
-                            f"{tuple(t.shape)} {t.dtype} on {t.device}")
-        st = t.stride()
-        if st[3] != 1:
-            raise AbftError(f"{name}: the last dimension must be contiguous")
-        return CrossTensor(t.data_ptr(), st[0], st[1], st[2])
+    def _tensors(self, names, tensors, shapes):
+        """The tensors' attn_cross_tensor records, one after the other; returns
+        them and the address of each."""
+        fields, dtype, index = [], self.cfg.torch_dtype, self.device.index
+        for name, t, shape in zip(names, tensors, shapes):
+            st = t.stride()
+            if t.get_device() != index or t.dtype != dtype or t.shape != shape or st[3] != 1:
+                raise AbftError(f"{name}: expected {shape} {dtype} on {self.device} with a "
+                                f"contiguous last dimension, got {tuple(t.shape)} {t.dtype} on "
+                                f"{t.device}, strides {st}")
+            fields += (t.data_ptr(), st[0], st[1], st[2])
+        records = array.array("q", fields)
+        at = records.buffer_info()[0]
+        return records, range(at, at + 32 * len(names), 32)
 
     def _vector(self, t, name, shape, dtype):
         if t is None:
@@ -547,8 +553,8 @@ class CrossAttention:
     def forward(self, Q, K, V, bias=None, k_lens=None, q_start=None, O=None):
         if O is None:
             O = torch.empty(self._q_shape, dtype=self.cfg.torch_dtype, device=self.device)
-        q, o = self._tensor(Q, "Q", self._q_shape), self._tensor(O, "O", self._q_shape)
-        k, v = self._tensor(K, "K", self._k_shape), self._tensor(V, "V", self._k_shape)
+        qs, ks = self._q_shape, self._k_shape
+        held, (q, k, v, o) = self._tensors("QKVO", (Q, K, V, O), (qs, ks, ks, qs))
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
         _check(_call(_lib.attn_cross_forward, self.device, self._c, q, k, v, bias, k_lens, q_start,
                      o, _data(self.lse), _data(self.rest), self.workspace.data_ptr(),
@@ -567,16 +573,15 @@ class CrossAttention:
         dQ, dK, dV = new(dQ, self._q_shape), new(dK, self._k_shape), new(dV, self._k_shape)
         if dbias is None and c.buckets:
             dbias = torch.empty((c.buckets, c.heads), dtype=torch.float32, device=self.device)
-        qs = [self._tensor(t, n, self._q_shape) for t, n in ((dO, "dO"), (Q, "Q"), (O, "O"),
-                                                             (dQ, "dQ"))]
-        ks = [self._tensor(t, n, self._k_shape) for t, n in ((K, "K"), (V, "V"), (dK, "dK"),
-                                                             (dV, "dV"))]
+        qs, ks = self._q_shape, self._k_shape
+        held, (do, q, k, v, o, dq, dk, dv) = self._tensors(
+            ("dO", "Q", "K", "V", "O", "dQ", "dK", "dV"), (dO, Q, K, V, O, dQ, dK, dV),
+            (qs, qs, ks, ks, qs, qs, ks, ks))
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
         db = self._vector(dbias, "dbias", (c.buckets, c.heads), torch.float32)
-        _check(_call(_lib.attn_cross_backward, self.device, self._c, qs[0], qs[1], ks[0], ks[1],
-                     qs[2], _data(self.lse), _data(self.rest), bias, k_lens, q_start, qs[3], ks[2],
-                     ks[3], db, self.workspace.data_ptr(), self.workspace.numel()),
-               "attn_cross_backward")
+        _check(_call(_lib.attn_cross_backward, self.device, self._c, do, q, k, v, o,
+                     _data(self.lse), _data(self.rest), bias, k_lens, q_start, dq, dk, dv, db,
+                     self.workspace.data_ptr(), self.workspace.numel()), "attn_cross_backward")
         return dQ, dK, dV, dbias
 
 

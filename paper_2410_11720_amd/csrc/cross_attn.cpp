@@ -73,19 +73,32 @@ int validate(const attn_cross_config* c, CrossBias* bias) {
   return ABFT_OK;
 }
 
-// Whether the short form takes a forward, and its key splits. It runs the
-// queries of all heads that share a key head as tiles of 32 rows.
+// Whether the short form takes a forward, and its key splits, by the steps (128
+// keys, a wave 32 of them) that follow each other on a CU. The short form runs the
+// queries of all heads that share a key head as tiles of 32 rows and may
+// split the keys over workgroups, which costs a second launch (about 3 us, a
+// step 0.65 us at head dim 64 and 1 us at 128); the tiled form runs every
+// 32 queries of a head over all keys. Measured: 8 heads x 2 sequences, 32 queries
+// over 2000 keys, head dim 64: 9.5 us, tiled 14.5; 12 x 16, 500 keys: tiled
+// 7.8, two splits 13.1.
 bool short_form(const attn_cross_config* c, int* splits) {
   *splits = 1;
-  if (c->q_len > 32) return false;
+  const int64_t row = int64_t(c->head_dim) * es_of(c);     // bytes
   const int64_t rows = int64_t(c->q_len) * (c->heads / c->kv_heads);
   const int64_t base = int64_t(c->batch) * c->kv_heads * ((rows + 31) / 32);
   if (base == 0) return false;
   const int64_t steps = (int64_t(c->k_len) + 127) / 128;
-  int64_t n = (512 + base - 1) / base;
-  n = std::min(n, steps / 2);
-  *splits = int(std::max<int64_t>(1, std::min<int64_t>(n, 64)));
-  return true;
+  const int64_t slots = row == 128 ? 512 : 256;            // workgroups at a time, by LDS
+  const int64_t join = es_of(c) == 4 ? 1 : (row == 128 ? 5 : 4);
+  const int64_t most = std::min<int64_t>({64, steps / 2, slots / base});
+  int64_t cost = (base + slots - 1) / slots * steps;
+  if (most > 1 && (steps + most - 1) / most + join < cost) {
+    *splits = int(most);
+    cost = (steps + most - 1) / most + join;
+  }
+  const int64_t tiles = int64_t(c->batch) * c->heads * cross_tiles(c->q_len, 32);
+  const int64_t tiled = std::max(steps, tiles * steps / slots);
+  return cost < tiled || (cost == tiled && rows <= 32);
 }
 
 struct Space {

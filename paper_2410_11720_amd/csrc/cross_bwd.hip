@@ -218,8 +218,18 @@ __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, flo
   const int h = blockIdx.x, lanes = 256 / buckets;  // partial sums of a bucket
   const int k = threadIdx.x % buckets, j = threadIdx.x / buckets;
   float v = 0.f;
-  if (j < lanes)
-    for (int x = j; x < n; x += lanes) v += part[(int64_t(h) * n + x) * buckets + k];
+  if (j < lanes) {
+    const float* p = part + int64_t(h) * n * buckets + k;
+    int x = j;
+    for (; x + 7 * lanes < n; x += 8 * lanes) {  // eight loads at a time
+      float y[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) y[u] = p[int64_t(x + u * lanes) * buckets];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v += y[u];
+    }
+    for (; x < n; x += lanes) v += p[int64_t(x) * buckets];
+  }
   sh[threadIdx.x] = v;
   __syncthreads();
   if (threadIdx.x < buckets) {
@@ -350,22 +360,20 @@ cross_bwd_kv_kernel(CrossArgs a) {
 #pragma unroll
     for (int m = 0; m < NB; ++m) {
       const int n = qh * NB + m;
-      floatx16 s = floatx16{}, dp, nl;
+      floatx16 s = floatx16{}, dp;
       typename Tile::RowFrag af;
       Tile::load_rows(af, img, 32 * n, lane);
       issue_loads<AHEAD>();
       Tile::rows(s, af, kf);
       if constexpr (!VLDS) Tile::load_rows(af, img + IMG, 32 * n, lane);
+      // (registers 4 q .. 4 q + 3: rows 8 q + 4 half on)
+      const float* nlr = nls + 32 * n + 4 * half;
+      const float* ndr = nds + 32 * n + 4 * half;
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const int row = 32 * n + 2 * r + 4 * half;  // 8 (r / 4) + 4 half
-        const floatx4 x = *reinterpret_cast<const floatx4*>(nls + row);
-        const floatx4 d = *reinterpret_cast<const floatx4*>(nds + row);
+        const floatx4 d = *reinterpret_cast<const floatx4*>(ndr + 2 * r);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          nl[r + e] = x[e];
-          dp[r + e] = d[e];
-        }
+        for (int e = 0; e < 4; ++e) dp[r + e] = d[e];
       }
       issue_loads<AHEAD>();
       if constexpr (VLDS)
@@ -400,7 +408,11 @@ cross_bwd_kv_kernel(CrossArgs a) {
         for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= from ? s[r] : NEG_INF;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, nl[r] + off));
+      for (int r = 0; r < 16; r += 4) {
+        const floatx4 l = *reinterpret_cast<const floatx4*>(nlr + 2 * r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[r + e] = exp2_hw(fmaf(s[r + e], ce, l[e] + off));
+      }
       typename Tile::Probs p;
       Tile::pack(p, s);
       typename Tile::ColFrag qf;

@@ -67,8 +67,8 @@ struct Online {
       Tile::pack(p, s[b]);
       typename Tile::ColFrag next;
       if (b + 1 < NB) Tile::load_cols(next, v, 32 * (b + 1), lane);
-        Tile::cols(o, vf, p, lane);
-        if (b + 1 < NB) vf = next;
+      Tile::cols(o, vf, p, lane);
+      if (b + 1 < NB) vf = next;
     }
   }
 };
@@ -408,27 +408,40 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
   }
 }
 
-// Joins the splits of the short form: a wave per row, the splits' weights
-// 2^(m_s - max m) l_s in the order of the splits.
+// Joins the splits of the short form, at most 64: a wave per row. Lane s holds
+// split s's maximum and sum; the outputs are read four splits at a time and
+// summed in the order of the splits (a split that saw no key wrote none).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   const int lane = threadIdx.x & 63;
   const int rows = a.Sq * a.group;
   const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (r >= int64_t(a.B) * a.kvh * rows) return;
-  const float* ml = a.part_ml + r * a.splits * 2;
-  const float* po = a.part_o + r * a.splits * D;
-  float m = NEG_INF;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[2 * s]);
-  constexpr int PER = D / 64;
-  float acc[PER] = {}, l = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float ls = ml[2 * s + 1];
-    if (ls == 0.f) continue;                 // no key seen: nothing was written
-    const float f = exp2_hw(ml[2 * s] - m);
-    l = fmaf(ls, f, l);
+  const bool in = lane < a.splits;
+  const float* ml = a.part_ml + (r * a.splits + (in ? lane : 0)) * 2;
+  const float ls = in ? ml[1] : 0.f, ms = in && ls != 0.f ? ml[0] : NEG_INF;
+  float m = ms;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = fmaf(po[s * D + lane * PER + e], f, acc[e]);
+  for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
+  const float f = ls != 0.f ? exp2_hw(ms - m) : 0.f;
+  const float l = group_sum<64>(ls * f);
+  constexpr int PER = D / 64, U = 4;
+  typedef float vec __attribute__((ext_vector_type(PER)));
+  const vec* po = reinterpret_cast<const vec*>(a.part_o + r * a.splits * D) + lane;
+  vec acc = {};
+  for (int s = 0; s < a.splits; s += U) {
+    vec x[U];
+    float w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = min(s + u, a.splits - 1);
+      x[u] = po[at * 64];
+      w[u] = __shfl(f, at, 64);
+      if (s + u >= a.splits) w[u] = 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (w[u] != 0.f) acc += x[u] * w[u];
   }
   const int bk = int(r / rows), row = int(r % rows);
   const int b = bk / a.kvh, h = (bk % a.kvh) * a.group + row % a.group, i = row / a.group;

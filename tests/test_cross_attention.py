@@ -1,6 +1,6 @@
 """Attention over keys of another length against its definition in 64 bits:
 forward, backward, the relative position bias and its gradient, the short form."""
-import itertools
+import ctypes
 import math
 import random
 
@@ -66,7 +66,7 @@ def test_workspace_bytes_cover_both_directions():
 def _c_tensor(ptr, shape, stride=None):
     if stride is None:
         stride = (shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
-    return abft.CrossTensor(ptr, *stride)
+    return ctypes.byref(abft.CrossTensor(ptr, *stride))
 
 
 def _forward_status(cfg, q=None, k=None, o=None, bias=0, ws=1 << 20, ws_ptr=4096):
