@@ -66,7 +66,7 @@ int validate(const attn_cross_config* c, CrossBias* bias) {
   if (c->q_len > MAX_LEN || c->k_len > MAX_LEN) return ABFT_ERR_UNSUPPORTED;
   const int64_t wgs = int64_t(c->batch) * c->heads;
   if (wgs > (int64_t(1) << 24) ||
-      wgs * cross_tiles(std::max(c->q_len, c->k_len), CROSS_QMIN) > (int64_t(1) << 30))
+      wgs * cross_tiles(std::max(c->q_len, c->k_len), 32) > (int64_t(1) << 30))
     return ABFT_ERR_UNSUPPORTED;
   if (c->buckets && !make_bias(c->buckets, c->max_distance, c->bidirectional, bias))
     return ABFT_ERR_INVALID;
@@ -104,10 +104,16 @@ bool short_form(const attn_cross_config* c, int* splits) {
 struct Space {
   size_t part_o = 0, part_ml = 0;        // forward, short form
   size_t nlse = 0, ndelta = 0, dbias = 0;  // backward
+  size_t sum = 0, part = 0, part2 = 0;     // its parts (one pass's at a time)
   size_t fwd = 0, bwd = 0;
 };
 
-Space make_space(const attn_cross_config* c) {
+CrossPlan plan_of(const attn_cross_config* c, const CrossBias& b) {
+  return cross_plan(c->batch, c->heads, c->kv_heads, c->q_len, c->k_len, es_of(c), c->head_dim,
+                    c->buckets ? bias_span_h(b) : 0);
+}
+
+Space make_space(const attn_cross_config* c, const CrossPlan& p) {
   Space L;
   int splits;
   if (short_form(c, &splits) && splits > 1) {
@@ -119,8 +125,13 @@ Space make_space(const attn_cross_config* c) {
   const size_t rows = size_t(c->batch) * c->heads * cross_tiles(c->q_len, CROSS_QT) * CROSS_QT;
   L.ndelta = align_up(rows * 4);
   L.dbias = 2 * L.ndelta;
-  L.bwd = L.dbias + align_up(size_t(c->batch) * c->heads *
-                              cross_tiles(c->k_len, CROSS_QMIN) * c->buckets * 4);
+  L.sum = L.dbias + align_up(size_t(c->batch) * c->heads * cross_tiles(c->k_len, 32 * p.kv_keys) *
+                             p.kv_parts * c->buckets * 4);
+  L.part = L.sum + (p.q_parts > 1 ? align_up(rows * 4 * p.q_parts) : 0);
+  const size_t dq = size_t(c->batch) * c->heads * c->q_len * c->head_dim * 4;
+  const size_t dk = align_up(size_t(c->batch) * c->kv_heads * c->k_len * c->head_dim * 4 * p.kv_parts);
+  L.part2 = L.part + dk;
+  L.bwd = L.part + std::max(p.q_parts > 1 ? align_up(dq * p.q_parts) : 0, p.kv_parts > 1 ? 2 * dk : 0);
   return L;
 }
 
@@ -201,7 +212,7 @@ int attn_rel_bucket(int64_t relative, int32_t buckets, int32_t max_distance,
 size_t attn_cross_workspace_bytes(const attn_cross_config* cfg) {
   CrossBias b;
   if (validate(cfg, &b) != ABFT_OK) return 0;
-  const Space L = make_space(cfg);
+  const Space L = make_space(cfg, plan_of(cfg, b));
   return std::max(std::max(L.fwd, L.bwd), ALIGN);
 }
 
@@ -217,7 +228,7 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
   TRY(take(cfg, K, cfg->k_len, cfg->kv_heads, false, &a.k));
   TRY(take(cfg, V, cfg->k_len, cfg->kv_heads, false, &a.v));
   TRY(take(cfg, O, cfg->q_len, cfg->heads, true, &a.o));
-  const Space L = make_space(cfg);
+  const Space L = make_space(cfg, plan_of(cfg, a.bias));
   if (L.fwd && !workspace) return ABFT_ERR_INVALID;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 || reinterpret_cast<uintptr_t>(rest) % 16)
     return ABFT_ERR_INVALID;
@@ -260,7 +271,8 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
   TRY(take(cfg, dV, cfg->k_len, cfg->kv_heads, true, &a.dv));
   const bool any_q = cfg->batch > 0 && cfg->q_len > 0, any_k = cfg->batch > 0 && cfg->k_len > 0;
   if (any_q && !lse) return ABFT_ERR_INVALID;
-  const Space L = make_space(cfg);
+  const CrossPlan plan = plan_of(cfg, a.bias);
+  const Space L = make_space(cfg, plan);
   if (L.bwd && !workspace) return ABFT_ERR_INVALID;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 || reinterpret_cast<uintptr_t>(rest) % 16)
     return ABFT_ERR_INVALID;
@@ -275,10 +287,15 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
   a.ndelta = reinterpret_cast<float*>(ws + L.ndelta);
   a.dbias_part = reinterpret_cast<float*>(ws + L.dbias);
   a.dbias = dbias;
+  a.q_parts = plan.q_parts;
+  a.kv_parts = plan.kv_parts;
+  a.part_sum = reinterpret_cast<float*>(ws + L.sum);
+  a.part_dq = a.part_dk = reinterpret_cast<float*>(ws + L.part);
+  a.part_dv = reinterpret_cast<float*>(ws + L.part2);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (any_q) CK(launch_cross_bwd_q(a, cfg->dtype, cfg->head_dim, s));
+  if (any_q) CK(launch_cross_bwd_q(a, plan, cfg->dtype, cfg->head_dim, s));
   if (any_k)
-    CK(launch_cross_bwd_kv(a, cfg->dtype, cfg->head_dim, s));
+    CK(launch_cross_bwd_kv(a, plan, cfg->dtype, cfg->head_dim, s));
   else if (cfg->buckets)
     CK(launch_cross_no_keys(a, s));
   return ABFT_OK;

@@ -23,11 +23,19 @@ namespace {
 template <typename T, int D>
 constexpr bool read_ahead() { return D * sizeof(T) == 128; }
 
+template <typename T>
+__device__ __forceinline__ void store4(char* p, floatx4 v) {
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  else
+    *reinterpret_cast<floatx4*>(p) = v;
+}
+
 // ---- query pass -----------------------------------------------------------
 template <typename T, int D, bool BIAS, int NQ, int KS>
 __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void cross_bwd_q_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int NW = NQ * KS, KT = cross_rows<T>(KS), NB = KT / 32 / KS;
+  constexpr int NW = NQ * KS, KT = cross_rows(sizeof(T), KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
   constexpr bool AHEAD = read_ahead<T, D>();
   __shared__ float row_sum[KS > 1 ? NW * 64 : 1];
@@ -38,7 +46,8 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
   const int nbk = a.B * a.kvh, ntile = cross_tiles(a.Sq, 32 * NQ);
   const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
   const int b = bk / a.kvh, kv = bk % a.kvh, h = kv * a.group + y % a.group;
-  int tile = y / a.group;
+  const int part = y / (a.group * ntile);
+  int tile = y / a.group % ntile;
   if (a.causal) tile = ntile - 1 - tile;
   const int q0 = tile * 32 * NQ;
   const int len = seq_len(a, b), start = seq_start(a, b);
@@ -46,6 +55,8 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
   if (a.causal) kend = min(kend, start + min(q0 + 32 * NQ, a.Sq));
   kend = max(kend, 0);
   const int nt = (kend + KT - 1) / KT;
+  // the workgroup's tiles
+  const int t0 = int(int64_t(nt) * part / a.q_parts), t1 = int(int64_t(nt) * (part + 1) / a.q_parts);
   const int qw = wave % NQ, ks = wave / NQ;
   const int w0 = q0 + 32 * qw, i = w0 + (lane & 31), ic = min(i, a.Sq - 1);
   const bool valid = i < a.Sq;
@@ -63,7 +74,7 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
     Tile::template issue<KT, NW>(vp + int64_t(t) * KT * a.v.t, a.v.t, len - t * KT, to + IMG, wave,
                                 lane);
   };
-  if (nt > 0) issue(0);
+  if (t1 > t0) issue(t0);
 
   typename Tile::RowFrag q, g;
   Tile::load_row(q, a.q.p + b * a.q.b + h * a.q.h + int64_t(ic) * a.q.t, half);
@@ -91,12 +102,13 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
   float sum = 0.f;  // of the row's dS
 
   // rows between the last query and the end of the key pass's tiles: P = 0
-  if (q0 + 32 * NQ >= a.Sq)
+  if (part == 0 && q0 + 32 * NQ >= a.Sq)
     for (int x = q0 + 32 * NQ + tid; x < a.q_pad; x += 64 * NW) {
       const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + x;
       a.nlse[at] = NEG_INF;
       a.ndelta[at] = 0.f;
     }
+  const float nd0 = nd;
   // a row's sum over its KS waves (all call it together, behind the last use of
   // the sums before)
   auto join_sum = [&](float x) {
@@ -116,10 +128,10 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
 #pragma unroll
   for (int d = 0; d < Tile::ND; ++d) dq[d] = floatx16{};
   const float c = a.scale * LOG2E;
-  for (int t = 0; t < nt; ++t) {
+  for (int t = t0; t < t1; ++t) {
     wait_vmcnt<0>();
     __syncthreads();
-    if (t + 1 < nt) issue(t + 1);
+    if (t + 1 < t1) issue(t + 1);
     const int k0 = t * KT + 32 * NB * ks;  // the wave's keys of the tile
     const char* img = smem + (t & 1) * 2 * IMG + 32 * NB * ks * Tile::ROWB;
     const bool masked = k0 + 32 * NB > len || (a.causal && k0 + 32 * NB - 1 > start + w0);
@@ -198,17 +210,62 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
   } else {
     sum = half_sum(sum);
   }
-  Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid, half);
-
   // For the key pass: -lse, and D so that the row's dS sum to zero as they must.
   // (O was formed from P rounded to bf16, which moves D by 2^-9 of its terms;
   // a bias gradient, the sum of many dS of either sign, was off by 0.1%.)
   nd -= sum;
-  if (half == 0) {
-    const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i;
+  const int64_t row = int64_t(b) * a.nh + h, at = row * a.q_pad + i;
+  if (a.q_parts == 1) {
+    Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid,
+                    half);
+  } else {
+    const int64_t rows = int64_t(a.B) * a.nh;
+    Tile::store_sums(a.part_dq + ((part * rows + row) * a.Sq + i) * D, dq, valid, half);
+    if (half == 0) a.part_sum[part * rows * a.q_pad + at] = nd0 - nd;
+    nd = nd0;  // (cross_join_q_kernel takes the parts' sums off)
+  }
+  if (half == 0 && part == 0) {
     a.nlse[at] = nl;
     a.ndelta[at] = nd;
   }
+}
+
+// Joins the query pass's parts in their order: dq, and -D less the sums of dS.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cross_join_q_kernel(CrossArgs a) {
+  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x, rows = int64_t(a.B) * a.nh;
+  const int64_t r = x / (D / 4);
+  const int e = int(x % (D / 4)) * 4;
+  if (r >= rows * a.Sq) return;
+  const int64_t bh = r / a.Sq, i = r % a.Sq;
+  floatx4 v = {};
+  for (int p = 0; p < a.q_parts; ++p)
+    v += *reinterpret_cast<const floatx4*>(a.part_dq + (p * rows * a.Sq + r) * D + e);
+  const int b = int(bh / a.nh), h = int(bh % a.nh);
+  store4<T>(a.dq.p + b * a.dq.b + h * a.dq.h + i * a.dq.t + e * int(sizeof(T)), v * a.scale);
+  if (e == 0) {
+    float s = 0.f;
+    for (int p = 0; p < a.q_parts; ++p) s += a.part_sum[(p * rows + bh) * a.q_pad + i];
+    a.ndelta[bh * a.q_pad + i] -= s;
+  }
+}
+
+// Joins the key pass's parts in their order: dk (y = 0) or dv.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cross_join_kv_kernel(CrossArgs a) {
+  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t r = x / (D / 4), rows = int64_t(a.B) * a.kvh * a.Sk;
+  const int e = int(x % (D / 4)) * 4;
+  if (r >= rows) return;
+  const float* from = blockIdx.y == 0 ? a.part_dk : a.part_dv;
+  const CrossTensor& to = blockIdx.y == 0 ? a.dk : a.dv;
+  floatx4 v = {};
+  for (int p = 0; p < a.kv_parts; ++p)
+    v += *reinterpret_cast<const floatx4*>(from + (p * rows + r) * D + e);
+  const int64_t bh = r / a.Sk, j = r % a.Sk;
+  const int b = int(bh / a.kvh), h = int(bh % a.kvh);
+  store4<T>(to.p + b * to.b + h * to.h + j * to.t + e * int(sizeof(T)),
+            v * (blockIdx.y == 0 ? a.scale : 1.f));
 }
 
 // Sums the key pass's partial bias gradients of one head in a fixed order.
@@ -249,27 +306,15 @@ __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, flo
 // 4 x 2048 queries over 1024 keys, 32 heads on 8, 720 us). In bf16 the values' are
 // read from LDS, which leaves room for one workgroup a CU, of 8 waves (260 us;
 // of 4 waves 345 us). fp32 runs one wave per SIMD.
-template <typename T, int D>
-struct KvShape {
-  static constexpr bool VLDS = D * int(sizeof(T)) == 256 && sizeof(T) == 2;
-  static constexpr int PER_SIMD = D * int(sizeof(T)) == 512 ? 1 : 2;
-};
-template <typename T, int D, int KW, int QH>
-constexpr size_t kv_lds(int span) {
-  return 2 * (size_t(2) * cross_rows<T>(QH) * D * sizeof(T) + 8 * cross_stats(cross_rows<T>(QH))) +
-         (KvShape<T, D>::VLDS ? size_t(32) * KW * D * sizeof(T) : 0) +
-         (span ? size_t(KW * QH + 1) * span * 4 : 0);
-}
-
 template <typename T, int D, bool BIAS, int KW, int QH>
-__global__ __launch_bounds__(64 * KW * QH, (KvShape<T, D>::PER_SIMD)) void
+__global__ __launch_bounds__(64 * KW * QH, (sizeof(T) * D == 512 ? 1 : 2)) void
 cross_bwd_kv_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int QT = cross_rows<T>(QH), NB = QT / 32 / QH, NW = KW * QH, KEYS = 32 * KW;
+  constexpr int QT = cross_rows(sizeof(T), QH), NB = QT / 32 / QH, NW = KW * QH, KEYS = 32 * KW;
   constexpr int IMG = QT * Tile::ROWB;
   constexpr int NS = cross_stats(QT);
   constexpr int STAGE = 2 * IMG + 8 * NS;  // Q, dO, -lse and -D of a tile
-  constexpr bool VLDS = KvShape<T, D>::VLDS, AHEAD = read_ahead<T, D>();
+  constexpr bool VLDS = cross_v_in_lds(sizeof(T), D), AHEAD = read_ahead<T, D>();
   extern __shared__ __align__(1024) char smem[];
   const char* vimg = smem + 2 * STAGE;
   float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS ? KEYS * Tile::ROWB : 0));
@@ -277,7 +322,9 @@ cross_bwd_kv_kernel(CrossArgs a) {
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
   const int nbk = a.B * a.kvh;
-  const int bk = blockIdx.x % nbk, tile = blockIdx.x / nbk;  // causal: heaviest first
+  const int ntile = cross_tiles(a.Sk, KEYS);
+  const int bk = blockIdx.x % nbk, y = blockIdx.x / nbk;
+  const int tile = y % ntile, part = y / ntile;  // causal: heaviest first
   const int b = bk / a.kvh, kv = bk % a.kvh;
   const int len = seq_len(a, b), start = seq_start(a, b);
   const int kw = wave % KW, qh = wave / KW;
@@ -287,7 +334,10 @@ cross_bwd_kv_kernel(CrossArgs a) {
   if (a.causal) first = max(0, key0 - start) / QT;
   int per = max(0, (a.Sq + QT - 1) / QT - first);
   if (key0 >= len) per = 0;
-  const int nt = per * a.group;
+  // the workgroup's tiles, over the heads of the group
+  const int all = per * a.group;
+  const int t0 = int(int64_t(all) * part / a.kv_parts);
+  const int t1 = int(int64_t(all) * (part + 1) / a.kv_parts);
 
   const uint32_t lds0 = lds_addr(smem);
   auto issue = [&](int t) {
@@ -308,8 +358,8 @@ cross_bwd_kv_kernel(CrossArgs a) {
       }
     }
   };
-  if (nt > 0) {
-    issue(0);
+  if (t1 > t0) {
+    issue(t0);
     if constexpr (VLDS)
       Tile::template issue<KEYS, NW>(a.v.p + b * a.v.b + kv * a.v.h + int64_t(key0) * a.v.t,
                                         a.v.t, len - key0, lds0 + 2 * STAGE, wave, lane);
@@ -317,7 +367,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
 
   typename Tile::RowFrag kf, vf;
   const int jc = max(0, min(j, len - 1));
-  if (nt > 0) {
+  if (t1 > t0) {
     Tile::load_row(kf, a.k.p + b * a.k.b + kv * a.k.h + int64_t(jc) * a.k.t, half);
     if constexpr (!VLDS) Tile::load_row(vf, a.v.p + b * a.v.b + kv * a.v.h + int64_t(jc) * a.v.t, half);
   }
@@ -327,33 +377,34 @@ cross_bwd_kv_kernel(CrossArgs a) {
     dk[d] = floatx16{};
     dv[d] = floatx16{};
   }
-  // the bias gradient's part of this workgroup's keys and head h
-  auto part = [&](int h) {
-    return a.dbias_part + ((int64_t(h) * a.B + b) * cross_tiles(a.Sk, KEYS) + tile) * a.bias.buckets;
+  // the bias gradient's sums of this workgroup's tiles of head h (of the group)
+  auto sums_of = [&](int h) {
+    const int64_t at = (int64_t(kv * a.group + h) * a.B + b) * ntile + tile;
+    return a.dbias_part + (at * a.kv_parts + part) * a.bias.buckets;
   };
   if constexpr (BIAS) {
     sums.init(tab + bias_span(a.bias), a.bias, wave);
-    if (nt == 0)
-      for (int x = tid; x < a.group * a.bias.buckets; x += 64 * NW)
-        part(kv * a.group + x / a.bias.buckets)[x % a.bias.buckets] = 0.f;
+    for (int x = tid; x < a.group * a.bias.buckets; x += 64 * NW) {
+      const int h = x / a.bias.buckets;
+      if (t0 >= t1 || t0 >= (h + 1) * per || t1 <= h * per) sums_of(h)[x % a.bias.buckets] = 0.f;
+    }
   }
   const float c = a.scale * LOG2E;
-  for (int t = 0; t < nt; ++t) {
+  for (int t = t0; t < t1; ++t) {
     wait_vmcnt<0>();
     __syncthreads();
-    if (t + 1 < nt) issue(t + 1);
+    if (t + 1 < t1) issue(t + 1);
     if constexpr (BIAS) {
-      if (t % per == 0) {  // the next head (every wave is past the last one's tiles)
-        const int h = kv * a.group + t / per;
-        if (t > 0) sums.flush(a.bias, part(h - 1), tid, lane, wave);
-        bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
+      if (t == t0 || t % per == 0) {  // the next head (every wave is past the last one's tiles)
+        if (t > t0) sums.flush(a.bias, sums_of(t / per - 1), tid, lane, wave);
+        bias_spread(tab, a.bias, kv * a.group + t / per, a.nh, tid, 64 * NW);
         __syncthreads();
         sums.clear(tid);
         __syncthreads();
       }
     }
     const int i0 = (first + t % per) * QT;
-    if (w0 >= len || (a.causal && start + i0 + 32 * NB * (qh + 1) - 1 < w0)) continue;
+    if (w0 >= len || i0 + 32 * NB * qh >= a.Sq || (a.causal && start + i0 + 32 * NB * (qh + 1) - 1 < w0)) continue;
     const char* img = smem + (t & 1) * STAGE;
     const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
     const float* nds = nls + NS;
@@ -442,7 +493,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
     }
   }
   if constexpr (BIAS) {
-    if (nt > 0) sums.flush(a.bias, part(kv * a.group + a.group - 1), tid, lane, wave);
+    if (t1 > t0) sums.flush(a.bias, sums_of((t1 - 1) / per), tid, lane, wave);
   }
   if constexpr (QH > 1) {
     // the others' sums to the first wave of the keys, one gradient after the other
@@ -477,23 +528,28 @@ cross_bwd_kv_kernel(CrossArgs a) {
       dv[d] = floatx16{};
     }
   }
+  if (a.kv_parts > 1) {
+    const int64_t rows = int64_t(a.B) * a.kvh * a.Sk;
+    const int64_t at = (part * rows + int64_t(bk) * a.Sk + j) * D;
+    Tile::store_sums(a.part_dk + at, dk, valid, half);
+    Tile::store_sums(a.part_dv + at, dv, valid, half);
+    return;
+  }
   Tile::store_row(a.dk.p + b * a.dk.b + kv * a.dk.h + int64_t(j) * a.dk.t, dk, a.scale, valid, half);
   Tile::store_row(a.dv.p + b * a.dv.b + kv * a.dv.h + int64_t(j) * a.dv.t, dv, 1.f, valid, half);
 }
 
-template <typename T, int D>
-size_t q_lds(const CrossArgs& a, int KS) {
-  return size_t(4) * cross_rows<T>(KS) * D * sizeof(T) +
-         (a.bias.buckets ? size_t(bias_span_h(a.bias)) * 4 : 0);
-}
-
 template <typename T, int D, bool BIAS, int NQ, int KS>
 hipError_t run_q(const CrossArgs& a, hipStream_t s) {
-  const size_t lds = q_lds<T, D>(a, KS);
+  const size_t lds = cross_q_lds(sizeof(T), D, KS, BIAS ? bias_span_h(a.bias) : 0);
   hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS, NQ, KS>>(CROSS_LDS - 2048);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NQ);
+  const int64_t heads = int64_t(a.B) * a.nh;
+  const int64_t grid = heads * cross_tiles(a.Sq, 32 * NQ) * a.q_parts;
   cross_bwd_q_kernel<T, D, BIAS, NQ, KS><<<dim3(uint32_t(grid)), 64 * NQ * KS, lds, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || a.q_parts == 1) return e;
+  const int64_t n = heads * a.Sq * (D / 4);
+  cross_join_q_kernel<T, D><<<dim3(uint32_t((n + 255) / 256)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -501,54 +557,49 @@ template <typename T, int D, bool BIAS, int KW, int QH>
 hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
   hipError_t e = lds_limit<cross_bwd_kv_kernel<T, D, BIAS, KW, QH>>(CROSS_LDS);
   if (e != hipSuccess) return e;
-  const size_t lds = kv_lds<T, D, KW, QH>(BIAS ? bias_span_h(a.bias) : 0);
-  const int64_t grid = int64_t(a.B) * a.kvh * cross_tiles(a.Sk, 32 * KW);
+  const size_t lds = cross_kv_lds(sizeof(T), D, KW, QH, BIAS ? bias_span_h(a.bias) : 0);
+  const int64_t heads = int64_t(a.B) * a.kvh;
+  const int64_t grid = heads * cross_tiles(a.Sk, 32 * KW) * a.kv_parts;
   cross_bwd_kv_kernel<T, D, BIAS, KW, QH><<<dim3(uint32_t(grid)), 64 * KW * QH, lds, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess || !BIAS) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.kv_parts > 1) {
+    const int64_t n = heads * a.Sk * (D / 4);
+    cross_join_kv_kernel<T, D><<<dim3(uint32_t((n + 255) / 256), 2), 256, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (!BIAS) return hipSuccess;
   cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
-      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk, 32 * KW), a.bias.buckets, a.nh);
+      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk, 32 * KW) * a.kv_parts, a.bias.buckets, a.nh);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cross_bwd_q(const CrossArgs& a, int dtype, int D, hipStream_t s) {
+hipError_t launch_cross_bwd_q(const CrossArgs& a, const CrossPlan& p, int dtype, int D,
+                              hipStream_t s) {
   return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
     using T = typename decltype(t)::type;
     constexpr int DD = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
-    const int64_t heads = int64_t(a.B) * a.nh, blocks = cross_tiles(a.Sk, 32);
-    if constexpr (DD * sizeof(T) < 512)  // (four 32-row tiles of 512 bytes do not fit LDS)
-      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), q_lds<T, DD>(a, 4), 2, blocks))
-        return run_q<T, DD, BIAS, 1, 4>(a, s);
-    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), q_lds<T, DD>(a, 2), 2, blocks))
-      return run_q<T, DD, BIAS, 2, 2>(a, s);
-    return run_q<T, DD, BIAS, 4, 1>(a, s);
+    if constexpr (DD * sizeof(T) < 512)
+      if (p.q_split == 4) return run_q<T, DD, BIAS, 1, 4>(a, s);
+    return p.q_split == 2 ? run_q<T, DD, BIAS, 2, 2>(a, s) : run_q<T, DD, BIAS, 4, 1>(a, s);
   });
 }
 
-hipError_t launch_cross_bwd_kv(const CrossArgs& a, int dtype, int D, hipStream_t s) {
+hipError_t launch_cross_bwd_kv(const CrossArgs& a, const CrossPlan& p, int dtype, int D,
+                               hipStream_t s) {
   return cross_pick(dtype, D, a.bias.buckets > 0, [&](auto t, auto d, auto bias) {
     using T = typename decltype(t)::type;
     constexpr int DD = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
-    const int64_t heads = int64_t(a.B) * a.kvh;
-    const int64_t blocks = int64_t(a.group) * cross_tiles(a.Sq, 32);
-    const int64_t one = heads * cross_tiles(a.Sk, 32), two = heads * cross_tiles(a.Sk, 64);
-    const int span = BIAS ? bias_span_h(a.bias) : 0;
-    if constexpr (KvShape<T, DD>::VLDS) {
-      // (8 waves a workgroup, and a CU; the sums of a wide bias leave room for 4)
-      if (cross_split_pays(4, two, kv_lds<T, DD, 2, 4>(span), 1, blocks))
-        return run_kv<T, DD, BIAS, 2, 4>(a, s);
-      if (kv_lds<T, DD, 4, 2>(span) <= CROSS_LDS) return run_kv<T, DD, BIAS, 4, 2>(a, s);
-      return run_kv<T, DD, BIAS, 2, 2>(a, s);
+    if constexpr (cross_v_in_lds(sizeof(T), DD)) {
+      if (p.kv_split == 4) return run_kv<T, DD, BIAS, 2, 4>(a, s);
+      return p.kv_keys == 2 ? run_kv<T, DD, BIAS, 2, 2>(a, s) : run_kv<T, DD, BIAS, 4, 2>(a, s);
     } else {
       if constexpr (DD * sizeof(T) < 512)
-        if (cross_split_pays(4, one, kv_lds<T, DD, 1, 4>(span), 2, blocks))
-          return run_kv<T, DD, BIAS, 1, 4>(a, s);
-      if (cross_split_pays(2, two, kv_lds<T, DD, 2, 2>(span), 2, blocks))
-        return run_kv<T, DD, BIAS, 2, 2>(a, s);
-      return run_kv<T, DD, BIAS, 4, 1>(a, s);
+        if (p.kv_split == 4) return run_kv<T, DD, BIAS, 1, 4>(a, s);
+      return p.kv_split == 2 ? run_kv<T, DD, BIAS, 2, 2>(a, s) : run_kv<T, DD, BIAS, 4, 1>(a, s);
     }
   });
 }

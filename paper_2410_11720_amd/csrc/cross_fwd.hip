@@ -102,7 +102,7 @@ __device__ __forceinline__ char* rest_row(const CrossArgs& a, int b, int h, int 
 template <typename T, int D, bool BIAS, int NQ, int KS>
 __global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
-  constexpr int NW = NQ * KS, KT = cross_rows<T>(KS), NB = KT / 32 / KS;
+  constexpr int NW = NQ * KS, KT = cross_rows(sizeof(T), KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
@@ -457,15 +457,9 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
     a.lse[(int64_t(b) * a.nh + h) * a.Sq + i] = l == 0.f ? NEG_INF : m + log2_hw(l);
 }
 
-template <typename T, int D>
-size_t fwd_lds(const CrossArgs& a, int KS) {
-  return size_t(4) * cross_rows<T>(KS) * D * sizeof(T) +
-         (a.bias.buckets ? size_t(bias_span_h(a.bias)) * 4 : 0);
-}
-
 template <typename T, int D, bool BIAS, int NQ, int KS>
 hipError_t run_fwd(const CrossArgs& a, hipStream_t s) {
-  const size_t lds = fwd_lds<T, D>(a, KS);
+  const size_t lds = cross_q_lds(sizeof(T), D, KS, BIAS ? bias_span_h(a.bias) : 0);
   hipError_t e = lds_limit<cross_fwd_kernel<T, D, BIAS, NQ, KS>>(CROSS_LDS);
   if (e != hipSuccess) return e;
   const int64_t grid = int64_t(a.B) * a.nh * cross_tiles(a.Sq, 32 * NQ);
@@ -496,11 +490,12 @@ hipError_t launch_cross_fwd(const CrossArgs& a, int dtype, int D, hipStream_t s)
     constexpr int D = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
     const int64_t heads = int64_t(a.B) * a.nh, blocks = cross_tiles(a.Sk, 32);
-    const int most = sizeof(T) * D == 128 ? 3 : 2;
+    const int most = sizeof(T) * D == 128 ? 3 : 2, span = BIAS ? bias_span_h(a.bias) : 0;
+    auto lds = [&](int split) { return cross_q_lds(sizeof(T), D, split, span); };
     if constexpr (D * sizeof(T) < 512)  // (four 32-row tiles of 512 bytes do not fit LDS)
-      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), fwd_lds<T, D>(a, 4), most, blocks))
+      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), lds(4), most, blocks))
         return run_fwd<T, D, BIAS, 1, 4>(a, s);
-    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), fwd_lds<T, D>(a, 2), most, blocks))
+    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), lds(2), most, blocks))
       return run_fwd<T, D, BIAS, 2, 2>(a, s);
     return run_fwd<T, D, BIAS, 4, 1>(a, s);
   });

@@ -46,16 +46,6 @@ __device__ __forceinline__ void issue_loads() {
   if constexpr (ON) __builtin_amdgcn_sched_barrier(0);
 }
 
-// Rows of a tile of the other axis, for S waves that share it.
-template <typename T>
-constexpr int cross_rows(int S) {
-  const int least = sizeof(T) == 2 ? 64 : 32;
-  return least > 32 * S ? least : 32 * S;
-}
-
-// Entries of a tile's row statistics in LDS (copied 64 at a time).
-constexpr int cross_stats(int rows) { return rows < 64 ? 64 : rows; }
-
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 // Keys of a sequence, and the position of its first query among them (values
@@ -333,6 +323,17 @@ struct CrossTile {
       }
     }
   }
+  // The same in fp32, unscaled: a part's sums.
+  __device__ static __forceinline__ void store_sums(float* row, const floatx16 (&c)[ND], bool valid,
+                                                    int half) {
+    if (!valid) return;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<floatx4*>(row + 32 * d + 8 * k + 4 * half) =
+            floatx4{c[d][4 * k], c[d][4 * k + 1], c[d][4 * k + 2], c[d][4 * k + 3]};
+  }
   // 8 elements of a row from both halves' groups of 4
   __device__ static __forceinline__ void store8(char* p, const float (&x)[8], bool valid) {
     const u32x2 a = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -483,7 +484,7 @@ struct BiasSums {
   }
   // Joins the arrays by t and writes the sum of every bucket. Called by the whole
   // workgroup, whose arrays are then free (behind a barrier). A side's buckets are
-  // runs of t; a thread sums one bucket's run.
+  // runs of t.
   __device__ __forceinline__ void flush(const CrossBias& b, float* out, int tid, int lane,
                                         int wave) {
     lo = group_sum<64>(lo);
@@ -509,8 +510,10 @@ struct BiasSums {
       below += ends[2 * w];
       above += ends[2 * w + 1];
     }
-    for (int k = tid; k < b.buckets; k += 64 * NW) {
+    // eight lanes a bucket
+    for (int x = tid; x < 8 * b.buckets; x += 64 * NW) {
       // distances [n0, n1) of the bucket; the last one of a side is open
+      const int k = x >> 3, j = x & 7;
       const int u = k % b.side;
       const bool ahead = k >= b.side, last = u == b.side - 1;
       const int n0 = u <= b.exact ? u : b.border[u - b.exact];
@@ -518,18 +521,19 @@ struct BiasSums {
       float v = 0.f;
       if (!ahead) {
         const int t0 = last ? b.lo - BIAS_PAD : 1 - n1;
-        for (int t = t0; t <= -n0; ++t) v += tab[t];
-        if (last) v += below;
+        for (int t = t0 + j; t <= -n0; t += 8) v += tab[t];
+        if (last && j == 0) v += below;
         if (!b.bidirectional && u == 0) {  // keys ahead share the bucket of t = 0
-          for (int t = 1; t <= b.hi + BIAS_PAD; ++t) v += tab[t];
-          v += above;
+          for (int t = 1 + j; t <= b.hi + BIAS_PAD; t += 8) v += tab[t];
+          if (j == 0) v += above;
         }
       } else {
         const int t1 = last ? b.hi + BIAS_PAD : n1 - 1;
-        for (int t = max(n0, 1); t <= t1; ++t) v += tab[t];
-        if (last) v += above;
+        for (int t = max(n0, 1) + j; t <= t1; t += 8) v += tab[t];
+        if (last && j == 0) v += above;
       }
-      out[k] = v;
+      v = group_sum<8>(v);
+      if (j == 0) out[k] = v;
     }
   }
 };

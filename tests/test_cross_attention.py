@@ -190,6 +190,15 @@ GRID = [
     (C(1, 96, 800, 2, 128, buckets=128, max_distance=1024), None, None),
     (C(1, 96, 800, 2, 128, dtype="f32", buckets=128, max_distance=1024), None, None),
     (C(1, 96, 800, 2, 64, dtype="f32", buckets=128, max_distance=1024), None, None),
+    # one axis over several workgroups, whose sums are joined
+    (C(1, 600, 40, 8, 64, kv_heads=1, buckets=32), [37], None),
+    (C(2, 525, 25, 8, 64, kv_heads=1, dtype="f32"), [25, 0], None),
+    (C(1, 40, 2000, 1, 128), [1990], None),
+    (C(2, 33, 1500, 2, 64, buckets=32), [1500, 70], [700, -5]),
+    (C(1, 700, 700, 2, 64, causal=True, buckets=32, bidirectional=False), None, None),
+    (C(2, 300, 900, 4, 128, kv_heads=1, causal=True, buckets=8), [900, 31], [600, -270]),
+    (C(1, 90, 1100, 2, 128, dtype="f32", buckets=32), None, None),
+    (C(1, 800, 90, 6, 128, kv_heads=2, dtype="f32", causal=True), None, [-100]),
     # another scale
     (C(1, 50, 60, 2, 64, scale=0.3), None, None),
 ]
