@@ -124,6 +124,10 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
     return x;
   };
 
+  // -D in every register of a block: what the products that form dP - D start
+  // from (where registers last; else moves before each product, a quarter of the
+  // vector instructions at head dim 64)
+  floatx16 minus_d = nd;
   floatx16 dq[Tile::ND];
 #pragma unroll
   for (int d = 0; d < Tile::ND; ++d) dq[d] = floatx16{};
@@ -148,8 +152,12 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
         Tile::load_rows(vf, img + IMG, 32 * n, lane);
         issue_loads<AHEAD>();
         Tile::rows(s, kf, q);
+        if constexpr (AHEAD) {
+          dp = minus_d;
+        } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = nd;
+          for (int r = 0; r < 16; ++r) dp[r] = nd;
+        }
         Tile::rows(dp, vf, g);
         typename Tile::ColFrag kc;
         if constexpr (AHEAD) Tile::load_cols(kc, img, 32 * n, lane);
@@ -187,6 +195,7 @@ __global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void 
       if (sweep == 0) {
         nd -= join_sum(sum);
         sum = 0.f;
+        minus_d = nd;
       }
     }
   }
@@ -340,13 +349,28 @@ cross_bwd_kv_kernel(CrossArgs a) {
   const int t1 = int(int64_t(all) * (part + 1) / a.kv_parts);
 
   const uint32_t lds0 = lds_addr(smem);
+  // (tile of the head, head of the group) of the next copy and of this step,
+  // counted along: divisions would be vector code
+  struct Place {
+    int i, h, per;
+    __device__ __forceinline__ void step() {
+      if (++i == per) {
+        i = 0;
+        ++h;
+      }
+    }
+  };
+  Place ahead{0, 0, per};
+  if (t1 > t0) ahead = Place{t0 % per, t0 / per, per};
+  Place now = ahead;
   auto issue = [&](int t) {
-    const int h = kv * a.group + t / per, i0 = (first + t % per) * QT;
+    const int h = kv * a.group + ahead.h, i0 = (first + ahead.i) * QT;
+    ahead.step();
     const uint32_t to = lds0 + (t & 1) * STAGE;
     Tile::template issue<QT, NW>(a.q.p + b * a.q.b + h * a.q.h + int64_t(i0) * a.q.t, a.q.t,
-                                a.Sq - i0, to, wave, lane);
+                                 a.Sq - i0, to, wave, lane);
     Tile::template issue<QT, NW>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
-                                a.dout.t, a.Sq - i0, to + IMG, wave, lane);
+                                 a.dout.t, a.Sq - i0, to + IMG, wave, lane);
     const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i0;
     if (wave < 2) {  // (64 at a time; a 32-row tile uses half of them)
 #pragma unroll
@@ -390,20 +414,20 @@ cross_bwd_kv_kernel(CrossArgs a) {
     }
   }
   const float c = a.scale * LOG2E;
-  for (int t = t0; t < t1; ++t) {
+  for (int t = t0; t < t1; ++t, now.step()) {
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < t1) issue(t + 1);
     if constexpr (BIAS) {
-      if (t == t0 || t % per == 0) {  // the next head (every wave is past the last one's tiles)
-        if (t > t0) sums.flush(a.bias, sums_of(t / per - 1), tid, lane, wave);
-        bias_spread(tab, a.bias, kv * a.group + t / per, a.nh, tid, 64 * NW);
+      if (t == t0 || now.i == 0) {  // the next head (every wave is past the last one's tiles)
+        if (t > t0) sums.flush(a.bias, sums_of(now.h - 1), tid, lane, wave);
+        bias_spread(tab, a.bias, kv * a.group + now.h, a.nh, tid, 64 * NW);
         __syncthreads();
         sums.clear(tid);
         __syncthreads();
       }
     }
-    const int i0 = (first + t % per) * QT;
+    const int i0 = (first + now.i) * QT;
     if (w0 >= len || i0 + 32 * NB * qh >= a.Sq || (a.causal && start + i0 + 32 * NB * (qh + 1) - 1 < w0)) continue;
     const char* img = smem + (t & 1) * STAGE;
     const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
@@ -462,7 +486,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
       for (int r = 0; r < 16; r += 4) {
         const floatx4 l = *reinterpret_cast<const floatx4*>(nlr + 2 * r);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[r + e] = exp2_hw(fmaf(s[r + e], ce, l[e] + off));
+        for (int e = 0; e < 4; ++e) s[r + e] = exp2_hw(fmaf(s[r + e], ce, BIAS ? l[e] + off : l[e]));
       }
       typename Tile::Probs p;
       Tile::pack(p, s);
