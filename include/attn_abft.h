@@ -362,9 +362,10 @@ typedef struct {
 
 /* A tensor [batch, tokens, heads, head_dim]; strides in elements, the last
  * one 1. data (device) and all strides are multiples of 16 bytes, a token
- * stride is at most 16 MiB. Inputs may repeat memory (stride 0), outputs not.
- * Strides of dimensions of extent 1 and tensors without elements are not
- * looked at. */
+ * stride is at most 16 MiB. Inputs may repeat memory (stride 0), outputs not:
+ * sorted, an output's strides each pass the extent of the one before. An output
+ * shares memory with no other argument. Strides of dimensions of extent 1 and
+ * tensors without elements are not looked at. */
 typedef struct {
   const void* data;
   int64_t batch_stride, token_stride, head_stride;
@@ -444,7 +445,8 @@ size_t clip_gradients_workspace_bytes(int32_t n);
 
 /* grads (host) n entries, any mix of types and sizes; stats (device, 8-byte
  * aligned) receives norm and nonfinite (and coef: 1 from global_grad_norm).
- * max_norm >= 0. An output that overlaps another one is ABFT_ERR_INVALID. */
+ * max_norm >= 0. An output that overlaps another one, or another gradient, is
+ * ABFT_ERR_INVALID. */
 int global_grad_norm(const abft_grad* grads, int32_t n, abft_grad_stats* stats, void* workspace,
                      size_t workspace_bytes, void* stream);
 int clip_gradients(const abft_grad* grads, int32_t n, double max_norm, abft_grad_stats* stats,

@@ -86,7 +86,7 @@ bool short_form(const attn_cross_config* c, int* splits) {
   const int64_t row = int64_t(c->head_dim) * es_of(c);     // bytes
   const int64_t rows = int64_t(c->q_len) * (c->heads / c->kv_heads);
   const int64_t base = int64_t(c->batch) * c->kv_heads * ((rows + 31) / 32);
-  if (base == 0) return false;
+  if (base == 0 || rows > 65536) return false;
   const int64_t steps = (int64_t(c->k_len) + 127) / 128;
   const int64_t slots = row == 128 ? 512 : 256;            // workgroups at a time, by LDS
   const int64_t join = es_of(c) == 4 ? 1 : (row == 128 ? 5 : 4);
@@ -147,7 +147,16 @@ int take(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh, 
   for (int k = 0; k < 3; ++k) {
     if (ext[k] == 1) continue;                  // the stride is not used
     if (st[k] < 0 || (st[k] * es) % 16) return ABFT_ERR_INVALID;
-    if (out && st[k] < c->head_dim) return ABFT_ERR_INVALID;  // rows written twice
+  }
+  if (out) {  // no element is written twice: from the smallest stride up, each passes the last
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int x, int y) { return st[x] < st[y]; });
+    int64_t extent = c->head_dim;
+    for (int k : order) {
+      if (ext[k] == 1) continue;
+      if (st[k] < extent) return ABFT_ERR_INVALID;
+      extent = st[k] * ext[k];
+    }
   }
   if (n > 1 && st[1] * es > MAX_TOKEN_BYTES) return ABFT_ERR_UNSUPPORTED;
   r->p = static_cast<char*>(const_cast<void*>(t->data));

@@ -215,26 +215,32 @@ bool valid_list(const abft_grad* g, int32_t n, bool out) {
   return true;
 }
 
-// Whether two outputs share memory (an element would be scaled twice).
+// Whether an output shares memory with another output or another gradient (an
+// element would be scaled twice, or read after it was written).
 bool outputs_overlap(const abft_grad* g, int32_t n) {
-  auto begin = [&](int32_t i) { return reinterpret_cast<uintptr_t>(g[i].out); };
-  auto end = [&](int32_t i) {
-    return begin(i) + uintptr_t(g[i].numel) * (g[i].dtype == ABFT_FP32 ? 4 : 2);
+  struct Range {
+    uintptr_t begin, end;
+    bool out;
+    int32_t i;
   };
-  bool ascending = true;
-  uintptr_t last = 0;
-  for (int32_t i = 0; i < n && ascending; ++i) {
+  std::vector<Range> v;
+  v.reserve(2 * size_t(n));
+  for (int32_t i = 0; i < n; ++i) {
     if (g[i].numel == 0) continue;
-    ascending = begin(i) >= last;
-    last = end(i);
+    const uintptr_t bytes = uintptr_t(g[i].numel) * (g[i].dtype == ABFT_FP32 ? 4 : 2);
+    const uintptr_t in = reinterpret_cast<uintptr_t>(g[i].grad);
+    const uintptr_t out = reinterpret_cast<uintptr_t>(g[i].out);
+    v.push_back({out, out + bytes, true, i});
+    if (in != out) v.push_back({in, in + bytes, false, i});
   }
-  if (ascending) return false;
-  std::vector<std::pair<uintptr_t, uintptr_t>> v;
-  for (int32_t i = 0; i < n; ++i)
-    if (g[i].numel > 0) v.emplace_back(begin(i), end(i));
-  std::sort(v.begin(), v.end());
-  for (size_t i = 1; i < v.size(); ++i)
-    if (v[i].first < v[i - 1].second) return true;
+  std::sort(v.begin(), v.end(), [](const Range& x, const Range& y) { return x.begin < y.begin; });
+  // the ends furthest up among outputs and among gradients so far
+  uintptr_t end_out = 0, end_in = 0;
+  for (const Range& r : v) {
+    if (r.begin < end_out || (r.out && r.begin < end_in)) return true;
+    uintptr_t& end = r.out ? end_out : end_in;
+    end = std::max(end, r.end);
+  }
   return false;
 }
 

@@ -90,6 +90,8 @@ def test_forward_refuses_before_any_launch():
     assert _forward_status(cfg, k=_c_tensor(8192, ks, (-768, 256, 64))) == -1
     assert _forward_status(cfg, k=_c_tensor(8192, ks, (2 ** 26, 2 ** 24, 64))) == -2
     assert _forward_status(cfg, o=_c_tensor(4096, qs, (768, 0, 64))) == -1  # written twice
+    assert _forward_status(cfg, o=_c_tensor(4096, qs, (768, 64, 64))) == -1  # heads on tokens
+    assert _forward_status(cfg, o=_c_tensor(4096, qs, (64, 64, 768))) == -1
     assert _forward_status(cfg, bias=4096) == -1                        # a table without buckets
     assert _forward_status(_cfg(buckets=32)) == -1                      # buckets without a table
     long = _cfg(batch=1, q_len=1, k_len=8192)

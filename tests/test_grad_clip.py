@@ -34,6 +34,11 @@ def test_refusals_before_any_launch():
     # the same output twice, and two that share a part, in any order
     assert _status([ok, ok]) == -1
     assert _status([(8192, 8192, 100, 1), (4096, 8188, 2, 1)]) == -1
+    # an output on another gradient, on a part of its own, or two exchanged
+    assert _status([(4096, 8192, 10, 1), (8192, 16384, 10, 1)]) == -1
+    assert _status([(4096, 4100, 10, 1)]) == -1
+    assert _status([(4096, 8192, 10, 1), (8192, 4096, 10, 1)]) == -1
+    assert _status([(4096, 4096, 10, 1), (4116, 4116, 10, 1)]) == -1
     assert abft._lib.clip_gradients_workspace_bytes(-1) == 0
     assert abft._lib.clip_gradients_workspace_bytes(0) > 0
 
