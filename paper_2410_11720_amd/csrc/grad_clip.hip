@@ -151,23 +151,37 @@ __global__ __launch_bounds__(NT) void grad_stats_kernel(const GradPartial* part,
 }
 
 template <typename T>
+__device__ __forceinline__ u32x4 scaled(u32x4 x, float f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2)
+      x[e] = uint32_t(f2bf(__uint_as_float(x[e] << 16) * f)) |
+             (uint32_t(f2bf(__uint_as_float(x[e] & 0xffff0000u) * f)) << 16);
+    else
+      x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+  }
+  return x;
+}
+
+template <typename T>
 __device__ __forceinline__ void scale_chunk(const T* g, T* o, int n, float f) {
   constexpr int V = 16 / int(sizeof(T));
   int at = 0;
   if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(o)) % 16 == 0) {
     const int nv = n / V;
-    for (int i = threadIdx.x; i < nv; i += NT) {
-      u32x4 x = reinterpret_cast<const u32x4*>(g)[i];
+    const u32x4* p = reinterpret_cast<const u32x4*>(g);
+    u32x4* q = reinterpret_cast<u32x4*>(o);
+    constexpr int U = 4;
+    int i = threadIdx.x;
+    for (; i + (U - 1) * NT < nv; i += U * NT) {
+      u32x4 x[U];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 2)
-          x[e] = uint32_t(f2bf(__uint_as_float(x[e] << 16) * f)) |
-                 (uint32_t(f2bf(__uint_as_float(x[e] & 0xffff0000u) * f)) << 16);
-        else
-          x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
-      }
-      reinterpret_cast<u32x4*>(o)[i] = x;
+      for (int u = 0; u < U; ++u) x[u] = __builtin_nontemporal_load(p + i + u * NT);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        __builtin_nontemporal_store(scaled<T>(x[u], f), q + i + u * NT);
     }
+    for (; i < nv; i += NT) q[i] = scaled<T>(p[i], f);
     at = nv * V;
   }
   for (int i = at + threadIdx.x; i < n; i += NT)
@@ -175,7 +189,9 @@ __device__ __forceinline__ void scale_chunk(const T* g, T* o, int n, float f) {
 }
 
 // Chunks are taken from the last on: the end of what the sums read is still in
-// the cache.
+// the cache. Both the last reading and the result go past it (12 attention
+// layers of 768 in fp32, tensors not in any cache before: 75.6 -> 60.0 us; 3.8
+// TB/s of gradients read once and written once, 5.7 counting both readings).
 __global__ __launch_bounds__(NT) void grad_scale_kernel(GradList L, const GradPartial* part,
                                                         int n_part, double max_norm,
                                                         abft_grad_stats* stats) {
