@@ -323,10 +323,12 @@ cross_bwd_kv_kernel(CrossArgs a) {
   constexpr int IMG = QT * Tile::ROWB;
   constexpr int NS = cross_stats(QT);
   constexpr int STAGE = 2 * IMG + 8 * NS;  // Q, dO, -lse and -D of a tile
+  constexpr bool KLDS = cross_k_in_lds(sizeof(T), D, QH, BIAS);
   constexpr bool VLDS = cross_v_in_lds(sizeof(T), D), AHEAD = read_ahead<T, D>();
   extern __shared__ __align__(1024) char smem[];
   const char* vimg = smem + 2 * STAGE;
-  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS ? KEYS * Tile::ROWB : 0));
+  const char* kimg = vimg + KEYS * Tile::ROWB;
+  float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS + KLDS) * KEYS * Tile::ROWB);
   BiasSums<NW> sums;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
@@ -386,14 +388,20 @@ cross_bwd_kv_kernel(CrossArgs a) {
     issue(t0);
     if constexpr (VLDS)
       Tile::template issue<KEYS, NW>(a.v.p + b * a.v.b + kv * a.v.h + int64_t(key0) * a.v.t,
-                                        a.v.t, len - key0, lds0 + 2 * STAGE, wave, lane);
+                                     a.v.t, len - key0, lds0 + 2 * STAGE, wave, lane);
+    if constexpr (KLDS)
+      Tile::template issue<KEYS, NW>(a.k.p + b * a.k.b + kv * a.k.h + int64_t(key0) * a.k.t,
+                                     a.k.t, len - key0, lds0 + 2 * STAGE + KEYS * Tile::ROWB, wave,
+                                     lane);
   }
 
   typename Tile::RowFrag kf, vf;
   const int jc = max(0, min(j, len - 1));
   if (t1 > t0) {
-    Tile::load_row(kf, a.k.p + b * a.k.b + kv * a.k.h + int64_t(jc) * a.k.t, half);
-    if constexpr (!VLDS) Tile::load_row(vf, a.v.p + b * a.v.b + kv * a.v.h + int64_t(jc) * a.v.t, half);
+    if constexpr (!KLDS)
+      Tile::load_row(kf, a.k.p + b * a.k.b + kv * a.k.h + int64_t(jc) * a.k.t, half);
+    if constexpr (!VLDS)
+      Tile::load_row(vf, a.v.p + b * a.v.b + kv * a.v.h + int64_t(jc) * a.v.t, half);
   }
   floatx16 dk[Tile::ND], dv[Tile::ND];
 #pragma unroll
@@ -428,7 +436,9 @@ cross_bwd_kv_kernel(CrossArgs a) {
       }
     }
     const int i0 = (first + now.i) * QT;
-    if (w0 >= len || i0 + 32 * NB * qh >= a.Sq || (a.causal && start + i0 + 32 * NB * (qh + 1) - 1 < w0)) continue;
+    if (w0 >= len || i0 + 32 * NB * qh >= a.Sq ||
+        (a.causal && start + i0 + 32 * NB * (qh + 1) - 1 < w0))
+      continue;
     const char* img = smem + (t & 1) * STAGE;
     const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
     const float* nds = nls + NS;
@@ -437,9 +447,13 @@ cross_bwd_kv_kernel(CrossArgs a) {
       const int n = qh * NB + m;
       floatx16 s = floatx16{}, dp;
       typename Tile::RowFrag af;
-      Tile::load_rows(af, img, 32 * n, lane);
-      issue_loads<AHEAD>();
-      Tile::rows(s, af, kf);
+      if constexpr (KLDS) {
+        Tile::rows(s, img, 32 * n, kimg, 32 * kw, lane);
+      } else {
+        Tile::load_rows(af, img, 32 * n, lane);
+        issue_loads<AHEAD>();
+        Tile::rows(s, af, kf);
+      }
       if constexpr (!VLDS) Tile::load_rows(af, img + IMG, 32 * n, lane);
       // (registers 4 q .. 4 q + 3: rows 8 q + 4 half on)
       const float* nlr = nls + 32 * n + 4 * half;

@@ -76,15 +76,20 @@ constexpr int cross_rows(int es, int split) {
 constexpr int cross_stats(int rows) { return std::max(64, rows); }
 
 // LDS of a workgroup: two stages of two images (forward, query pass); in the
-// key pass the statistics too, for bf16 rows of 256 bytes the values, and the sums
-// of the bias gradient.
+// key pass the statistics too, for bf16 rows of 256 bytes the values (and with a
+// bias the keys, which leaves its registers for the diagonal sums), and the sums of
+// the bias gradient.
 constexpr size_t cross_q_lds(int es, int D, int split, int span) {
   return size_t(4) * cross_rows(es, split) * D * es + size_t(span) * 4;
 }
 constexpr bool cross_v_in_lds(int es, int D) { return es == 2 && D == 128; }
+constexpr bool cross_k_in_lds(int es, int D, int QH, bool bias) {
+  return cross_v_in_lds(es, D) && bias && QH == 2;
+}
 constexpr size_t cross_kv_lds(int es, int D, int KW, int QH, int span) {
   return 2 * (size_t(2) * cross_rows(es, QH) * D * es + 8 * cross_stats(cross_rows(es, QH))) +
          (cross_v_in_lds(es, D) ? size_t(32) * KW * D * es : 0) +
+         (cross_k_in_lds(es, D, QH, span > 0) ? size_t(32) * KW * D * es : 0) +
          size_t(span ? KW * QH + 1 : 0) * span * 4;
 }
 
