@@ -259,29 +259,11 @@ __global__ __launch_bounds__(256) void cross_join_q_kernel(CrossArgs a) {
   }
 }
 
-// Joins the key pass's parts in their order: dk (y = 0) or dv.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_join_kv_kernel(CrossArgs a) {
-  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t r = x / (D / 4), rows = int64_t(a.B) * a.kvh * a.Sk;
-  const int e = int(x % (D / 4)) * 4;
-  if (r >= rows) return;
-  const float* from = blockIdx.y == 0 ? a.part_dk : a.part_dv;
-  const CrossTensor& to = blockIdx.y == 0 ? a.dk : a.dv;
-  floatx4 v = {};
-  for (int p = 0; p < a.kv_parts; ++p)
-    v += *reinterpret_cast<const floatx4*>(from + (p * rows + r) * D + e);
-  const int64_t bh = r / a.Sk, j = r % a.Sk;
-  const int b = int(bh / a.kvh), h = int(bh % a.kvh);
-  store4<T>(to.p + b * to.b + h * to.h + j * to.t + e * int(sizeof(T)),
-            v * (blockIdx.y == 0 ? a.scale : 1.f));
-}
-
 // Sums the key pass's partial bias gradients of one head in a fixed order.
-__global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, float* dbias, int n,
-                                                          int buckets, int heads) {
+__device__ __forceinline__ void sum_dbias(const float* part, float* dbias, int n, int buckets,
+                                          int heads, int h) {
   __shared__ float sh[256];
-  const int h = blockIdx.x, lanes = 256 / buckets;  // partial sums of a bucket
+  const int lanes = 256 / buckets;  // partial sums of a bucket
   const int k = threadIdx.x % buckets, j = threadIdx.x / buckets;
   float v = 0.f;
   if (j < lanes) {
@@ -302,6 +284,35 @@ __global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, flo
     for (int x = 1; x < lanes; ++x) v += sh[x * buckets + threadIdx.x];
     dbias[int64_t(threadIdx.x) * heads + h] = v;
   }
+}
+
+__global__ __launch_bounds__(256) void cross_dbias_kernel(const float* part, float* dbias, int n,
+                                                          int buckets, int heads) {
+  sum_dbias(part, dbias, n, buckets, heads, blockIdx.x);
+}
+
+// Joins the key pass's parts in their order: dk (y = 0) or dv (1), and the bias
+// gradient of head x (2), from n partial sums.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cross_join_kv_kernel(CrossArgs a, int n) {
+  if (blockIdx.y == 2) {
+    if (blockIdx.x < uint32_t(a.nh))
+      sum_dbias(a.dbias_part, a.dbias, n, a.bias.buckets, a.nh, blockIdx.x);
+    return;
+  }
+  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t r = x / (D / 4), rows = int64_t(a.B) * a.kvh * a.Sk;
+  const int e = int(x % (D / 4)) * 4;
+  if (r >= rows) return;
+  const float* from = blockIdx.y == 0 ? a.part_dk : a.part_dv;
+  const CrossTensor& to = blockIdx.y == 0 ? a.dk : a.dv;
+  floatx4 v = {};
+  for (int p = 0; p < a.kv_parts; ++p)
+    v += *reinterpret_cast<const floatx4*>(from + (p * rows + r) * D + e);
+  const int64_t bh = r / a.Sk, j = r % a.Sk;
+  const int b = int(bh / a.kvh), h = int(bh % a.kvh);
+  store4<T>(to.p + b * to.b + h * to.h + j * to.t + e * int(sizeof(T)),
+            v * (blockIdx.y == 0 ? a.scale : 1.f));
 }
 
 // ---- key pass ---------------------------------------------------------------
@@ -600,14 +611,16 @@ hipError_t run_kv(const CrossArgs& a, hipStream_t s) {
   const int64_t grid = heads * cross_tiles(a.Sk, 32 * KW) * a.kv_parts;
   cross_bwd_kv_kernel<T, D, BIAS, KW, QH><<<dim3(uint32_t(grid)), 64 * KW * QH, lds, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int n = a.B * cross_tiles(a.Sk, 32 * KW) * a.kv_parts;
   if (a.kv_parts > 1) {
-    const int64_t n = heads * a.Sk * (D / 4);
-    cross_join_kv_kernel<T, D><<<dim3(uint32_t((n + 255) / 256), 2), 256, 0, s>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t wgs = (heads * a.Sk * (D / 4) + 255) / 256;
+    const dim3 grid(uint32_t(BIAS ? std::max<int64_t>(wgs, a.nh) : wgs), BIAS ? 3 : 2);
+    cross_join_kv_kernel<T, D><<<grid, 256, 0, s>>>(a, n);
+    return hipGetLastError();
   }
   if (!BIAS) return hipSuccess;
-  cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(
-      a.dbias_part, a.dbias, a.B * cross_tiles(a.Sk, 32 * KW) * a.kv_parts, a.bias.buckets, a.nh);
+  cross_dbias_kernel<<<dim3(uint32_t(a.nh)), 256, 0, s>>>(a.dbias_part, a.dbias, n,
+                                                          a.bias.buckets, a.nh);
   return hipGetLastError();
 }
 
