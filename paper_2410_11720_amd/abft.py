@@ -501,7 +501,8 @@ class CrossAttention:
 
     Q, O, dO, dQ [batch, q_len, heads, head_dim]; K, V, dK, dV [batch, k_len,
     kv_heads, head_dim]; any strides with whole rows at multiples of 16 bytes
-    (views of packed projections, of a cache). bias, dbias [buckets, heads]
+    (views of packed projections, of a cache); results not given are laid out as
+    torch.empty_like of Q, K or V. bias, dbias [buckets, heads]
     fp32; k_lens, q_start [batch] int32."""
 
     def __init__(self, cfg: CrossConfig, device="cuda", training=True):
@@ -552,7 +553,7 @@ class CrossAttention:
 
     def forward(self, Q, K, V, bias=None, k_lens=None, q_start=None, O=None):
         if O is None:
-            O = torch.empty(self._q_shape, dtype=self.cfg.torch_dtype, device=self.device)
+            O = torch.empty_like(Q)
         qs, ks = self._q_shape, self._k_shape
         held, (q, k, v, o) = self._tensors("QKVO", (Q, K, V, O), (qs, ks, ks, qs))
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
@@ -566,11 +567,9 @@ class CrossAttention:
         c = self.cfg
         if self.lse is None:
             raise AbftError("backward: made with training=False")
-
-        def new(t, shape):
-            return t if t is not None else torch.empty(shape, dtype=c.torch_dtype,
-                                                       device=self.device)
-        dQ, dK, dV = new(dQ, self._q_shape), new(dK, self._k_shape), new(dV, self._k_shape)
+        dQ = torch.empty_like(Q) if dQ is None else dQ
+        dK = torch.empty_like(K) if dK is None else dK
+        dV = torch.empty_like(V) if dV is None else dV
         if dbias is None and c.buckets:
             dbias = torch.empty((c.buckets, c.heads), dtype=torch.float32, device=self.device)
         qs, ks = self._q_shape, self._k_shape
