@@ -412,8 +412,8 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
 int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* dO,
                         const attn_cross_tensor* Q, const attn_cross_tensor* K,
                         const attn_cross_tensor* V, const attn_cross_tensor* O, const float* lse,
-                        const void* rest, const float* bias, const int32_t* k_lens, const int32_t* q_start,
-                        const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
+                        const void* rest, const float* bias, const int32_t* k_lens,
+                        const int32_t* q_start, const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
                         const attn_cross_tensor* dV, float* dbias, void* workspace,
                         size_t workspace_bytes, void* stream);
 

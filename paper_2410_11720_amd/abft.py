@@ -483,13 +483,18 @@ def _data(t):
     return None if t is None else t.data_ptr()
 
 
+# (a stream object costs 2.7 us, a quarter of a small call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(fn, device, *args):
     """fn(*args, current stream of the device) with that device current."""
     index = device.index
     if index == torch.cuda.current_device():
-        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        return fn(*args, _raw_stream(index))
     with torch.cuda.device(index):
-        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        return fn(*args, _raw_stream(index))
 
 
 class CrossAttention:

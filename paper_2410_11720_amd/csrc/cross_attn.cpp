@@ -129,9 +129,11 @@ Space make_space(const attn_cross_config* c, const CrossPlan& p) {
                              p.kv_parts * c->buckets * 4);
   L.part = L.sum + (p.q_parts > 1 ? align_up(rows * 4 * p.q_parts) : 0);
   const size_t dq = size_t(c->batch) * c->heads * c->q_len * c->head_dim * 4;
-  const size_t dk = align_up(size_t(c->batch) * c->kv_heads * c->k_len * c->head_dim * 4 * p.kv_parts);
+  const size_t dk =
+      align_up(size_t(c->batch) * c->kv_heads * c->k_len * c->head_dim * 4 * p.kv_parts);
   L.part2 = L.part + dk;
-  L.bwd = L.part + std::max(p.q_parts > 1 ? align_up(dq * p.q_parts) : 0, p.kv_parts > 1 ? 2 * dk : 0);
+  L.bwd = L.part + std::max(p.q_parts > 1 ? align_up(dq * p.q_parts) : 0,
+                            p.kv_parts > 1 ? 2 * dk : 0);
   return L;
 }
 
@@ -262,8 +264,8 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
 int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* dO,
                         const attn_cross_tensor* Q, const attn_cross_tensor* K,
                         const attn_cross_tensor* V, const attn_cross_tensor* O, const float* lse,
-                        const void* rest, const float* bias, const int32_t* k_lens, const int32_t* q_start,
-                        const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
+                        const void* rest, const float* bias, const int32_t* k_lens,
+                        const int32_t* q_start, const attn_cross_tensor* dQ, const attn_cross_tensor* dK,
                         const attn_cross_tensor* dV, float* dbias, void* workspace,
                         size_t workspace_bytes, void* stream) {
   CrossArgs a;

@@ -125,7 +125,8 @@ inline CrossPlan cross_plan(int64_t B, int nh, int kvh, int64_t Sq, int64_t Sk, 
                             int span) {
   CrossPlan p;
   const bool wide = D * es == 512;  // (four 32-row tiles of 512 bytes do not fit LDS)
-  const int64_t qh = B * nh, kh = B * kvh, sq = cross_tiles(int(Sq), 32), sk = cross_tiles(int(Sk), 32);
+  const int64_t qh = B * nh, kh = B * kvh;
+  const int64_t sq = cross_tiles(int(Sq), 32), sk = cross_tiles(int(Sk), 32);
   const int64_t cost = es == 4 ? 1 : 4;
   const int most = wide ? 1 : 2;
   if (!wide && cross_split_pays(4, qh * sq, cross_q_lds(es, D, 4, span), most, sk))
