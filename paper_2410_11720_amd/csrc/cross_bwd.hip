@@ -37,13 +37,14 @@ __device__ __forceinline__ void store4(char* p, floatx4 v) {
 }
 
 // ---- query pass -----------------------------------------------------------
-template <typename T, int D, bool BIAS, int NQ, int KS>
-__global__ __launch_bounds__(64 * NQ * KS, (sizeof(T) * D == 512 ? 1 : 2)) void
+// WV: workgroups a CU that its registers allow; at three nothing is read ahead.
+template <typename T, int D, bool BIAS, int NQ, int KS, int WV>
+__global__ __launch_bounds__(64 * NQ * KS, WV) void
 cross_bwd_q_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
   constexpr int NW = NQ * KS, KT = cross_rows(sizeof(T), KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
-  constexpr bool AHEAD = read_ahead<T, D>();
+  constexpr bool AHEAD = WV < 3 && read_ahead<T, D>();
   __shared__ float row_sum[KS > 1 ? NW * 64 : 1];
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
@@ -594,14 +595,14 @@ cross_bwd_kv_kernel(CrossArgs a) {
   Tile::store_row(a.dv.p + b * a.dv.b + kv * a.dv.h + int64_t(j) * a.dv.t, dv, 1.f, valid, half);
 }
 
-template <typename T, int D, bool BIAS, int NQ, int KS>
+template <typename T, int D, bool BIAS, int NQ, int KS, int WV>
 hipError_t run_q(const CrossArgs& a, hipStream_t s) {
   const size_t lds = cross_q_lds(sizeof(T), D, KS, BIAS ? bias_span_h(a.bias) : 0);
-  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS, NQ, KS>>(CROSS_LDS - 2048);
+  hipError_t e = lds_limit<cross_bwd_q_kernel<T, D, BIAS, NQ, KS, WV>>(CROSS_LDS - 2048);
   if (e != hipSuccess) return e;
   const int64_t heads = int64_t(a.B) * a.nh;
   const int64_t grid = heads * cross_tiles(a.Sq, 32 * NQ) * a.q_parts;
-  cross_bwd_q_kernel<T, D, BIAS, NQ, KS><<<dim3(uint32_t(grid)), 64 * NQ * KS, lds, s>>>(a);
+  cross_bwd_q_kernel<T, D, BIAS, NQ, KS, WV><<<dim3(uint32_t(grid)), 64 * NQ * KS, lds, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || a.q_parts == 1) return e;
   const int64_t n = heads * a.Sq * (D / 4);
   cross_join_q_kernel<T, D><<<dim3(uint32_t((n + 255) / 256)), 256, 0, s>>>(a);
@@ -638,9 +639,14 @@ hipError_t launch_cross_bwd_q(const CrossArgs& a, const CrossPlan& p, int dtype,
     using T = typename decltype(t)::type;
     constexpr int DD = decltype(d)::value;
     constexpr bool BIAS = decltype(bias)::value;
+    constexpr int WV = DD * sizeof(T) == 512 ? 1 : 2;
     if constexpr (DD * sizeof(T) < 512)
-      if (p.q_split == 4) return run_q<T, DD, BIAS, 1, 4>(a, s);
-    return p.q_split == 2 ? run_q<T, DD, BIAS, 2, 2>(a, s) : run_q<T, DD, BIAS, 4, 1>(a, s);
+      if (p.q_split == 4) return run_q<T, DD, BIAS, 1, 4, WV>(a, s);
+    if constexpr (cross_three(sizeof(T), DD))
+      if (p.q_three)
+        return p.q_split == 2 ? run_q<T, DD, BIAS, 2, 2, 3>(a, s)
+                              : run_q<T, DD, BIAS, 4, 1, 3>(a, s);
+    return p.q_split == 2 ? run_q<T, DD, BIAS, 2, 2, WV>(a, s) : run_q<T, DD, BIAS, 4, 1, WV>(a, s);
   });
 }
 

@@ -115,9 +115,17 @@ inline int cross_parts(int64_t wgs, size_t lds, int most, int64_t steps, int64_t
   return n > 1 && steps - (steps + n - 1) / n > cost ? int(n) : 1;
 }
 
+// Whether the query pass has a form with fewer registers, three workgroups to a
+// CU. It takes grids that two a CU do not hold at once (cross attention of 8 x
+// 512 over 1000, 12 heads: both passes 68 -> 64 us; 2 x 4096, 32 heads: 997 ->
+// 979); a grid that two a CU hold is better off with fragments read ahead (16
+// heads x 4096: 258, in three 262 us).
+constexpr bool cross_three(int es, int D) { return es * D == 128; }
+
 // Shapes of the backward passes.
 struct CrossPlan {
   int q_split = 1, q_parts = 1;    // waves, workgroups that share 32 queries
+  bool q_three = false;            // three workgroups of the query pass a CU, not two
   int kv_keys = 4, kv_split = 1;   // 32s of keys of a workgroup, waves that share 32 keys
   int kv_parts = 1;
 };
@@ -131,10 +139,12 @@ inline CrossPlan cross_plan(int64_t B, int nh, int kvh, int64_t Sq, int64_t Sk, 
   const int most = wide ? 1 : 2;
   if (!wide && cross_split_pays(4, qh * sq, cross_q_lds(es, D, 4, span), most, sk))
     p.q_split = 4;
-  else if (cross_split_pays(2, qh * ((sq + 1) / 2), cross_q_lds(es, D, 2, span), most, sk))
+  else if (cross_split_pays(2, qh * ((sq + 1) / 2), cross_q_lds(es, D, 2, span),
+                            cross_three(es, D) ? 3 : most, sk))
     p.q_split = 2;
-  p.q_parts = cross_parts(qh * cross_tiles(int(sq), 4 / p.q_split),
-                          cross_q_lds(es, D, p.q_split, span), most,
+  const int64_t wgs = qh * cross_tiles(int(sq), 4 / p.q_split);
+  p.q_three = cross_three(es, D) && wgs > 256 * most;
+  p.q_parts = cross_parts(wgs, cross_q_lds(es, D, p.q_split, span), most,
                           cross_tiles(int(Sk), cross_rows(es, p.q_split)), cost);
   const int64_t blocks = nh / kvh * sq, two = kh * ((sk + 1) / 2);
   if (cross_v_in_lds(es, D)) {

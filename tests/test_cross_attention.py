@@ -235,6 +235,24 @@ def test_short_form(n):
     _check(cfg, 200 + n, lens, starts)
 
 
+# more workgroups of the query pass than the chip holds two a CU: of 64 and of
+# 128 queries
+_LENS = [130 - 11 * (i % 5) if i % 7 else 0 for i in range(16)]
+MANY = [
+    (C(16, 140, 200, 16, 64), None, None),
+    (C(16, 140, 130, 16, 64, causal=True, buckets=32), _LENS, [n - 140 for n in _LENS]),
+    (C(16, 300, 130, 16, 64), _LENS, None),
+    (C(16, 300, 130, 16, 64, kv_heads=4, causal=True, buckets=32, bidirectional=False), None, None),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", range(len(MANY)))
+def test_many_workgroups(n):
+    cfg, lens, starts = MANY[n]
+    _check(cfg, 300 + n, lens, starts)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d,q_len", [("bf16", 64, 70), ("bf16", 128, 2), ("f32", 64, 70),
                                            ("f32", 128, 1)])
