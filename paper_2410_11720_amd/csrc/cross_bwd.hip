@@ -14,9 +14,9 @@
 // other axis too, over the waves of a workgroup and over workgroups (cross_plan).
 // The price of two passes is a second S and dP (14 d flops a pair against 10 d in
 // one). Both are bound by their matrix and vector instructions, which hardly
-// overlap: 4 x 2048 queries over 1024 keys, 32 heads on 8, head dim 128: 257 and
-// 286 us, 0.80 and 0.96 PFLOP/s of bf16; 8 x 1024 causal, 12 heads, head dim 64,
-// with a bias: 46 and 58 us.
+// overlap: 4 x 2048 queries over 1024 keys, 32 heads on 8, head dim 128: 250 and
+// 271 us, 0.82 and 1.01 PFLOP/s of bf16; 8 x 1024 causal, 12 heads, head dim 64,
+// with a bias: 43 and 59 us.
 #include "cross_tile.hpp"
 
 namespace abft {
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void cross_join_kv_kernel(CrossArgs a, int n) 
 // At head dim 128 the accumulators of both gradients and the keys' and values' own
 // fragments do not fit 256 registers beside the scores (36 spilled: the pass of
 // 4 x 2048 queries over 1024 keys, 32 heads on 8, 720 us). In bf16 the values' are
-// read from LDS, which leaves room for one workgroup a CU, of 8 waves (286 us;
+// read from LDS, which leaves room for one workgroup a CU, of 8 waves (260 us;
 // of 4 waves 345 us). fp32 runs one wave per SIMD.
 template <typename T, int D, bool BIAS, int KW, int QH>
 __global__ __launch_bounds__(64 * KW * QH, (sizeof(T) * D == 512 ? 1 : 2)) void
