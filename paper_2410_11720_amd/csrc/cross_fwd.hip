@@ -496,9 +496,9 @@ hipError_t launch_cross_fwd(const CrossArgs& a, int dtype, int D, hipStream_t s)
     const int most = sizeof(T) * D == 128 ? 3 : 2, span = BIAS ? bias_span_h(a.bias) : 0;
     auto lds = [&](int split) { return cross_q_lds(sizeof(T), D, split, span); };
     if constexpr (D * sizeof(T) < 512)  // (four 32-row tiles of 512 bytes do not fit LDS)
-      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), lds(4), most, blocks))
+      if (cross_split_pays(4, heads * cross_tiles(a.Sq, 32), lds(4), most, blocks, int(sizeof(T))))
         return run_fwd<T, D, BIAS, 1, 4>(a, s);
-    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), lds(2), most, blocks))
+    if (cross_split_pays(2, heads * cross_tiles(a.Sq, 64), lds(2), most, blocks, int(sizeof(T))))
       return run_fwd<T, D, BIAS, 2, 2>(a, s);
     return run_fwd<T, D, BIAS, 4, 1>(a, s);
   });

@@ -100,9 +100,13 @@ constexpr size_t cross_kv_lds(int es, int D, int KW, int QH, int span) {
 // queries and keys: 67 -> 35 us by 4; fp32 374 -> 121 us); one that does loses what
 // the smaller tiles read twice (16 heads x 4096: 345 -> 449 us).
 // wgs: workgroups of the shape; lds: bytes each takes; most: that a CU's
-// registers hold; blocks: 32s along the split axis.
-inline bool cross_split_pays(int split, int64_t wgs, size_t lds, int most, int64_t blocks) {
-  if (lds > CROSS_LDS || blocks < 2 * split) return false;
+// registers hold; blocks: 32s along the split axis. In bf16 each wave needs two of
+// them to make up for the join; in fp32, with matrix cores at a sixteenth of the
+// rate, one will do (2 x 128 over 96, 8 heads of 64: forward and backward 45 -> 37
+// us; in bf16 8 x 64 over 64, 16 heads, takes 17 us, split 19).
+inline bool cross_split_pays(int split, int64_t wgs, size_t lds, int most, int64_t blocks,
+                             int es) {
+  if (lds > CROSS_LDS || blocks < (es == 4 ? split : 2 * split)) return false;
   return wgs <= 256 * std::min<int64_t>(most, int64_t(CROSS_LDS / lds));
 }
 
@@ -137,10 +141,10 @@ inline CrossPlan cross_plan(int64_t B, int nh, int kvh, int64_t Sq, int64_t Sk, 
   const int64_t sq = cross_tiles(int(Sq), 32), sk = cross_tiles(int(Sk), 32);
   const int64_t cost = es == 4 ? 1 : 4;
   const int most = wide ? 1 : 2;
-  if (!wide && cross_split_pays(4, qh * sq, cross_q_lds(es, D, 4, span), most, sk))
+  if (!wide && cross_split_pays(4, qh * sq, cross_q_lds(es, D, 4, span), most, sk, es))
     p.q_split = 4;
   else if (cross_split_pays(2, qh * ((sq + 1) / 2), cross_q_lds(es, D, 2, span),
-                            cross_three(es, D) ? 3 : most, sk))
+                            cross_three(es, D) ? 3 : most, sk, es))
     p.q_split = 2;
   const int64_t wgs = qh * cross_tiles(int(sq), 4 / p.q_split);
   p.q_three = cross_three(es, D) && wgs > 256 * most;
@@ -150,16 +154,17 @@ inline CrossPlan cross_plan(int64_t B, int nh, int kvh, int64_t Sq, int64_t Sk, 
   if (cross_v_in_lds(es, D)) {
     // (8 waves a workgroup, and a CU; the sums of a wide bias leave room for 4)
     p.kv_split = 2;
-    if (cross_split_pays(4, two, cross_kv_lds(es, D, 2, 4, span), 1, blocks)) {
+    if (cross_split_pays(4, two, cross_kv_lds(es, D, 2, 4, span), 1, blocks, es)) {
       p.kv_keys = 2;
       p.kv_split = 4;
     } else if (cross_kv_lds(es, D, 4, 2, span) > CROSS_LDS) {
       p.kv_keys = 2;
     }
-  } else if (!wide && cross_split_pays(4, kh * sk, cross_kv_lds(es, D, 1, 4, span), most, blocks)) {
+  } else if (!wide &&
+             cross_split_pays(4, kh * sk, cross_kv_lds(es, D, 1, 4, span), most, blocks, es)) {
     p.kv_keys = 1;
     p.kv_split = 4;
-  } else if (cross_split_pays(2, two, cross_kv_lds(es, D, 2, 2, span), most, blocks)) {
+  } else if (cross_split_pays(2, two, cross_kv_lds(es, D, 2, 2, span), most, blocks, es)) {
     p.kv_keys = p.kv_split = 2;
   }
   const int64_t heads = nh / kvh;

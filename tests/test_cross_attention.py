@@ -253,6 +253,22 @@ def test_many_workgroups(n):
     _check(cfg, 300 + n, lens, starts)
 
 
+# fp32, few keys (queries): waves that share 32 rows have one block of the other
+# axis each, or a part of one, or none
+FEW = [C(3, q, k, 2, d, dtype="f32", causal=causal, buckets=buckets)
+       for q, k, d, causal, buckets in [(61, 47, 128, False, 0), (33, 33, 128, True, 32),
+                                        (100, 97, 64, False, 32), (97, 128, 64, True, 0),
+                                        (128, 33, 64, False, 0), (40, 200, 128, False, 32)]]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [None, [1, 1000, 0], [32, 31, 33]])
+@pytest.mark.parametrize("n", range(len(FEW)))
+def test_few_blocks(n, lens):
+    cfg = FEW[n]
+    _check(cfg, 400 + n, lens and [min(x, cfg.k_len) for x in lens], None)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d,q_len", [("bf16", 64, 70), ("bf16", 128, 2), ("f32", 64, 70),
                                            ("f32", 128, 1)])
