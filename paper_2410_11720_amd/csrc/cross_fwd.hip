@@ -211,8 +211,9 @@ __global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a)
 #pragma unroll
     for (int k = 1; k < KS; ++k) {
       const float* p = box + (wave + (k - 1) * NQ) * BOX;
-      // (a wave whose scores are all NaN has no maximum and l = NaN, which has to
-      // come through: 0 x NaN is NaN)
+      // (a wave that saw no key adds nothing; one whose scores are all NaN has no
+      // maximum either, but l = NaN)
+      if (!__any(p[64] != 0.f)) continue;
       const float mk = p[0], mn = fmaxf(on.m, mk);
       const float f = mn == NEG_INF ? 1.f : exp2_hw(on.m - mn);
       const float g = mn == NEG_INF ? 0.f : exp2_hw(mk - mn);
