@@ -171,13 +171,17 @@ cross_bwd_q_kernel(CrossArgs a) {
         issue_loads<AHEAD>();
         float ce = c, off = nl;
         if constexpr (BIAS) {
-          const int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
-          if (tb + 31 <= a.bias.lo) {
-            off += tab[0];
-          } else if (tb - 31 >= a.bias.hi) {
-            off += tab[bias_span(a.bias) - 1];
-          } else {
+          int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
+          bool apart = false;
+          // (read here: kept in registers it makes three workgroups a CU spill)
+          if (tb + 31 <= a.bias.lo || tb - 31 >= a.bias.hi) {
+            const float x = BiasSides::read(tab + (tb < a.bias.hi ? 0 : bias_span(a.bias) - 1));
+            apart = side_apart(x);
+            if (apart) off += x;
+          }
+          if (!apart) {
             ce = 1.f;
+            tb = clampi(tb, a.bias.lo - 32, a.bias.hi + 32);  // (where the table has entries)
             const float* p = tab + (tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[8 * (r >> 2) + (r & 3)]);
@@ -348,6 +352,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
   const char* kimg = vimg + KEYS * Tile::ROWB;
   float* tab = reinterpret_cast<float*>(smem + 2 * STAGE + (VLDS + KLDS) * KEYS * Tile::ROWB);
   BiasSums<NW> sums;
+  BiasSides sides;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5;
   const int nbk = a.B * a.kvh;
@@ -449,6 +454,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
         if (t > t0) sums.flush(a.bias, sums_of(now.h - 1), tid, lane, wave);
         bias_spread(tab, a.bias, kv * a.group + now.h, a.nh, tid, 64 * NW);
         __syncthreads();
+        sides.load(tab, a.bias);
         sums.clear(tid);
         __syncthreads();
       }
@@ -491,19 +497,16 @@ cross_bwd_kv_kernel(CrossArgs a) {
       if constexpr (AHEAD) Tile::load_cols(cf, img + IMG, 32 * n, lane);
       issue_loads<AHEAD>();
       float ce = c, off = 0.f;
-      int side = 0, at = 0;  // -1, 1: in a constant side of the bias
+      int side = 0, at = 0;  // -1, 1: in a constant side, its entry taken apart
       if constexpr (BIAS) {
         const int tb = w0 - start - i0 - 32 * n;  // the block spans [tb - 31, tb + 31]
-        if (tb + 31 <= a.bias.lo) {
-          off = tab[0];
-          side = -1;
-        } else if (tb - 31 >= a.bias.hi) {
-          off = tab[bias_span(a.bias) - 1];
-          side = 1;
+        side = sides.of(a.bias, tb - 31, tb + 31);
+        if (side != 0) {
+          off = sides.entry(side);
         } else {
           ce = 1.f;
-          at = tb;
-          const float* p = tab + (tb + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD);
+          at = clampi(tb, a.bias.lo - 32, a.bias.hi + 32);  // (where the table has entries)
+          const float* p = tab + (at + (lane & 31) - 4 * half - a.bias.lo + BIAS_PAD);
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, p[-(8 * (r >> 2) + (r & 3))]);
         }

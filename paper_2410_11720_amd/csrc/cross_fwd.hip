@@ -147,6 +147,7 @@ __global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a)
   typename Tile::RowFrag q;
   Tile::load_row(q, a.q.p + b * a.q.b + h * a.q.h + int64_t(min(i, a.Sq - 1)) * a.q.t, half);
   if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
+  BiasSides sides;
 
   Online<T, D> on;
   on.init();
@@ -155,6 +156,7 @@ __global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a)
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < nt) issue(t + 1);
+    if (BIAS && t == 0) sides.load(tab, a.bias);
     const int k0 = t * KT + 32 * NB * ks;    // the wave's keys of the tile
     if (k0 >= wend) continue;
     const char* img = smem + (t & 1) * 2 * IMG + 32 * NB * ks * Tile::ROWB;
@@ -172,10 +174,8 @@ __global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a)
     if constexpr (BIAS) {
       // t of the corner; the wave's keys span [t0 - 31, t0 + 32 NB - 1]
       const int t0 = k0 - start - w0;
-      if (t0 + 32 * NB - 1 <= a.bias.lo) {
-        off = tab[0];
-      } else if (t0 - 31 >= a.bias.hi) {
-        off = tab[bias_span(a.bias) - 1];
+      if (const int side = sides.of(a.bias, t0 - 31, t0 + 32 * NB - 1)) {
+        off = sides.entry(side);
       } else {
         ce = 1.f;
 #pragma unroll
@@ -289,6 +289,7 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
   Tile::load_row(q, a.q.p + b * a.q.b + h * a.q.h + int64_t(i) * a.q.t, half);
   if (nt > 0) issue(0);
   if (NS > 1 && nt > 1) issue(1);
+  bool lo_apart = true, hi_apart = true;
   if constexpr (BIAS) {
     const int n = a.bias.hi - a.bias.lo + 1;
     for (int x = tid; x < n; x += 256) lut[x] = uint8_t(bias_bucket(a.bias, x + a.bias.lo));
@@ -300,6 +301,8 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
     if (tid < 64)
       side[tid & 31][tid >> 5] = col[32 * lut[tid < 32 ? 0 : n - 1] + (tid & 31)];
     __syncthreads();
+    lo_apart = __all(side_apart(side[lane & 31][0]));
+    hi_apart = __all(side_apart(side[lane & 31][1]));
   }
 
   Online<T, D> on;
@@ -321,9 +324,9 @@ __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
     float ce = c, off = 0.f;
     if constexpr (BIAS) {
       const int lo = a.bias.lo, hi = a.bias.hi;
-      if (k0 + 31 - start - i0 <= lo) {
+      if (lo_apart && k0 + 31 - start - i0 <= lo) {
         off = side[lane & 31][0];
-      } else if (k0 - start - i1 >= hi) {
+      } else if (hi_apart && k0 - start - i1 >= hi) {
         off = side[lane & 31][1];
       } else {
         ce = 1.f;

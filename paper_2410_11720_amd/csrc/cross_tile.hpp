@@ -382,6 +382,41 @@ __device__ __forceinline__ float bias_entry(float x) {
   return x < -1e30f ? NEG_INF : x * LOG2E;
 }
 
+// Whether a constant side's entry may enter the exponent apart from the scores.
+// A score is the fp32 sum of product and entry; next to an entry of -1e9 that sum
+// has no bits of an ordinary product left, kept apart it has all: weights would
+// differ from those of the same sums near the diagonal, and 2^(s - m) could pass
+// 1 without bound. Up to 2^10 the two ways differ by less than 2^-13. (An entry of
+// -INF masks: no sum to form.)
+__device__ __forceinline__ bool side_apart(float entry) {
+  return !(fabsf(entry) > 1024.f) || entry == NEG_INF;
+}
+
+// The entries of a head's constant sides, from its spread table, in scalar registers.
+struct BiasSides {
+  uint32_t lo = 0, hi = 0;
+  uint32_t lo_apart = 0, hi_apart = 0;
+
+  __device__ __forceinline__ static float read(const float* p) {
+    return __uint_as_float(uni(__float_as_uint(*p)));
+  }
+  __device__ __forceinline__ void load(const float* tab, const CrossBias& b) {
+    const float x = read(tab), y = read(tab + bias_span(b) - 1);
+    lo = __float_as_uint(x);
+    hi = __float_as_uint(y);
+    lo_apart = uni(side_apart(x));
+    hi_apart = uni(side_apart(y));
+  }
+  // The constant side that all t of [first, last] lie in, if it is taken apart:
+  // -1, 1; else 0.
+  __device__ __forceinline__ int of(const CrossBias& b, int first, int last) const {
+    return lo_apart && last <= b.lo ? -1 : (hi_apart && first >= b.hi ? 1 : 0);
+  }
+  __device__ __forceinline__ float entry(int side) const {
+    return __uint_as_float(side < 0 ? lo : hi);
+  }
+};
+
 // the spread table of one head: tab[t - lo + BIAS_PAD]
 __device__ __forceinline__ void bias_spread(float* tab, const CrossBias& b, int head, int heads,
                                             int tid, int nthreads) {
@@ -477,7 +512,7 @@ struct BiasSums {
     lo = hi = 0.f;
   }
   // Adds a block (lane: key, registers: queries) whose corner (first key, first
-  // query) has t = tb, inside (lo - 31, hi + 31).
+  // query) has t = tb, inside [lo - 32, hi + 32].
   __device__ __forceinline__ void add(const CrossBias& b, const floatx16& s, int tb, int lane) {
     const float v = diagonal_sums(s, lane);
     if (lane > 0) mine[tb - 32 + lane - b.lo + BIAS_PAD] += v;
