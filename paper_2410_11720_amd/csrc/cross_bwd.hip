@@ -6,6 +6,11 @@
 //   dv_j = sum_i P_ij dO_i,  dtable[t] = sum over pairs of bucket t of dS_ij,
 // with dk_j and dv_j summed over the query heads that share a key head.
 //
+// lse is one fp32 number: beside scores of 1e6 the logarithm of a row's sum has
+// few bits left in it, beside 1e9 none, and the row's P sum to anything up to
+// its number of keys. Where an lse is that large the query pass sums its row's P
+// too, and both passes divide by the sum.
+//
 // Two passes, each of which owns what it sums (no atomics on memory, so
 // results do not depend on the order of workgroups): a workgroup of the query
 // pass owns 32 to 128 queries and runs over the keys (dq; it leaves -lse and -D
@@ -28,6 +33,10 @@ namespace {
 template <typename T, int D>
 constexpr bool read_ahead() { return D * sizeof(T) == 128; }
 
+// |lse| past which a row's P are summed (its rounding is 2^-17 there)
+constexpr float LARGE_LSE = 256.f;
+__device__ __forceinline__ float inverse(float total) { return total == 0.f ? 1.f : 1.f / total; }
+
 template <typename T>
 __device__ __forceinline__ void store4(char* p, floatx4 v) {
   if constexpr (sizeof(T) == 2)
@@ -45,7 +54,7 @@ cross_bwd_q_kernel(CrossArgs a) {
   constexpr int NW = NQ * KS, KT = cross_rows(sizeof(T), KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
   constexpr bool AHEAD = WV < 3 && read_ahead<T, D>();
-  __shared__ float row_sum[KS > 1 ? NW * 64 : 1];
+  __shared__ float row_sum[KS > 1 ? 2 * NW * 64 : 1];
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
 
@@ -106,7 +115,9 @@ cross_bwd_q_kernel(CrossArgs a) {
     }
   }
   if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
-  float sum = 0.f;  // of the row's dS
+  // of the row's dS and, if any lse of the wave's rows is large, of its P
+  float sum = 0.f, total = 0.f;
+  const bool large = __any(nl != NEG_INF && !(fabsf(nl) <= LARGE_LSE));
 
   // rows between the last query and the end of the key pass's tiles: P = 0
   if (part == 0 && q0 + 32 * NQ >= a.Sq)
@@ -114,21 +125,26 @@ cross_bwd_q_kernel(CrossArgs a) {
       const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + x;
       a.nlse[at] = NEG_INF;
       a.ndelta[at] = 0.f;
+      a.norm[at] = 1.f;
     }
   const float nd0 = nd;
-  // a row's sum over its KS waves (all call it together, behind the last use of
+  // a row's sums over its KS waves (all call it together, behind the last use of
   // the sums before)
-  auto join_sum = [&](float x) {
-    x = half_sum(x);
+  auto join_sums = [&] {
+    sum = half_sum(sum);
+    total = half_sum(total);
     if constexpr (KS > 1) {
-      row_sum[wave * 64 + lane] = x;
+      row_sum[wave * 64 + lane] = sum;
+      row_sum[(NW + wave) * 64 + lane] = total;
       __syncthreads();
-      x = 0.f;
+      sum = total = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) x += row_sum[(qw + k * NQ) * 64 + lane];
+      for (int k = 0; k < KS; ++k) {
+        sum += row_sum[(qw + k * NQ) * 64 + lane];
+        total += row_sum[(NW + qw + k * NQ) * 64 + lane];
+      }
       __syncthreads();
     }
-    return x;
   };
 
   // -D in every register of a block: what the products that form dP - D start
@@ -192,9 +208,14 @@ cross_bwd_q_kernel(CrossArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < lim ? s[r] : NEG_INF;
         }
+        for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, off));
+        if (large) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) total += s[r];
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
+          s[r] *= dp[r];
           sum += s[r];
         }
         if (sweep == 0) continue;
@@ -204,17 +225,18 @@ cross_bwd_q_kernel(CrossArgs a) {
         Tile::cols(dq, kc, p, lane);
       }
       if (sweep == 0) {
-        nd -= join_sum(sum);
-        sum = 0.f;
+        join_sums();
+        nd -= large ? sum * inverse(total) : sum;
+        sum = total = 0.f;
         minus_d = nd;
       }
     }
   }
+  join_sums();  // (KS > 1: a barrier, the tiles are no longer read)
   if constexpr (KS > 1) {
     float* box = reinterpret_cast<float*>(smem) + lane;
     constexpr int BOX = 64 * 16 * Tile::ND;
     static_assert(NQ * (KS - 1) * BOX * 4 <= 4 * IMG, "the tiles' space holds the boxes");
-    sum = join_sum(sum);  // (a barrier: the tiles are no longer read)
     if (ks > 0) {
 #pragma unroll
       for (int e = 0; e < 16 * Tile::ND; ++e)
@@ -227,30 +249,38 @@ cross_bwd_q_kernel(CrossArgs a) {
 #pragma unroll
       for (int e = 0; e < 16 * Tile::ND; ++e)
         dq[e / 16][e % 16] += box[(wave + (k - 1) * NQ) * BOX + 64 * e];
-  } else {
-    sum = half_sum(sum);
   }
-  // For the key pass: -lse, and D so that the row's dS sum to zero as they must.
-  // (O was formed from P rounded to bf16, which moves D by 2^-9 of its terms;
-  // a bias gradient, the sum of many dS of either sign, was off by 0.1%.)
-  nd -= sum;
+  // For the key pass: -lse, what P is multiplied by, and D so that the row's dS sum
+  // to zero as they must. (O was formed from P rounded to bf16, which moves D by
+  // 2^-9 of its terms; a bias gradient, the sum of many dS of either sign, was off
+  // by 0.1%.)
   const int64_t row = int64_t(b) * a.nh + h, at = row * a.q_pad + i;
+  float norm = 1.f;
   if (a.q_parts == 1) {
-    Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale, valid,
-                    half);
+    if (large) norm = inverse(total);
+    nd -= sum * norm;
+    Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale * norm,
+                    valid, half);
   } else {
     const int64_t rows = int64_t(a.B) * a.nh;
     Tile::store_sums(a.part_dq + ((part * rows + row) * a.Sq + i) * D, dq, valid, half);
-    if (half == 0) a.part_sum[part * rows * a.q_pad + at] = nd0 - nd;
+    if (half == 0) {
+      // (a part that corrected D has all of the row)
+      const float own = large ? total : (part == 0 ? 1.f : 0.f);
+      a.part_sum[part * rows * a.q_pad + at] = sum + (nd0 - nd) * (large ? total : 1.f);
+      a.part_total[part * rows * a.q_pad + at] = own;
+    }
     nd = nd0;  // (cross_join_q_kernel takes the parts' sums off)
   }
   if (half == 0 && part == 0) {
     a.nlse[at] = nl;
     a.ndelta[at] = nd;
+    a.norm[at] = norm;
   }
 }
 
-// Joins the query pass's parts in their order: dq, and -D less the sums of dS.
+// Joins the query pass's parts in their order: dq, -D less the sums of dS, and
+// what P is multiplied by.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_q_kernel(CrossArgs a) {
   const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x, rows = int64_t(a.B) * a.nh;
@@ -259,14 +289,20 @@ __global__ __launch_bounds__(256) void cross_join_q_kernel(CrossArgs a) {
   if (r >= rows * a.Sq) return;
   const int64_t bh = r / a.Sq, i = r % a.Sq;
   floatx4 v = {};
-  for (int p = 0; p < a.q_parts; ++p)
+  float total = 0.f;
+  for (int p = 0; p < a.q_parts; ++p) {
     v += *reinterpret_cast<const floatx4*>(a.part_dq + (p * rows * a.Sq + r) * D + e);
+    total += a.part_total[(p * rows + bh) * a.q_pad + i];
+  }
+  const float norm = inverse(total);
   const int b = int(bh / a.nh), h = int(bh % a.nh);
-  store4<T>(a.dq.p + b * a.dq.b + h * a.dq.h + i * a.dq.t + e * int(sizeof(T)), v * a.scale);
+  store4<T>(a.dq.p + b * a.dq.b + h * a.dq.h + i * a.dq.t + e * int(sizeof(T)),
+            v * (a.scale * norm));
   if (e == 0) {
     float s = 0.f;
     for (int p = 0; p < a.q_parts; ++p) s += a.part_sum[(p * rows + bh) * a.q_pad + i];
-    a.ndelta[bh * a.q_pad + i] -= s;
+    a.ndelta[bh * a.q_pad + i] -= s * norm;
+    a.norm[bh * a.q_pad + i] = norm;
   }
 }
 
@@ -344,7 +380,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
   constexpr int QT = cross_rows(sizeof(T), QH), NB = QT / 32 / QH, NW = KW * QH, KEYS = 32 * KW;
   constexpr int IMG = QT * Tile::ROWB;
   constexpr int NS = cross_stats(QT);
-  constexpr int STAGE = 2 * IMG + 8 * NS;  // Q, dO, -lse and -D of a tile
+  constexpr int STAGE = 2 * IMG + 12 * NS;  // Q, dO, -lse, -D and norm of a tile
   constexpr bool KLDS = cross_k_in_lds(sizeof(T), D, QH, BIAS);
   constexpr bool VLDS = cross_v_in_lds(sizeof(T), D), AHEAD = read_ahead<T, D>();
   extern __shared__ __align__(1024) char smem[];
@@ -397,12 +433,12 @@ cross_bwd_kv_kernel(CrossArgs a) {
     Tile::template issue<QT, NW>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
                                  a.dout.t, a.Sq - i0, to + IMG, wave, lane);
     const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i0;
-    if (wave < 2) {  // (64 at a time; a 32-row tile uses half of them)
+    if (wave < 3) {  // (64 at a time; a 32-row tile uses half of them)
 #pragma unroll
       for (int x = 0; x < NS; x += 64) {
         const int n = min(64, a.q_pad - i0 - x);  // the end of the rows: the last one again
         if (n > 0)
-          dma4(rsrc_of((wave == 0 ? a.nlse : a.ndelta) + at + x, 256),
+          dma4(rsrc_of((wave == 0 ? a.nlse : (wave == 1 ? a.ndelta : a.norm)) + at + x, 256),
                uni(to + 2 * IMG + wave * 4 * NS + 4 * x), uint32_t(min(lane, n - 1) * 4), 0u);
       }
     }
@@ -466,6 +502,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
     const char* img = smem + (t & 1) * STAGE;
     const float* nls = reinterpret_cast<const float*>(img + 2 * IMG);
     const float* nds = nls + NS;
+    const float* norms = nds + NS;
 #pragma unroll
     for (int m = 0; m < NB; ++m) {
       const int n = qh * NB + m;
@@ -479,6 +516,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
         Tile::rows(s, af, kf);
       }
       if constexpr (!VLDS) Tile::load_rows(af, img + IMG, 32 * n, lane);
+      const bool scaled = __any(norms[32 * n + (lane & 31)] != 1.f);
       // (registers 4 q .. 4 q + 3: rows 8 q + 4 half on)
       const float* nlr = nls + 32 * n + 4 * half;
       const float* ndr = nds + 32 * n + 4 * half;
@@ -522,6 +560,10 @@ cross_bwd_kv_kernel(CrossArgs a) {
         const floatx4 l = *reinterpret_cast<const floatx4*>(nlr + 2 * r);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[r + e] = exp2_hw(fmaf(s[r + e], ce, BIAS ? l[e] + off : l[e]));
+      }
+      if (scaled) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= norms[32 * n + 4 * half + 8 * (r >> 2) + (r & 3)];
       }
       typename Tile::Probs p;
       Tile::pack(p, s);

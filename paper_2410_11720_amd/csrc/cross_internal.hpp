@@ -51,11 +51,13 @@ struct CrossArgs {
   int q_pad = 0;                           // Sq rounded up to the query tile
   float* nlse = nullptr;                   // [B][nh][q_pad]: -lse (-inf: no key)
   float* ndelta = nullptr;                 // [B][nh][q_pad]: -D
+  float* norm = nullptr;                   // [B][nh][q_pad]: 1 / sum of the row's 2^(s - lse)
   float* dbias_part = nullptr;             // [nh][B * key tiles * kv_parts][buckets]
   // the passes' other axis split over workgroups, and the parts' results
   int q_parts = 1, kv_parts = 1;
   float* part_dq = nullptr;                // [q_parts][B][nh][Sq][D]
   float* part_sum = nullptr;               // [q_parts][B][nh][q_pad]
+  float* part_total = nullptr;             // the same
   float* part_dk = nullptr;                // [kv_parts][B][kvh][Sk][D]
   float* part_dv = nullptr;
   float* dbias = nullptr;                  // [buckets][nh]
@@ -87,7 +89,7 @@ constexpr bool cross_k_in_lds(int es, int D, int QH, bool bias) {
   return cross_v_in_lds(es, D) && bias && QH == 2;
 }
 constexpr size_t cross_kv_lds(int es, int D, int KW, int QH, int span) {
-  return 2 * (size_t(2) * cross_rows(es, QH) * D * es + 8 * cross_stats(cross_rows(es, QH))) +
+  return 2 * (size_t(2) * cross_rows(es, QH) * D * es + 12 * cross_stats(cross_rows(es, QH))) +
          (cross_v_in_lds(es, D) ? size_t(32) * KW * D * es : 0) +
          (cross_k_in_lds(es, D, QH, span > 0) ? size_t(32) * KW * D * es : 0) +
          size_t(span ? KW * QH + 1 : 0) * span * 4;
