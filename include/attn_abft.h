@@ -339,8 +339,9 @@ int attn_abft_workspace_tensor(const attn_abft_config* cfg, int32_t which, size_
  *   O_i  = sum_j softmax_j(S_ij) V_j   over j < n, and j <= s + i if causal
  * Each group of heads / kv_heads consecutive query heads shares one key head.
  * A query without keys gets O = 0, and no gradient comes from it. K and V behind a
- * sequence's n keys are not read, whatever they hold; a key that only the causal
- * mask hides must be finite. These calls carry no checksums (the
+ * sequence's n keys, Q and dO of queries in front of its first key (causal, s + i <
+ * 0) reach no result, whatever they hold; what only the causal mask or the bias
+ * hides must be finite. These calls carry no checksums (the
  * counterpart of ABFT_FLAG_UNPROTECTED): encode_checksums and
  * verify_and_correct guard what they read and write while it is stored.
  * Results do not depend on scheduling. Conventions as at the top; nothing

@@ -107,9 +107,9 @@ cross_bwd_q_kernel(CrossArgs a) {
     }
     nd = -half_sum(nd);
     const float lse = a.lse[(int64_t(b) * a.nh + h) * a.Sq + ic];
-    // rows without keys and rows past the last query: P = 0
+    // rows without keys (whatever they hold) and rows past the last query: P = 0
     nl = valid && lse != NEG_INF ? -lse : NEG_INF;
-    if (!valid) {
+    if (nl == NEG_INF) {
       nd = 0.f;
       Tile::zero_row(g);
     }
@@ -403,7 +403,7 @@ cross_bwd_kv_kernel(CrossArgs a) {
   int first = 0;
   if (a.causal) first = max(0, key0 - start) / QT;
   int per = max(0, (a.Sq + QT - 1) / QT - first);
-  if (key0 >= len) per = 0;
+  if (key0 >= len || (a.causal && start + a.Sq <= key0)) per = 0;
   // the workgroup's tiles, over the heads of the group
   const int all = per * a.group;
   const int t0 = int(int64_t(all) * part / a.kv_parts);
@@ -428,10 +428,12 @@ cross_bwd_kv_kernel(CrossArgs a) {
     const int h = kv * a.group + ahead.h, i0 = (first + ahead.i) * QT;
     ahead.step();
     const uint32_t to = lds0 + (t & 1) * STAGE;
+    // queries in front of the first key: not read (0 x NaN would reach every key)
+    const int low = a.causal ? -start - i0 : 0;
     Tile::template issue<QT, NW>(a.q.p + b * a.q.b + h * a.q.h + int64_t(i0) * a.q.t, a.q.t,
-                                 a.Sq - i0, to, wave, lane);
+                                 a.Sq - i0, to, wave, lane, low);
     Tile::template issue<QT, NW>(a.dout.p + b * a.dout.b + h * a.dout.h + int64_t(i0) * a.dout.t,
-                                 a.dout.t, a.Sq - i0, to + IMG, wave, lane);
+                                 a.dout.t, a.Sq - i0, to + IMG, wave, lane, low);
     const int64_t at = (int64_t(b) * a.nh + h) * a.q_pad + i0;
     if (wave < 3) {  // (64 at a time; a 32-row tile uses half of them)
 #pragma unroll

@@ -141,15 +141,15 @@ struct CrossTile {
   // Copies ROWS rows starting at `src` (rows ldb bytes apart) to the image at
   // `lds`, split over NW waves. Rows from `left` on repeat row left - 1, so
   // nothing past a sequence's end is read: what they bring is masked or never
-  // stored. left >= 1.
+  // stored. Likewise rows in front of row `low`. left > low, left >= 1.
   template <int ROWS, int NW>
   __device__ static __forceinline__ void issue(const char* src, uint32_t ldb, int left,
-                                               uint32_t lds, int wave, int lane) {
+                                               uint32_t lds, int wave, int lane, int low = 0) {
     constexpr int PW = ROWS / RPR / NW;  // runs of this wave
     static_assert(PW * RPR * NW == ROWS, "whole runs a wave");
     const u32x4 rs = rsrc_of(src, 0x7fffffffu);
     const int r = lane / CPR, pos = lane % CPR;
-    if (left >= ROWS) {
+    if (left >= ROWS && low <= 0) {
 #pragma unroll
       for (int j = 0; j < PW; ++j) {
         const int i = wave * PW + j;
@@ -162,7 +162,7 @@ struct CrossTile {
       for (int j = 0; j < PW; ++j) {
         const int i = wave * PW + j, row = i * RPR + r;
         const uint32_t vo =
-            uint32_t(min(row, left - 1)) * ldb + uint32_t((pos ^ swz(row)) << 4);
+            uint32_t(clampi(row, low, left - 1)) * ldb + uint32_t((pos ^ swz(row)) << 4);
         dma16(rs, uni(lds + i * 1024), vo, 0u);
       }
     }

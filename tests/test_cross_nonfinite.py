@@ -69,3 +69,38 @@ def test_queries_that_see_nothing_but_nan(dtype, d, k_len):
     assert o[:, :32].isnan().all() and att.lse[:, :, :32].isnan().all()
     dq, _, dv, _ = att.backward(g, q, k, v, o, bias=table, q_start=start)
     assert dq[:, :32].isnan().all() and dv[:, k_len - 32:].isnan().all()
+
+
+# queries in front of the first key; a query pass of one, two, four waves on
+# the queries, its other axis over several workgroups; a key pass likewise
+AHEAD = [C(2, 90, 60, 2, 64, causal=True), C(8, 300, 200, 32, 64, causal=True),
+         C(2, 200, 300, 4, 128, kv_heads=2, causal=True), C(1, 700, 64, 2, 64, causal=True),
+         C(1, 80, 1500, 1, 128, causal=True), C(2, 90, 60, 2, 64, dtype="f32", causal=True),
+         C(1, 300, 90, 2, 128, dtype="f32", causal=True),
+         C(2, 150, 150, 2, 64, causal=True, buckets=32)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", range(len(AHEAD)))
+@pytest.mark.parametrize("ahead", [1, 37, 64])
+@pytest.mark.parametrize("junk", [math.nan, math.inf])
+def test_no_gradient_comes_from_a_query_without_keys(n, ahead, junk):
+    """Whatever Q and dO hold there (padding in front of a sequence)."""
+    cfg = AHEAD[n]
+    print(f"[case] {cfg} {ahead} {junk}", flush=True)
+    q, k, v, g = _inputs(cfg, 80 + n)
+    keys = dict(q_start=torch.full((cfg.batch,), -ahead, dtype=torch.int32, device="cuda"))
+    if cfg.buckets:
+        keys["bias"] = torch.randn((cfg.buckets, cfg.heads), device="cuda")
+    att = abft.CrossAttention(cfg)
+    results = []
+    for fill in (0.0, junk):
+        q[:, :ahead] = fill
+        g[:, :ahead] = fill
+        o = att.forward(q, k, v, **keys)
+        results.append((o, *att.backward(g, q, k, v, o, **keys)))
+    for a, b in zip(*results):
+        assert a is None or torch.equal(a, b)
+    o, dq = results[1][:2]
+    assert (o[:, :ahead] == 0).all() and (dq[:, :ahead] == 0).all()
+    assert (att.lse[:, :, :ahead] == -math.inf).all()
