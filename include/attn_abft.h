@@ -365,7 +365,9 @@ typedef struct {
  * one 1. data (device) and all strides are multiples of 16 bytes, a token
  * stride is at most 16 MiB. Inputs may repeat memory (stride 0), outputs not:
  * sorted, an output's strides each pass the extent of the one before. An output
- * shares memory with no other argument. Strides of dimensions of extent 1 and
+ * (lse, rest, dbias and the workspace among them) shares memory with no other
+ * argument (ABFT_ERR_INVALID; views of one buffer whose rows interleave do not
+ * share memory). Strides of dimensions of extent 1 and
  * tensors without elements are not looked at. */
 typedef struct {
   const void* data;

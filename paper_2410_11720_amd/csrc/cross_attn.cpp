@@ -4,6 +4,7 @@
 #include <cmath>
 
 #include "cross_internal.hpp"
+#include "overlap.hpp"
 
 namespace abft {
 namespace {
@@ -11,6 +12,7 @@ namespace {
 constexpr size_t ALIGN = 256;
 constexpr int MAX_LEN = 1 << 29;             // positions and their differences fit 32 bits
 constexpr int64_t MAX_TOKEN_BYTES = 1 << 24; // a tile's rows fit the copies' 32-bit offsets
+constexpr int64_t MAX_EXTENT = int64_t(1) << 56;  // bytes between a dimension's ends
 
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 int es_of(const attn_cross_config* c) { return c->dtype == ABFT_FP32 ? 4 : 2; }
@@ -150,7 +152,7 @@ int take(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh, 
   if (!t->data || reinterpret_cast<uintptr_t>(t->data) % 16) return ABFT_ERR_INVALID;
   for (int k = 0; k < 3; ++k) {
     if (ext[k] == 1) continue;                  // the stride is not used
-    if (st[k] < 0 || (st[k] * es) % 16) return ABFT_ERR_INVALID;
+    if (st[k] < 0 || st[k] > MAX_EXTENT / es / ext[k] || (st[k] * es) % 16) return ABFT_ERR_INVALID;
   }
   if (out) {  // no element is written twice: from the smallest stride up, each passes the last
     int order[3] = {0, 1, 2};
@@ -168,6 +170,26 @@ int take(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh, 
   r->t = n > 1 ? uint32_t(st[1] * es) : 0;
   r->h = nh > 1 ? st[2] * es : 0;
   return ABFT_OK;
+}
+
+// The memory of an operand that `take` accepted.
+Area area(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh) {
+  const int es = es_of(c);
+  if (c->batch == 0 || n == 0) return Area{};
+  Area a = Area::flat(t->data, size_t(c->head_dim) * es);
+  a.dim(0, t->batch_stride * es, c->batch);
+  a.dim(1, t->token_stride * es, n);
+  a.dim(2, t->head_stride * es, nh);
+  return a;
+}
+
+// Whether one of the first n_out areas, which are written, shares memory with
+// another area.
+bool written_overlap(const Area* a, int n_out, int n) {
+  for (int i = 0; i < n_out; ++i)
+    for (int k = i + 1; k < n; ++k)
+      if (overlap(a[i], a[k])) return true;
+  return false;
 }
 
 void common(const attn_cross_config* c, const float* bias, const int32_t* k_lens,
@@ -247,6 +269,18 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
     return ABFT_ERR_INVALID;
   if (workspace_bytes < L.fwd) return ABFT_ERR_WORKSPACE;
   if (cfg->batch == 0 || cfg->q_len == 0) return ABFT_OK;
+  const size_t rows = size_t(cfg->batch) * cfg->heads * cfg->q_len;
+  const Area mem[] = {area(cfg, O, cfg->q_len, cfg->heads),
+                      Area::flat(lse, rows * 4),
+                      Area::flat(cfg->dtype == ABFT_BF16 ? rest : nullptr, rows * cfg->head_dim * 2),
+                      Area::flat(workspace, L.fwd),
+                      area(cfg, Q, cfg->q_len, cfg->heads),
+                      area(cfg, K, cfg->k_len, cfg->kv_heads),
+                      area(cfg, V, cfg->k_len, cfg->kv_heads),
+                      Area::flat(bias, size_t(cfg->buckets) * cfg->heads * 4),
+                      Area::flat(k_lens, size_t(cfg->batch) * 4),
+                      Area::flat(q_start, size_t(cfg->batch) * 4)};
+  if (written_overlap(mem, 4, 10)) return ABFT_ERR_INVALID;
   TRY(check_device());
   common(cfg, bias, k_lens, q_start, &a);
   a.lse = lse;
@@ -290,6 +324,24 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
   if (reinterpret_cast<uintptr_t>(workspace) % 16 || reinterpret_cast<uintptr_t>(rest) % 16)
     return ABFT_ERR_INVALID;
   if (workspace_bytes < L.bwd) return ABFT_ERR_WORKSPACE;
+  const size_t rows = size_t(cfg->batch) * cfg->heads * cfg->q_len;
+  const size_t table = size_t(cfg->buckets) * cfg->heads * 4;
+  const Area mem[] = {area(cfg, dQ, cfg->q_len, cfg->heads),
+                      area(cfg, dK, cfg->k_len, cfg->kv_heads),
+                      area(cfg, dV, cfg->k_len, cfg->kv_heads),
+                      Area::flat(dbias, table),
+                      Area::flat(workspace, L.bwd),
+                      area(cfg, dO, cfg->q_len, cfg->heads),
+                      area(cfg, Q, cfg->q_len, cfg->heads),
+                      area(cfg, K, cfg->k_len, cfg->kv_heads),
+                      area(cfg, V, cfg->k_len, cfg->kv_heads),
+                      area(cfg, O, cfg->q_len, cfg->heads),
+                      Area::flat(lse, rows * 4),
+                      Area::flat(cfg->dtype == ABFT_BF16 ? rest : nullptr, rows * cfg->head_dim * 2),
+                      Area::flat(bias, table),
+                      Area::flat(k_lens, size_t(cfg->batch) * 4),
+                      Area::flat(q_start, size_t(cfg->batch) * 4)};
+  if (written_overlap(mem, 5, 15)) return ABFT_ERR_INVALID;
   TRY(check_device());
   common(cfg, bias, k_lens, q_start, &a);
   a.lse = const_cast<float*>(lse);
