@@ -497,12 +497,29 @@ def _call(fn, device, *args):
         return fn(*args, _raw_stream(index))
 
 
+class CrossSaved:
+    """What a forward leaves for its backward: the row statistics `lse`, and
+    `rest`, what rounding took off O (None in fp32)."""
+
+    def __init__(self, cfg: CrossConfig, device):
+        rows = (cfg.batch, cfg.heads, cfg.q_len)
+        self.lse = torch.empty(rows, dtype=torch.float32, device=device)
+        self.rest = None
+        if cfg.dtype != "f32":
+            self.rest = torch.empty((*rows, cfg.head_dim), dtype=torch.bfloat16, device=device)
+        self._of = None              # where the O that they belong to was written
+
+
 class CrossAttention:
     """Attention of q_len queries over k_len keys a sequence: owns the
-    workspace of one shape and what the forward leaves for the backward (the row
-    statistics `lse`, and `rest`, what rounding took off O), as
-    ProtectedAttention does for its layer; with training=False neither is
-    kept. Calls run on the current stream of the tensors' device.
+    workspace of one shape and one record of what a forward leaves for its
+    backward (`lse`, `rest`), as ProtectedAttention does for its layer; with
+    training=False it has no record. A forward replaces the record: backward
+    raises if its O is not the last forward's. Where other forwards come in
+    between (layers that share the object, micro-batches), or O has moved since,
+    pass a record of `new_saved` to both calls as `saved`; which O belongs to it
+    is then the caller's to know. Calls run on the current stream of the tensors'
+    device.
 
     Q, O, dO, dQ [batch, q_len, heads, head_dim]; K, V, dK, dV [batch, k_len,
     kv_heads, head_dim]; any strides with whole rows at multiples of 16 bytes
@@ -516,16 +533,30 @@ class CrossAttention:
         self._c = cfg.to_c()
         self.workspace = torch.empty(attn_cross_workspace_bytes(cfg), dtype=torch.uint8,
                                      device=self.device)
-        self.lse = self.rest = None
-        rows = (cfg.batch, cfg.heads, cfg.q_len)
-        if training:
-            self.lse = torch.empty(rows, dtype=torch.float32, device=self.device)
-        if training and cfg.dtype != "f32":
-            self.rest = torch.empty((*rows, cfg.head_dim), dtype=torch.bfloat16,
-                                    device=self.device)
+        self._saved = self.new_saved() if training else None
         kvh = cfg.kv_heads or cfg.heads
         self._q_shape = (cfg.batch, cfg.q_len, cfg.heads, cfg.head_dim)
         self._k_shape = (cfg.batch, cfg.k_len, kvh, cfg.head_dim)
+
+    @property
+    def lse(self):
+        return self._saved and self._saved.lse
+
+    @property
+    def rest(self):
+        return self._saved and self._saved.rest
+
+    def new_saved(self):
+        """Another record for a forward and its backward."""
+        return CrossSaved(self.cfg, self.device)
+
+    def _record(self, saved):
+        c = self.cfg
+        if (saved.lse.shape != (c.batch, c.heads, c.q_len) or saved.lse.device != self.device
+                or (saved.rest is None) != (c.dtype == "f32")
+                or saved.rest is not None and saved.rest.shape[3] != c.head_dim):
+            raise AbftError("saved: made for another shape, type or device")
+        return saved
 
     def _tensors(self, names, tensors, shapes):
         """The tensors' attn_cross_tensor records, one after the other; returns
@@ -556,22 +587,33 @@ class CrossAttention:
                 self._vector(k_lens, "k_lens", (c.batch,), torch.int32),
                 self._vector(q_start, "q_start", (c.batch,), torch.int32))
 
-    def forward(self, Q, K, V, bias=None, k_lens=None, q_start=None, O=None):
+    def forward(self, Q, K, V, bias=None, k_lens=None, q_start=None, O=None, saved=None):
         if O is None:
             O = torch.empty_like(Q)
         qs, ks = self._q_shape, self._k_shape
         held, (q, k, v, o) = self._tensors("QKVO", (Q, K, V, O), (qs, ks, ks, qs))
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
+        saved = self._saved if saved is None else self._record(saved)
+        lse = rest = None
+        if saved is not None:
+            lse, rest, saved._of = _data(saved.lse), _data(saved.rest), None
         _check(_call(_lib.attn_cross_forward, self.device, self._c, q, k, v, bias, k_lens, q_start,
-                     o, _data(self.lse), _data(self.rest), self.workspace.data_ptr(),
-                     self.workspace.numel()), "attn_cross_forward")
+                     o, lse, rest, self.workspace.data_ptr(), self.workspace.numel()),
+               "attn_cross_forward")
+        if saved is not None:
+            saved._of = O.data_ptr()
         return O
 
     def backward(self, dO, Q, K, V, O, bias=None, k_lens=None, q_start=None, dQ=None, dK=None,
-                 dV=None, dbias=None):
+                 dV=None, dbias=None, saved=None):
         c = self.cfg
-        if self.lse is None:
+        own = saved is None
+        saved = self._saved if own else self._record(saved)
+        if saved is None:
             raise AbftError("backward: made with training=False")
+        if saved._of is None or own and saved._of != O.data_ptr():
+            raise AbftError("backward: O is not what the last forward left" if saved._of is not None
+                            else "backward: no forward has left its statistics")
         dQ = torch.empty_like(Q) if dQ is None else dQ
         dK = torch.empty_like(K) if dK is None else dK
         dV = torch.empty_like(V) if dV is None else dV
@@ -584,7 +626,7 @@ class CrossAttention:
         bias, k_lens, q_start = self._keys(bias, k_lens, q_start)
         db = self._vector(dbias, "dbias", (c.buckets, c.heads), torch.float32)
         _check(_call(_lib.attn_cross_backward, self.device, self._c, do, q, k, v, o,
-                     _data(self.lse), _data(self.rest), bias, k_lens, q_start, dq, dk, dv, db,
+                     _data(saved.lse), _data(saved.rest), bias, k_lens, q_start, dq, dk, dv, db,
                      self.workspace.data_ptr(), self.workspace.numel()), "attn_cross_backward")
         return dQ, dK, dV, dbias
 
