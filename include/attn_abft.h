@@ -425,7 +425,9 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
  * training step, where gradients that no check has seen show up.
  *   norm = sqrt(sum of all squares), coef = min(1, max_norm / norm),
  *   out = coef * gradient
- * Squares and sums are formed in 64 bits. Where an element is INF or NaN, so is
+ * Squares and sums are formed in 64 bits; norm and coef are reported in fp32 (norm
+ * INF past its range, coef 0 below it), the gradients are scaled by the factor
+ * itself. Where an element is INF or NaN, so is
  * the norm; the gradients are then left as they are (coef = 1) and nonfinite
  * is the caller's cue to skip the step or to fall back to checkpoint/restore.
  * ------------------------------------------------------------------------- */

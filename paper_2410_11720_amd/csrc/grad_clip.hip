@@ -126,8 +126,9 @@ __global__ __launch_bounds__(NT) void grad_sum_kernel(GradList L, GradPartial* p
 }
 
 // The statistics of all partial sums, the same in every workgroup.
+// `ratio`: coef before its rounding to fp32.
 __device__ __forceinline__ abft_grad_stats stats_of(const GradPartial* part, int n, double max_norm,
-                                                    double* sh) {
+                                                    double* sh, double* ratio) {
   double s = 0.0, bad = 0.0;
   for (int i = threadIdx.x; i < n; i += NT) {
     s += part[i].sum;
@@ -138,7 +139,8 @@ __device__ __forceinline__ abft_grad_stats stats_of(const GradPartial* part, int
   const double norm = sqrt(s);
   abft_grad_stats r;
   r.norm = float(norm);
-  r.coef = bad == 0.0 && norm > max_norm ? float(max_norm / norm) : 1.f;
+  *ratio = bad == 0.0 && norm > max_norm ? max_norm / norm : 1.0;
+  r.coef = float(*ratio);
   r.nonfinite = int64_t(bad);
   return r;
 }
@@ -146,25 +148,39 @@ __device__ __forceinline__ abft_grad_stats stats_of(const GradPartial* part, int
 __global__ __launch_bounds__(NT) void grad_stats_kernel(const GradPartial* part, int n,
                                                         abft_grad_stats* stats) {
   __shared__ double sh[4];
-  const abft_grad_stats r = stats_of(part, n, double(__builtin_inff()), sh);
+  double ratio;
+  const abft_grad_stats r = stats_of(part, n, double(__builtin_inff()), sh, &ratio);
   if (threadIdx.x == 0) *stats = r;
 }
 
-template <typename T>
-__device__ __forceinline__ u32x4 scaled(u32x4 x, float f) {
+// The factor max_norm / norm as f * 2^e: below 2^-100 fp32 would hold fewer of its
+// bits (none below 2^-149), while its product with a gradient of 1e38 is an
+// ordinary number.
+struct Factor {
+  float f;
+  int e;
+  __device__ __forceinline__ float operator()(float x) const { return ldexpf(x * f, e); }
+};
+struct Plain {
+  float f;
+  __device__ __forceinline__ float operator()(float x) const { return x * f; }
+};
+
+template <typename T, typename F>
+__device__ __forceinline__ u32x4 scaled(u32x4 x, F f) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if constexpr (sizeof(T) == 2)
-      x[e] = uint32_t(f2bf(__uint_as_float(x[e] << 16) * f)) |
-             (uint32_t(f2bf(__uint_as_float(x[e] & 0xffff0000u) * f)) << 16);
+      x[e] = uint32_t(f2bf(f(__uint_as_float(x[e] << 16)))) |
+             (uint32_t(f2bf(f(__uint_as_float(x[e] & 0xffff0000u)))) << 16);
     else
-      x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+      x[e] = __float_as_uint(f(__uint_as_float(x[e])));
   }
   return x;
 }
 
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const T* g, T* o, int n, float f) {
+template <typename T, typename F>
+__device__ __forceinline__ void scale_chunk(const T* g, T* o, int n, F f) {
   constexpr int V = 16 / int(sizeof(T));
   int at = 0;
   if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(o)) % 16 == 0) {
@@ -185,7 +201,7 @@ __device__ __forceinline__ void scale_chunk(const T* g, T* o, int n, float f) {
     at = nv * V;
   }
   for (int i = at + threadIdx.x; i < n; i += NT)
-    o[i] = Storage<T>::store(Storage<T>::load(g[i]) * f);
+    o[i] = Storage<T>::store(f(Storage<T>::load(g[i])));
 }
 
 // Chunks are taken from the last on: the end of what the sums read is still in
@@ -196,8 +212,14 @@ __global__ __launch_bounds__(NT) void grad_scale_kernel(GradList L, const GradPa
                                                         int n_part, double max_norm,
                                                         abft_grad_stats* stats) {
   __shared__ double sh[4];
-  const abft_grad_stats r = stats_of(part, n_part, max_norm, sh);
+  double ratio;
+  const abft_grad_stats r = stats_of(part, n_part, max_norm, sh, &ratio);
   if (stats && blockIdx.x == 0 && threadIdx.x == 0) *stats = r;
+  Factor small = {r.coef, 0};
+  if (ratio > 0.0 && ratio < 0x1p-100) {
+    small.e = ilogb(ratio) + 1;  // (f < 1: no overflow in front of the shift)
+    small.f = float(ldexp(ratio, -small.e));
+  }
   const int chunks = L.first[L.count];
   for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
     const int c = chunks - 1 - k;
@@ -205,12 +227,18 @@ __global__ __launch_bounds__(NT) void grad_scale_kernel(GradList L, const GradPa
     if (r.coef == 1.f && L.out[t] == L.g[t]) continue;
     const int64_t at = int64_t(c - L.first[t]) * GRAD_CHUNK;
     const int n = int(min(int64_t(GRAD_CHUNK), L.n[t] - at));
-    if (L.bf16[t])
-      scale_chunk(static_cast<const bf16_t*>(L.g[t]) + at, static_cast<bf16_t*>(L.out[t]) + at, n,
-                  r.coef);
+    auto by_type = [&](auto f) {
+      if (L.bf16[t])
+        scale_chunk(static_cast<const bf16_t*>(L.g[t]) + at, static_cast<bf16_t*>(L.out[t]) + at,
+                    n, f);
+      else
+        scale_chunk(static_cast<const float*>(L.g[t]) + at, static_cast<float*>(L.out[t]) + at, n,
+                    f);
+    };
+    if (small.e == 0)
+      by_type(Plain{r.coef});
     else
-      scale_chunk(static_cast<const float*>(L.g[t]) + at, static_cast<float*>(L.out[t]) + at, n,
-                  r.coef);
+      by_type(small);
   }
 }
 
