@@ -172,6 +172,10 @@ int take(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh, 
   return ABFT_OK;
 }
 
+// Whether a launch is in HIP's range (fewer than 2^32 threads). Only whole grids
+// come near it; what splits an axis fills the chip at most.
+bool launchable(int64_t wgs, int threads) { return wgs * threads < (int64_t(1) << 32); }
+
 // The memory of an operand that `take` accepted.
 Area area(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh) {
   const int es = es_of(c);
@@ -281,12 +285,17 @@ int attn_cross_forward(const attn_cross_config* cfg, const attn_cross_tensor* Q,
                       Area::flat(k_lens, size_t(cfg->batch) * 4),
                       Area::flat(q_start, size_t(cfg->batch) * 4)};
   if (written_overlap(mem, 4, 10)) return ABFT_ERR_INVALID;
+  const bool is_short = short_form(cfg, &a.splits);
+  const int64_t shared = int64_t(cfg->q_len) * (cfg->heads / cfg->kv_heads);
+  if (!launchable(is_short ? int64_t(cfg->batch) * cfg->kv_heads * ((shared + 31) / 32) * a.splits
+                           : int64_t(cfg->batch) * cfg->heads * cross_tiles(cfg->q_len, 128), 256))
+    return ABFT_ERR_UNSUPPORTED;
   TRY(check_device());
   common(cfg, bias, k_lens, q_start, &a);
   a.lse = lse;
   a.rest = static_cast<char*>(rest);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (short_form(cfg, &a.splits)) {
+  if (is_short) {
     char* ws = static_cast<char*>(workspace);
     a.part_o = reinterpret_cast<float*>(ws + L.part_o);
     a.part_ml = reinterpret_cast<float*>(ws + L.part_ml);
@@ -342,6 +351,11 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
                       Area::flat(k_lens, size_t(cfg->batch) * 4),
                       Area::flat(q_start, size_t(cfg->batch) * 4)};
   if (written_overlap(mem, 5, 15)) return ABFT_ERR_INVALID;
+  if (!launchable(int64_t(cfg->batch) * cfg->heads * cross_tiles(cfg->q_len, 128), 256) ||
+      !launchable(int64_t(cfg->batch) * cfg->kv_heads * cross_tiles(cfg->k_len, 32 * plan.kv_keys) *
+                      plan.kv_parts, 64 * plan.kv_keys * plan.kv_split) ||
+      !launchable(cfg->buckets ? cfg->heads : 0, 256))
+    return ABFT_ERR_UNSUPPORTED;
   TRY(check_device());
   common(cfg, bias, k_lens, q_start, &a);
   a.lse = const_cast<float*>(lse);
