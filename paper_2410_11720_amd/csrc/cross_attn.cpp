@@ -106,7 +106,7 @@ bool short_form(const attn_cross_config* c, int* splits) {
 struct Space {
   size_t part_o = 0, part_ml = 0;        // forward, short form
   size_t nlse = 0, ndelta = 0, norm = 0, dbias = 0;  // backward
-  size_t sum = 0, total = 0, part = 0, part2 = 0;    // its parts (one pass's at a time)
+  size_t sum = 0, part = 0, part2 = 0;               // its parts (one pass's at a time)
   size_t fwd = 0, bwd = 0;
 };
 
@@ -130,8 +130,7 @@ Space make_space(const attn_cross_config* c, const CrossPlan& p) {
   L.dbias = 3 * L.ndelta;
   L.sum = L.dbias + align_up(size_t(c->batch) * c->heads * cross_tiles(c->k_len, 32 * p.kv_keys) *
                              p.kv_parts * c->buckets * 4);
-  L.total = L.sum + (p.q_parts > 1 ? align_up(rows * 4 * p.q_parts) : 0);
-  L.part = L.total + (L.total - L.sum);
+  L.part = L.sum + (p.q_parts > 1 ? align_up(rows * 4 * p.q_parts) : 0);
   const size_t dq = size_t(c->batch) * c->heads * c->q_len * c->head_dim * 4;
   const size_t dk =
       align_up(size_t(c->batch) * c->kv_heads * c->k_len * c->head_dim * 4 * p.kv_parts);
@@ -370,7 +369,6 @@ int attn_cross_backward(const attn_cross_config* cfg, const attn_cross_tensor* d
   a.q_parts = plan.q_parts;
   a.kv_parts = plan.kv_parts;
   a.part_sum = reinterpret_cast<float*>(ws + L.sum);
-  a.part_total = reinterpret_cast<float*>(ws + L.total);
   a.part_dq = a.part_dk = reinterpret_cast<float*>(ws + L.part);
   a.part_dv = reinterpret_cast<float*>(ws + L.part2);
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -8,8 +8,8 @@
 //
 // lse is one fp32 number: beside scores of 1e6 the logarithm of a row's sum has
 // few bits left in it, beside 1e9 none, and the row's P sum to anything up to
-// its number of keys. Where an lse is that large the query pass sums its row's P
-// too, and both passes divide by the sum.
+// its number of keys. Where an lse is that large the query pass first sums its
+// row's P, and both passes divide by the sum.
 //
 // Two passes, each of which owns what it sums (no atomics on memory, so
 // results do not depend on the order of workgroups): a workgroup of the query
@@ -37,6 +37,55 @@ constexpr bool read_ahead() { return D * sizeof(T) == 128; }
 constexpr float LARGE_LSE = 256.f;
 __device__ __forceinline__ float inverse(float total) { return total == 0.f ? 1.f : 1.f / total; }
 
+// Sum of 2^(s - lse) over the lane's row i, for the 32 rows of a wave from w0 on:
+// keys straight from memory, an entry of the bias from its bucket. Slow, and
+// rare: the passes' own loops do without.
+template <typename T, int D, bool BIAS>
+__device__ __forceinline__ float row_total(const CrossArgs& a, const typename CrossTile<T, D>::RowFrag& q,
+                                        float nl, int b, int h, int w0, int end, int lane) {
+  using Tile = CrossTile<T, D>;
+  const int half = lane >> 5, i = w0 + (lane & 31);
+  const int len = seq_len(a, b), start = seq_start(a, b);
+  const int limit = a.causal ? min(len, start + i + 1) : len;
+  const char* kp = a.k.p + b * a.k.b + (h / a.group) * a.k.h;
+  const float c = a.scale * LOG2E;
+  auto entry = [&](int bucket) {
+    return bias_entry(a.bias.table[int64_t(bucket) * a.nh + h]);
+  };
+  float total = 0.f;
+  for (int k0 = 0; k0 < end; k0 += 32) {
+    typename Tile::RowFrag kf;
+    Tile::load_row(kf, kp + int64_t(min(k0 + (lane & 31), len - 1)) * a.k.t, half);
+    floatx16 s = floatx16{};
+    Tile::rows(s, kf, q);
+    float ce = c, off = nl;
+    if constexpr (BIAS) {
+      const int tb = k0 - start - w0;
+      float x = 0.f;
+      bool apart = false;
+      if (tb + 31 <= a.bias.lo || tb - 31 >= a.bias.hi) {
+        x = entry(bias_bucket(a.bias, tb));
+        apart = side_apart(x);
+      }
+      if (apart) {
+        off += x;
+      } else {
+        ce = 1.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[r] = fmaf(s[r], c, entry(bias_bucket(a.bias, k0 + 8 * (r >> 2) + 4 * half + (r & 3) -
+                                                             start - i)));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const bool seen = k0 + 8 * (r >> 2) + 4 * half + (r & 3) < limit;
+      total += seen ? exp2_hw(fmaf(s[r], ce, off)) : 0.f;
+    }
+  }
+  return half_sum(total);
+}
+
 template <typename T>
 __device__ __forceinline__ void store4(char* p, floatx4 v) {
   if constexpr (sizeof(T) == 2)
@@ -54,7 +103,7 @@ cross_bwd_q_kernel(CrossArgs a) {
   constexpr int NW = NQ * KS, KT = cross_rows(sizeof(T), KS), NB = KT / 32 / KS;
   constexpr int IMG = KT * Tile::ROWB;
   constexpr bool AHEAD = WV < 3 && read_ahead<T, D>();
-  __shared__ float row_sum[KS > 1 ? 2 * NW * 64 : 1];
+  __shared__ float row_sum[KS > 1 ? NW * 64 : 1];
   extern __shared__ __align__(1024) char smem[];
   float* tab = reinterpret_cast<float*>(smem + 4 * IMG);
 
@@ -115,9 +164,10 @@ cross_bwd_q_kernel(CrossArgs a) {
     }
   }
   if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
-  // of the row's dS and, if any lse of the wave's rows is large, of its P
-  float sum = 0.f, total = 0.f;
-  const bool large = __any(nl != NEG_INF && !(fabsf(nl) <= LARGE_LSE));
+  float sum = 0.f;   // of the row's dS
+  float norm = 1.f;  // what its P (and with them dS) are to be multiplied by
+  if (__any(nl != NEG_INF && !(fabsf(nl) <= LARGE_LSE)))
+    norm = inverse(row_total<T, D, BIAS>(a, q, nl, b, h, w0, wend, lane));
 
   // rows between the last query and the end of the key pass's tiles: P = 0
   if (part == 0 && q0 + 32 * NQ >= a.Sq)
@@ -128,23 +178,19 @@ cross_bwd_q_kernel(CrossArgs a) {
       a.norm[at] = 1.f;
     }
   const float nd0 = nd;
-  // a row's sums over its KS waves (all call it together, behind the last use of
+  // a row's sum over its KS waves (all call it together, behind the last use of
   // the sums before)
-  auto join_sums = [&] {
-    sum = half_sum(sum);
-    total = half_sum(total);
+  auto join_sum = [&](float x) {
+    x = half_sum(x);
     if constexpr (KS > 1) {
-      row_sum[wave * 64 + lane] = sum;
-      row_sum[(NW + wave) * 64 + lane] = total;
+      row_sum[wave * 64 + lane] = x;
       __syncthreads();
-      sum = total = 0.f;
+      x = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        sum += row_sum[(qw + k * NQ) * 64 + lane];
-        total += row_sum[(NW + qw + k * NQ) * 64 + lane];
-      }
+      for (int k = 0; k < KS; ++k) x += row_sum[(qw + k * NQ) * 64 + lane];
       __syncthreads();
     }
+    return x;
   };
 
   // -D in every register of a block: what the products that form dP - D start
@@ -208,14 +254,8 @@ cross_bwd_q_kernel(CrossArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < lim ? s[r] : NEG_INF;
         }
-        for (int r = 0; r < 16; ++r) s[r] = exp2_hw(fmaf(s[r], ce, off));
-        if (large) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) total += s[r];
-        }
-#pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] *= dp[r];
+          s[r] = exp2_hw(fmaf(s[r], ce, off)) * dp[r];
           sum += s[r];
         }
         if (sweep == 0) continue;
@@ -225,18 +265,17 @@ cross_bwd_q_kernel(CrossArgs a) {
         Tile::cols(dq, kc, p, lane);
       }
       if (sweep == 0) {
-        join_sums();
-        nd -= large ? sum * inverse(total) : sum;
-        sum = total = 0.f;
+        nd -= join_sum(sum) * norm;
+        sum = 0.f;
         minus_d = nd;
       }
     }
   }
-  join_sums();  // (KS > 1: a barrier, the tiles are no longer read)
   if constexpr (KS > 1) {
     float* box = reinterpret_cast<float*>(smem) + lane;
     constexpr int BOX = 64 * 16 * Tile::ND;
     static_assert(NQ * (KS - 1) * BOX * 4 <= 4 * IMG, "the tiles' space holds the boxes");
+    sum = join_sum(sum);  // (a barrier: the tiles are no longer read)
     if (ks > 0) {
 #pragma unroll
       for (int e = 0; e < 16 * Tile::ND; ++e)
@@ -249,27 +288,22 @@ cross_bwd_q_kernel(CrossArgs a) {
 #pragma unroll
       for (int e = 0; e < 16 * Tile::ND; ++e)
         dq[e / 16][e % 16] += box[(wave + (k - 1) * NQ) * BOX + 64 * e];
+  } else {
+    sum = half_sum(sum);
   }
   // For the key pass: -lse, what P is multiplied by, and D so that the row's dS sum
   // to zero as they must. (O was formed from P rounded to bf16, which moves D by
   // 2^-9 of its terms; a bias gradient, the sum of many dS of either sign, was off
   // by 0.1%.)
   const int64_t row = int64_t(b) * a.nh + h, at = row * a.q_pad + i;
-  float norm = 1.f;
+  nd -= sum * norm;
   if (a.q_parts == 1) {
-    if (large) norm = inverse(total);
-    nd -= sum * norm;
     Tile::store_row(a.dq.p + b * a.dq.b + h * a.dq.h + int64_t(i) * a.dq.t, dq, a.scale * norm,
                     valid, half);
   } else {
     const int64_t rows = int64_t(a.B) * a.nh;
     Tile::store_sums(a.part_dq + ((part * rows + row) * a.Sq + i) * D, dq, valid, half);
-    if (half == 0) {
-      // (a part that corrected D has all of the row)
-      const float own = large ? total : (part == 0 ? 1.f : 0.f);
-      a.part_sum[part * rows * a.q_pad + at] = sum + (nd0 - nd) * (large ? total : 1.f);
-      a.part_total[part * rows * a.q_pad + at] = own;
-    }
+    if (half == 0) a.part_sum[part * rows * a.q_pad + at] = nd0 - nd;
     nd = nd0;  // (cross_join_q_kernel takes the parts' sums off)
   }
   if (half == 0 && part == 0) {
@@ -279,8 +313,7 @@ cross_bwd_q_kernel(CrossArgs a) {
   }
 }
 
-// Joins the query pass's parts in their order: dq, -D less the sums of dS, and
-// what P is multiplied by.
+// Joins the query pass's parts in their order: dq, and -D less the sums of dS.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_q_kernel(CrossArgs a) {
   const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x, rows = int64_t(a.B) * a.nh;
@@ -289,20 +322,15 @@ __global__ __launch_bounds__(256) void cross_join_q_kernel(CrossArgs a) {
   if (r >= rows * a.Sq) return;
   const int64_t bh = r / a.Sq, i = r % a.Sq;
   floatx4 v = {};
-  float total = 0.f;
-  for (int p = 0; p < a.q_parts; ++p) {
+  for (int p = 0; p < a.q_parts; ++p)
     v += *reinterpret_cast<const floatx4*>(a.part_dq + (p * rows * a.Sq + r) * D + e);
-    total += a.part_total[(p * rows + bh) * a.q_pad + i];
-  }
-  const float norm = inverse(total);
   const int b = int(bh / a.nh), h = int(bh % a.nh);
   store4<T>(a.dq.p + b * a.dq.b + h * a.dq.h + i * a.dq.t + e * int(sizeof(T)),
-            v * (a.scale * norm));
+            v * (a.scale * a.norm[bh * a.q_pad + i]));
   if (e == 0) {
     float s = 0.f;
     for (int p = 0; p < a.q_parts; ++p) s += a.part_sum[(p * rows + bh) * a.q_pad + i];
-    a.ndelta[bh * a.q_pad + i] -= s * norm;
-    a.norm[bh * a.q_pad + i] = norm;
+    a.ndelta[bh * a.q_pad + i] -= s;
   }
 }
 

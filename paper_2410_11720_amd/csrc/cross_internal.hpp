@@ -57,7 +57,6 @@ struct CrossArgs {
   int q_parts = 1, kv_parts = 1;
   float* part_dq = nullptr;                // [q_parts][B][nh][Sq][D]
   float* part_sum = nullptr;               // [q_parts][B][nh][q_pad]
-  float* part_total = nullptr;             // the same
   float* part_dk = nullptr;                // [kv_parts][B][kvh][Sk][D]
   float* part_dv = nullptr;
   float* dbias = nullptr;                  // [buckets][nh]
