@@ -219,6 +219,12 @@ cross_bwd_q_kernel(CrossArgs a) {
         typename Tile::RowFrag kf, vf;
         Tile::load_rows(kf, img, 32 * n, lane);
         Tile::load_rows(vf, img + IMG, 32 * n, lane);
+        float x = 0.f;
+        int tb = 0;
+        if constexpr (BIAS) {
+          tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
+          x = tab[tb < a.bias.hi ? 0 : bias_span(a.bias) - 1];  // the side's entry, if in one
+        }
         issue_loads<AHEAD>();
         Tile::rows(s, kf, q);
         if constexpr (AHEAD) {
@@ -233,15 +239,9 @@ cross_bwd_q_kernel(CrossArgs a) {
         issue_loads<AHEAD>();
         float ce = c, off = nl;
         if constexpr (BIAS) {
-          int tb = k0 + 32 * n - start - w0;  // the block spans [tb - 31, tb + 31]
-          bool apart = false;
-          // (read here: kept in registers it makes three workgroups a CU spill)
-          if (tb + 31 <= a.bias.lo || tb - 31 >= a.bias.hi) {
-            const float x = BiasSides::read(tab + (tb < a.bias.hi ? 0 : bias_span(a.bias) - 1));
-            apart = side_apart(x);
-            if (apart) off += x;
-          }
-          if (!apart) {
+          if ((tb + 31 <= a.bias.lo || tb - 31 >= a.bias.hi) && uni(side_apart(x))) {
+            off += x;
+          } else {
             ce = 1.f;
             tb = clampi(tb, a.bias.lo - 32, a.bias.hi + 32);  // (where the table has entries)
             const float* p = tab + (tb - (lane & 31) + 4 * half - a.bias.lo + BIAS_PAD);
@@ -546,7 +546,9 @@ cross_bwd_kv_kernel(CrossArgs a) {
         Tile::rows(s, af, kf);
       }
       if constexpr (!VLDS) Tile::load_rows(af, img + IMG, 32 * n, lane);
-      const bool scaled = __any(norms[32 * n + (lane & 31)] != 1.f);
+      // (fp32 reads it where it is used: it has no register left)
+      float norm = 1.f;
+      if constexpr (sizeof(T) == 2) norm = norms[32 * n + (lane & 31)];
       // (registers 4 q .. 4 q + 3: rows 8 q + 4 half on)
       const float* nlr = nls + 32 * n + 4 * half;
       const float* ndr = nds + 32 * n + 4 * half;
@@ -591,7 +593,8 @@ cross_bwd_kv_kernel(CrossArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[r + e] = exp2_hw(fmaf(s[r + e], ce, BIAS ? l[e] + off : l[e]));
       }
-      if (scaled) {
+      if constexpr (sizeof(T) == 4) norm = norms[32 * n + (lane & 31)];
+      if (__any(norm != 1.f)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] *= norms[32 * n + 4 * half + 8 * (r >> 2) + (r & 3)];
       }
