@@ -180,9 +180,9 @@ Area area(const attn_cross_config* c, const attn_cross_tensor* t, int n, int nh)
   const int es = es_of(c);
   if (c->batch == 0 || n == 0) return Area{};
   Area a = Area::flat(t->data, size_t(c->head_dim) * es);
-  a.dim(0, t->batch_stride * es, c->batch);
-  a.dim(1, t->token_stride * es, n);
-  a.dim(2, t->head_stride * es, nh);
+  a.dim(0, t->batch_stride, c->batch, es);
+  a.dim(1, t->token_stride, n, es);
+  a.dim(2, t->head_stride, nh, es);
   return a;
 }
 

@@ -21,11 +21,12 @@ struct Area {
     a.row = int64_t(bytes);
     return a;
   }
-  void dim(int k, int64_t s, int64_t n) {
+  // (stride of s units; not looked at in a dimension of extent 1)
+  void dim(int k, int64_t s, int64_t n, int64_t unit = 1) {
     if (n < 2 || s == 0) return;
-    stride[k] = s;
+    stride[k] = s * unit;
     last[k] = n - 1;
-    end += uintptr_t(s) * uintptr_t(n - 1);
+    end += uintptr_t(stride[k]) * uintptr_t(n - 1);
   }
 };
 
