@@ -353,7 +353,9 @@ typedef struct {
                                    may be 0, lengths up to 2^29                   */
   int32_t heads, kv_heads;      /* kv_heads divides heads                          */
   int32_t head_dim;             /* 64 or 128                                       */
-  int32_t dtype;                /* ABFT_BF16 | ABFT_FP32 (every tensor; sums fp32)  */
+  int32_t dtype;                /* ABFT_BF16 | ABFT_FP32 (every tensor; sums and
+                                   statistics fp32; in bf16 the softmax's weights
+                                   and dS are rounded to it for their products)    */
   int32_t causal;               /* 1: key j > query position s + i is masked       */
   float   scale;                /* softmax scale; <= 0 -> 1/sqrt(head_dim)         */
   int32_t buckets;              /* rows of the bias table; 0: no bias              */

@@ -18,10 +18,10 @@
 // queries of all heads that share them (dk, dv, dtable). Small grids split the
 // other axis too, over the waves of a workgroup and over workgroups (cross_plan).
 // The price of two passes is a second S and dP (14 d flops a pair against 10 d in
-// one). Both are bound by their matrix and vector instructions, which hardly
-// overlap: 4 x 2048 queries over 1024 keys, 32 heads on 8, head dim 128: 250 and
-// 271 us, 0.82 and 1.01 PFLOP/s of bf16; 8 x 1024 causal, 12 heads, head dim 64,
-// with a bias: 43 and 59 us.
+// one). Matrix cores are busy for 41% and 49% of the passes' cycles at 4 x 2048
+// queries over 1024 keys, 32 heads on 8, head dim 128, the vector ALU for 43% and
+// 28%: 268 and 303 us (medians), 0.77 and 0.91 PFLOP/s of bf16. 8 x 1024 causal,
+// 12 heads, head dim 64, with a bias: 44 and 61 us.
 #include "cross_tile.hpp"
 
 namespace abft {
@@ -96,6 +96,8 @@ __device__ __forceinline__ void store4(char* p, floatx4 v) {
 
 // ---- query pass -----------------------------------------------------------
 // WV: workgroups a CU that its registers allow; at three nothing is read ahead.
+// (With a bias four forms spill: at three a CU 1 and 5 registers, at head dim 128
+// where waves share queries 5 and 9.)
 template <typename T, int D, bool BIAS, int NQ, int KS, int WV>
 __global__ __launch_bounds__(64 * NQ * KS, WV) void
 cross_bwd_q_kernel(CrossArgs a) {
@@ -397,10 +399,14 @@ __global__ __launch_bounds__(256) void cross_join_kv_kernel(CrossArgs a, int n) 
 // A workgroup has KW x QH waves: 32 KW keys, and QH waves on the same 32 that
 // take different rows of a query tile and join their sums at the end.
 // At head dim 128 the accumulators of both gradients and the keys' and values' own
-// fragments do not fit 256 registers beside the scores (36 spilled: the pass of
-// 4 x 2048 queries over 1024 keys, 32 heads on 8, 720 us). In bf16 the values' are
-// read from LDS, which leaves room for one workgroup a CU, of 8 waves (260 us;
-// of 4 waves 345 us). fp32 runs one wave per SIMD.
+// fragments do not fit 256 registers beside the scores (36 spilled, and the pass of
+// 4 x 2048 queries over 1024 keys, 32 heads on 8, took more than twice as long). In
+// bf16 the values' are read from LDS, which leaves room for one workgroup a CU, of 8
+// waves (of 4 waves a third slower). fp32 runs one wave per SIMD.
+// The forms that grids fill the chip with keep to their registers, but for fp32
+// with a bias at head dim 128 (4 spilled). Some for small grids do not: bf16 at
+// head dim 128, 2 x 4 waves with a bias (53 spilled) and 2 x 2 without (10); fp32 at
+// head dim 64 without a bias spills 18 to 33 in all three.
 template <typename T, int D, bool BIAS, int KW, int QH>
 __global__ __launch_bounds__(64 * KW * QH, (sizeof(T) * D == 512 ? 1 : 2)) void
 cross_bwd_kv_kernel(CrossArgs a) {

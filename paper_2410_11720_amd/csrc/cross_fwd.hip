@@ -98,9 +98,10 @@ __device__ __forceinline__ char* rest_row(const CrossArgs& a, int b, int h, int 
 // Tiled form: a workgroup owns 32 NQ queries of one head, KS waves for each 32 of
 // them; key tiles pass through LDS in two stages, the next one copied while this
 // one is worked on. The KS waves take different keys of a tile and join their
-// sums at the end. Bound by its matrix and vector instructions, which hardly
-// overlap: 4 x 2048 queries over 1024 keys, 32 heads on 8, head dim 128: 168 us,
-// 0.82 PFLOP/s of bf16; 8 x 1024 causal, 12 heads, head dim 64, with a bias: 28 us.
+// sums at the end. Matrix cores are busy for 45% of its cycles at 4 x 2048 queries
+// over 1024 keys, 32 heads on 8, head dim 128, the vector ALU for 50%: 171 us
+// (median), 0.80 PFLOP/s of bf16. 8 x 1024 causal, 12 heads, head dim 64, with a
+// bias: 24% and 56%, 28 us.
 template <typename T, int D, bool BIAS, int NQ, int KS>
 __global__ __launch_bounds__(64 * NQ * KS, 2) void cross_fwd_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;
@@ -242,7 +243,7 @@ constexpr int short_stages() { return D * int(sizeof(T)) > 256 ? 1 : 2; }
 // its own 32-key tiles in two stages without workgroup barriers; the waves'
 // results are joined in LDS, the splits' by cross_join_kernel. Bound by
 // reading K and V (32 sequences of one query over up to 1500 keys, 32 heads, head
-// dim 128: 118 us, 5.3 TB/s).
+// dim 128: 116 us, 5.4 TB/s).
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(256) void cross_short_kernel(CrossArgs a) {
   using Tile = CrossTile<T, D>;

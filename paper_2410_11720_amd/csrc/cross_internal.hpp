@@ -122,9 +122,9 @@ inline int cross_parts(int64_t wgs, size_t lds, int most, int64_t steps, int64_t
 
 // Whether the query pass has a form with fewer registers, three workgroups to a
 // CU. It takes grids that two a CU do not hold at once (cross attention of 8 x
-// 512 over 1000, 12 heads: both passes 68 -> 64 us; 2 x 4096, 32 heads: 997 ->
-// 979); a grid that two a CU hold is better off with fragments read ahead (16
-// heads x 4096: 258, in three 262 us).
+// 512 over 1000, 12 heads: both passes in 6% less; 2 x 4096, 32 heads: 2%); a
+// grid that two a CU hold is better off with fragments read ahead (16 heads x
+// 4096: in three 2% more).
 constexpr bool cross_three(int es, int D) { return es * D == 128; }
 
 // Shapes of the backward passes.

@@ -215,8 +215,11 @@ struct CrossTile {
     }
   }
 
-  // P as the second operand of `cols`: bf16 rounds it (the products take
-  // bf16 operands and sum in fp32), fp32 keeps it
+  // P (dS) as the second operand of `cols`. bf16 rounds it: the products take
+  // bf16 operands and sum in fp32. A result is then off by 0.0021 to 0.0024 of its
+  // norm, where its own rounding to bf16 is 0.0017; both parts of a split P would
+  // take a second product each (one of the forward's two, three of the
+  // passes' seven). fp32 keeps it.
   struct Probs {
     float x[BF ? 1 : 16];
     u32x4 b[BF ? 2 : 1];
