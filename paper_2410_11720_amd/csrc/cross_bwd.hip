@@ -33,8 +33,12 @@ namespace {
 template <typename T, int D>
 constexpr bool read_ahead() { return D * sizeof(T) == 128; }
 
-// |lse| past which a row's P are summed (its rounding is 2^-17 there)
-constexpr float LARGE_LSE = 256.f;
+// |lse| past which a row's P are summed: below, its rounding moves them by less than
+// 2^-12 in bf16, an eighth of their own rounding, and 2^-16 in fp32. (The sums cost a wave a
+// third pass over its keys: 8 x 512 over 1000, 12 heads, all rows large: 75 -> 119
+// us, with a bias of -1e9 throughout 100 -> 336.)
+template <typename T>
+constexpr float large_lse() { return sizeof(T) == 2 ? 4096.f : 256.f; }
 __device__ __forceinline__ float inverse(float total) { return total == 0.f ? 1.f : 1.f / total; }
 
 // Sum of 2^(s - lse) over the lane's row i, for the 32 rows of a wave from w0 on:
@@ -168,7 +172,7 @@ cross_bwd_q_kernel(CrossArgs a) {
   if constexpr (BIAS) bias_spread(tab, a.bias, h, a.nh, tid, 64 * NW);
   float sum = 0.f;   // of the row's dS
   float norm = 1.f;  // what its P (and with them dS) are to be multiplied by
-  if (__any(nl != NEG_INF && !(fabsf(nl) <= LARGE_LSE)))
+  if (__any(nl != NEG_INF && !(fabsf(nl) <= large_lse<T>())))
     norm = inverse(row_total<T, D, BIAS>(a, q, nl, b, h, w0, wend, lane));
 
   // rows between the last query and the end of the key pass's tiles: P = 0
