@@ -460,6 +460,148 @@ int clip_gradients(const abft_grad* grads, int32_t n, double max_norm, abft_grad
                    void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * What stands between attention layers in a block: layer norm, dropout whose mask
+ * is never stored, both behind a residual in one pass, rotary positions. No
+ * checksums, like attention over keys of another length; conventions as at the
+ * top. Sums and statistics are fp32, results do not depend on scheduling, and
+ * calls that share neither workspace nor outputs may overlap.
+ * ------------------------------------------------------------------------- */
+
+/* A tensor [batch, tokens, cols]; strides in elements, columns contiguous, any
+ * alignment of the element. Inputs may repeat memory (stride 0: one row for all
+ * tokens, one sequence for the batch; a gradient is that of each row, and the
+ * caller sums it over the repeats), outputs not: sorted, an output's strides each
+ * pass the extent of the one before. An output may be one of the call's inputs of
+ * this type (same data and strides), and shares no memory with any other argument
+ * (ABFT_ERR_INVALID). Strides of dimensions of extent 1 and tensors without
+ * elements are not looked at. batch * tokens < 2^31. */
+typedef struct {
+  const void* data;
+  int64_t batch_stride, token_stride;
+} attn_rows;
+
+/* Dropout. Element (b, token, col) of row r = b * tokens + token stays if its draw
+ * of 16 bits, a function of (seed, offset, site, r, col) alone, is at least
+ *   t = floor(65536 p + 1/2)
+ * and is then scaled by 65536 / (65536 - t): the sum's expectation is kept for the
+ * probability t / 65536 that is drawn. Dropped elements are 0 whatever they held.
+ * The draw is half col % 8 (low half of word 0 first) of the Philox4x32-10 block
+ * (Salmon et al., SC 2011) of counter (col / 8 + 2^13 site, r, offset low, offset
+ * high) under the key (seed low, seed high). rng (device, 8-byte aligned) holds
+ * seed and offset: a captured graph draws anew once its owner has advanced offset.
+ * Calls that share both keep apart by `site`. A backward takes the values that its
+ * forward had. */
+typedef struct {
+  int32_t batch, tokens;
+  int32_t cols;                 /* 1 .. 65536                                     */
+  int32_t dtype;                /* ABFT_BF16 | ABFT_FP32                          */
+  double  dropout;              /* p in [0, 1]                                    */
+  uint32_t site;                /* below 2^16                                     */
+  int32_t reserved;
+} attn_dropout_config;
+
+/* The draw of an element, in [0, 65535] (host only). */
+int attn_dropout_draw(uint64_t seed, uint64_t offset, uint32_t site, uint32_t row, uint32_t col);
+
+/* y = residual + dropout(x); residual NULL (or its data): none. Its backward is
+ * dx = dropout(dy) by the same call (the residual's gradient is dy itself). rng is
+ * not looked at where p < 2^-17. */
+int attn_dropout(const attn_dropout_config* cfg, const attn_rows* x, const attn_rows* residual,
+                 const uint64_t* rng, const attn_rows* y, void* stream);
+
+/* Layer norm: with mean and var (over cols, not cols - 1) of a row of h,
+ *   y = (h - mean) / sqrt(var + eps) weight + bias,
+ * of h = x, or of h = residual + dropout(x) as it is stored (in bf16 rounded once):
+ * the same bits as attn_dropout and a norm of its result. A row of finite elements
+ * up to 2^125 gives finite results, one with INF or NaN gives NaN. */
+typedef struct {
+  int32_t batch, tokens;
+  int32_t cols;                 /* 1 .. 16384                                     */
+  int32_t dtype;                /* of rows: ABFT_BF16 | ABFT_FP32                 */
+  int32_t weight_dtype;         /* of weight and bias; their gradients are fp32   */
+  uint32_t site;                /* dropout, as above: p > 0 needs a residual      */
+  double  dropout;
+  double  eps;                  /* >= 1e-30                                       */
+} attn_norm_config;
+
+/* Forward.
+ *   x, residual (NULL: none); weight, bias (device) [cols], NULL: 1 and 0
+ *   lens (device) [batch] int32 tokens of each sequence, NULL: all. Rows behind
+ *     them are not read, whatever they hold; results and gradients there are 0
+ *   h, y  results; h (with a residual) may be NULL, stats too
+ *   stats (device) [batch][tokens][2] fp32, 8-byte aligned: mean and 1 / sqrt(var +
+ *     eps) of each row, what the backward takes */
+int attn_norm_forward(const attn_norm_config* cfg, const attn_rows* x, const attn_rows* residual,
+                      const void* weight, const void* bias, const int32_t* lens, const uint64_t* rng,
+                      const attn_rows* h, const attn_rows* y, float* stats, void* stream);
+
+/* Bytes of device workspace the backward needs for dweight and dbias; 0 if the
+ * config is invalid. Its contents do not outlive a call. */
+size_t attn_norm_workspace_bytes(const attn_norm_config* cfg /* host */);
+
+/* Backward: from dy, dh (what else comes to h, NULL: nothing), h (x without a
+ * residual) and the forward's stats,
+ *   dresidual = the gradient of h, dx = dropout(dresidual),
+ *   dweight, dbias (device) [cols] fp32, over all rows (0 where there are none).
+ * Each result may be NULL (without dropout dx and dresidual are alike, and one of
+ * them is enough); the workspace is needed for the last two. */
+int attn_norm_backward(const attn_norm_config* cfg, const attn_rows* dy, const attn_rows* dh,
+                       const attn_rows* h, const void* weight, const float* stats,
+                       const int32_t* lens, const uint64_t* rng, const attn_rows* dx,
+                       const attn_rows* dresidual, float* dweight, float* dbias, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Rotary positions of queries and keys: of a head's first rotary_dim dims, pair k
+ * (dims k and rotary_dim / 2 + k; interleaved: 2 k and 2 k + 1) of the token at
+ * position p is turned by the angle p freqs[k] and scaled by magnitude,
+ *   (a, c) -> magnitude (a cos - c sin, a sin + c cos);
+ * the other dims stay. Token i of sequence b lies at position q_start[b] + i, as in
+ * attn_cross_forward; negative ones are turned back. Angles are formed and reduced
+ * in 64 bits. */
+typedef struct {
+  int32_t batch, tokens;
+  int32_t heads, kv_heads;      /* of Q and of K; either may be 0 (its tensors are
+                                   then not looked at); heads + 2 kv_heads <= 65536 */
+  int32_t head_dim;             /* 1 .. 512                                       */
+  int32_t rotary_dim;           /* even, 0 .. head_dim                            */
+  int32_t interleaved;
+  int32_t dtype;                /* ABFT_BF16 | ABFT_FP32                          */
+  float   magnitude;            /* <= 0 -> 1                                      */
+} attn_rotary_config;
+
+/* Frequencies in radians a position, freqs[rotary_dim / 2] (host):
+ *   PLAIN   f_k = base^(-2 k / rotary_dim)
+ *   LINEAR  f_k / factor (positions interpolated)
+ *   PARTS   f_k where its angle makes high_turns or more over original_len
+ *           positions, f_k / factor where it makes low_turns or fewer, and in
+ *           between their mean by the number of turns
+ * Any other table may be used in their place. Returns ABFT_OK or ABFT_ERR_INVALID. */
+#define ABFT_ROTARY_PLAIN 0
+#define ABFT_ROTARY_LINEAR 1
+#define ABFT_ROTARY_PARTS 2
+int attn_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                            double original_len, double low_turns, double high_turns, double* freqs);
+
+/* Q_out, K_out [batch, tokens, heads or kv_heads, head_dim] from Q and K, or with
+ * backward = 1 dQ and dK from the gradients of the turned ones. freqs (device)
+ * [rotary_dim / 2]; q_start (device) [batch], NULL: 0. Tensors need the alignment of
+ * their element only; outputs as in attn_cross_forward, or in place (Q_out on Q,
+ * K_out on K). */
+int attn_rotary(const attn_rotary_config* cfg, int32_t backward, const attn_cross_tensor* Q,
+                const attn_cross_tensor* K, const double* freqs, const int32_t* q_start,
+                const attn_cross_tensor* Q_out, const attn_cross_tensor* K_out, void* stream);
+
+/* The same (forward) for new tokens over a cache: turned keys and the values go to
+ * rows q_start[b] + i of K_cache and V_cache [batch, capacity, kv_heads, head_dim],
+ * which attn_cross_forward reads. Tokens whose row is not in [0, capacity) are left
+ * out; no other row of the caches is touched. */
+int attn_rotary_append(const attn_rotary_config* cfg, const attn_cross_tensor* Q,
+                       const attn_cross_tensor* K, const attn_cross_tensor* V, const double* freqs,
+                       const int32_t* q_start, int32_t capacity, const attn_cross_tensor* Q_out,
+                       const attn_cross_tensor* K_cache, const attn_cross_tensor* V_cache,
+                       void* stream);
+
+/* ---------------------------------------------------------------------------
  * Adaptive detection frequencies (paper Sec. 4.5, Algorithm 1). Host-only
  * calls (no device memory, no stream): they choose how often each
  * protection section is checked and produce the `sections` mask of a

@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libattn_abft.so")
 SOURCES = ["gemm_abft.hip", "gemm_wide.hip", "softmax_abft.hip", "encode_verify.hip", "fused_attn.hip", "attn_abft.hip",
-           "cross_fwd.hip", "cross_bwd.hip", "cross_attn.cpp", "grad_clip.hip", "adaptive.cpp"]
+           "cross_fwd.hip", "cross_bwd.hip", "cross_attn.cpp", "grad_clip.hip",
+           "norm_fwd.hip", "norm_bwd.hip", "dropout.hip", "rotary.hip", "block_ops.cpp", "adaptive.cpp"]
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 FLAGS = [

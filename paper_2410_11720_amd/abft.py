@@ -88,6 +88,30 @@ class Grad(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class NormConfigC(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("site", ctypes.c_uint32), ("dropout", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class DropoutConfigC(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("dropout", ctypes.c_double), ("site", ctypes.c_uint32),
+                ("reserved", ctypes.c_int32)]
+
+
+class RotaryConfigC(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64)]
+
+
 REPORT_HEADER = 32  # bytes before the event array
 assert ctypes.sizeof(Event) == 40 and ctypes.sizeof(Fault) == 28
 
@@ -95,6 +119,8 @@ _vp, _sz, _i32, _i64, _f32, _u32 = (ctypes.c_void_p, ctypes.c_size_t, ctypes.c_i
                                    ctypes.c_int64, ctypes.c_float, ctypes.c_uint32)
 _P = ctypes.POINTER(Config)
 _CP = ctypes.POINTER(CrossConfigC)
+_NP, _DP, _RP = map(ctypes.POINTER, (NormConfigC, DropoutConfigC, RotaryConfigC))
+_u64, _f64 = ctypes.c_uint64, ctypes.c_double
 _sig = {
     "attn_abft_workspace_bytes": (_sz, [_P]),
     "attn_abft_report_bytes": (_sz, [_i32]),
@@ -131,6 +157,15 @@ _sig = {
     "global_grad_norm": (ctypes.c_int, [_vp, _i32, _vp, _vp, _sz, _vp]),
     "clip_gradients": (ctypes.c_int, [_vp, _i32, ctypes.c_double, _vp, _vp, _sz, _vp]),
     "attn_abft_forward_noalloc": (ctypes.c_int, [_P, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "attn_dropout_draw": (ctypes.c_int, [_u64, _u64, _u32, _u32, _u32]),
+    "attn_dropout": (ctypes.c_int, [_DP, _vp, _vp, _vp, _vp, _vp]),
+    "attn_norm_workspace_bytes": (_sz, [_NP]),
+    "attn_norm_forward": (ctypes.c_int, [_NP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "attn_norm_backward": (ctypes.c_int, [_NP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                          _vp, _vp, _sz, _vp]),
+    "attn_rotary_frequencies": (ctypes.c_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp]),
+    "attn_rotary": (ctypes.c_int, [_RP, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "attn_rotary_append": (ctypes.c_int, [_RP, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -706,3 +741,372 @@ class GradientClip:
                      self.stats.raw.data_ptr(), self.workspace.data_ptr(),
                      self.workspace.numel()), "clip_gradients")
         return self.stats
+
+
+# ---- layer norm, dropout, rotary positions ----------------------------------------
+
+_DTYPES = {"bf16": (BF16, torch.bfloat16), "f32": (FP32, torch.float32)}
+
+
+def _dtype_of(name, what):
+    if name not in _DTYPES:
+        raise AbftError(f"{what}: {name!r} is neither \"bf16\" nor \"f32\"")
+    return _DTYPES[name]
+
+
+class _Op:
+    """Marshalling that the classes below share: tensors of one type and device
+    as records of address and strides."""
+
+    def _records(self, names, tensors, shapes):
+        """Records (address, all strides but the last) one after the other, None
+        for an absent tensor; returns them and the address of each."""
+        fields, at, dtype, index = [], [], self._dtype, self.device.index
+        for name, t, shape in zip(names, tensors, shapes):
+            at.append(None)
+            if t is None:
+                continue
+            st = t.stride()
+            if t.get_device() != index or t.dtype != dtype or t.shape != shape or (
+                    st[-1] != 1 and shape[-1] > 1):
+                raise AbftError(f"{name}: expected {tuple(shape)} {dtype} on {self.device} with a "
+                                f"contiguous last dimension, got {tuple(t.shape)} {t.dtype} on "
+                                f"{t.device}, strides {st}")
+            at[-1] = 8 * len(fields)
+            fields.append(t.data_ptr())
+            fields += st[:-1]
+        held = array.array("q", fields)
+        base = held.buffer_info()[0]
+        return held, [None if a is None else base + a for a in at]
+
+    def _vector(self, t, name, shape, dtype):
+        if t is None:
+            return None
+        if (t.get_device() != self.device.index or t.dtype != dtype or t.shape != shape
+                or not t.is_contiguous()):
+            raise AbftError(f"{name}: expected contiguous {shape} {dtype} on {self.device}, got "
+                            f"{tuple(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def _state(self, rng, used):
+        if rng is None and used:
+            raise AbftError("rng: dropout needs its seed and offset")
+        return self._vector(rng, "rng", (2,), torch.int64)
+
+
+def attn_dropout_draw(seed: int, offset: int, site: int, row: int, col: int) -> int:
+    """The 16-bit draw of an element (host only): it stays if the draw is at least
+    floor(65536 p + 1/2)."""
+    k = _lib.attn_dropout_draw(seed % 2 ** 64, offset % 2 ** 64, site, row, col)
+    if k < 0:
+        raise AbftError(f"attn_dropout_draw: {strerror(k)} ({k})")
+    return k
+
+
+@dataclasses.dataclass
+class DropoutConfig:
+    batch: int
+    tokens: int
+    cols: int
+    dtype: str = "bf16"          # "bf16" | "f32"
+    p: float = 0.1
+    site: int = 0                # tells calls that share seed and offset apart
+
+    def to_c(self) -> DropoutConfigC:
+        return DropoutConfigC(self.batch, self.tokens, self.cols, _dtype_of(self.dtype, "dtype")[0],
+                              self.p, self.site, 0)
+
+
+class Dropout(_Op):
+    """Dropout of rows [batch, tokens, cols], with an optional residual. No mask is
+    stored: which elements stay follows from their position, `site` and `rng`, an
+    int64 tensor (seed, offset) on the device, whose owner advances the offset from
+    step to step; a backward takes the values that its forward had. Any strides with
+    contiguous columns; results not given are laid out as torch.empty_like of x or
+    dy, and may be an input (in place). Calls run on the current stream of the
+    tensors' device."""
+
+    def __init__(self, cfg: DropoutConfig, device="cuda"):
+        self.cfg = cfg
+        self.device = torch.empty(0, device=device).device
+        self._c = cfg.to_c()
+        self._dtype = _DTYPES[cfg.dtype][1]
+        self._shape = (cfg.batch, cfg.tokens, cfg.cols)
+
+    def _run(self, names, x, residual, rng, y):
+        held, (x, r, y) = self._records(names, (x, residual, y), (self._shape,) * 3)
+        rng = self._state(rng, self.cfg.p >= 2.0 ** -17)
+        _check(_call(_lib.attn_dropout, self.device, self._c, x, r, rng, y), "attn_dropout")
+
+    def forward(self, x, rng=None, residual=None, y=None):
+        """residual + dropout(x)."""
+        y = torch.empty_like(x) if y is None else y
+        self._run(("x", "residual", "y"), x, residual, rng, y)
+        return y
+
+    def backward(self, dy, rng=None, dx=None):
+        """dropout(dy), the gradient of x; that of the residual is dy itself."""
+        dx = torch.empty_like(dy) if dx is None else dx
+        self._run(("dy", "", "dx"), dy, None, rng, dx)
+        return dx
+
+
+@dataclasses.dataclass
+class NormConfig:
+    batch: int
+    tokens: int
+    cols: int
+    dtype: str = "bf16"          # of the rows: "bf16" | "f32"
+    weight_dtype: str = "f32"    # of gain and offset; their gradients are fp32
+    eps: float = 1e-5
+    dropout: float = 0.0         # ResidualNorm only
+    site: int = 0
+
+    def to_c(self) -> NormConfigC:
+        return NormConfigC(self.batch, self.tokens, self.cols, _dtype_of(self.dtype, "dtype")[0],
+                           _dtype_of(self.weight_dtype, "weight_dtype")[0], self.site, self.dropout,
+                           self.eps)
+
+
+def attn_norm_workspace_bytes(cfg: NormConfig) -> int:
+    c = cfg.to_c()
+    n = _lib.attn_norm_workspace_bytes(ctypes.byref(c))
+    if n == 0:
+        raise AbftError("invalid configuration")
+    return n
+
+
+class NormSaved:
+    """What a forward leaves for its backward: mean and 1 / deviation of each row."""
+
+    def __init__(self, cfg: NormConfig, device):
+        self.stats = torch.empty((cfg.batch, cfg.tokens, 2), dtype=torch.float32, device=device)
+        self._of = None              # where the rows that they belong to are
+
+
+class _Norm(_Op):
+    def __init__(self, cfg: NormConfig, device="cuda", training=True):
+        self.cfg = cfg
+        self.device = torch.empty(0, device=device).device
+        self._c = cfg.to_c()
+        n = attn_norm_workspace_bytes(cfg)
+        self.workspace = None
+        if training:
+            self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self._saved = self.new_saved() if training else None
+        self._dtype, self._wdtype = _DTYPES[cfg.dtype][1], _DTYPES[cfg.weight_dtype][1]
+        self._shape = (cfg.batch, cfg.tokens, cfg.cols)
+
+    @property
+    def stats(self):
+        return self._saved and self._saved.stats
+
+    def new_saved(self):
+        """Another record for a forward and its backward."""
+        return NormSaved(self.cfg, self.device)
+
+    def _record(self, saved):
+        if saved.stats.shape != (*self._shape[:2], 2) or saved.stats.device != self.device:
+            raise AbftError("saved: made for another shape or device")
+        return saved
+
+    def _forward(self, x, residual, weight, bias, lens, rng, h, y, saved):
+        held, (x_, r_, h_, y_) = self._records(("x", "residual", "h", "y"), (x, residual, h, y),
+                                               (self._shape,) * 4)
+        cols = self._shape[2:]
+        saved = self._saved if saved is None else self._record(saved)
+        stats = None
+        if saved is not None:
+            stats, saved._of = saved.stats.data_ptr(), None
+        _check(_call(_lib.attn_norm_forward, self.device, self._c, x_, r_,
+                     self._vector(weight, "weight", cols, self._wdtype),
+                     self._vector(bias, "bias", cols, self._wdtype),
+                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, h_, y_, stats),
+               "attn_norm_forward")
+        if saved is not None:
+            saved._of = (x if residual is None else h).data_ptr()
+
+    def _backward(self, dy, dh, h, weight, lens, rng, dx, dresidual, dweight, dbias, saved):
+        own = saved is None
+        saved = self._saved if own else self._record(saved)
+        if saved is None or self.workspace is None:
+            raise AbftError("backward: made with training=False")
+        if saved._of is None or own and saved._of != h.data_ptr():
+            raise AbftError("backward: the rows are not those of the last forward"
+                            if saved._of is not None
+                            else "backward: no forward has left its statistics")
+        cols = self._shape[2:]
+        if dweight is None:
+            dweight = torch.empty(cols, dtype=torch.float32, device=self.device)
+        if dbias is None:
+            dbias = torch.empty(cols, dtype=torch.float32, device=self.device)
+        held, (dy_, dh_, h_, dx_, dr_) = self._records(
+            ("dy", "dh", "h", "dx", "dresidual"), (dy, dh, h, dx, dresidual), (self._shape,) * 5)
+        _check(_call(_lib.attn_norm_backward, self.device, self._c, dy_, dh_, h_,
+                     self._vector(weight, "weight", cols, self._wdtype), saved.stats.data_ptr(),
+                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, dx_, dr_,
+                     self._vector(dweight, "dweight", cols, torch.float32),
+                     self._vector(dbias, "dbias", cols, torch.float32),
+                     self.workspace.data_ptr(), self.workspace.numel()), "attn_norm_backward")
+        return dweight, dbias
+
+
+class LayerNorm(_Norm):
+    """Layer norm of rows [batch, tokens, cols]: owns the workspace of one shape
+    and one record of what a forward leaves for its backward (`stats`), as
+    CrossAttention does; with training=False it has neither. A forward replaces the
+    record: backward raises if x is not the last forward's. Where other forwards come
+    in between, or x has moved since, pass a record of `new_saved` to both calls as
+    `saved`; which x belongs to it is then the caller's to know. Calls run on the
+    current stream of the tensors' device.
+
+    weight and bias [cols] may be None (1 and 0); lens [batch] int32: tokens of
+    each sequence, behind them nothing is read and results are 0. Any strides with
+    contiguous columns; results not given are laid out as torch.empty_like of x or
+    dy, and may be an input (in place; y on x only where no backward follows)."""
+
+    def __init__(self, cfg: NormConfig, device="cuda", training=True):
+        if cfg.dropout != 0.0:
+            raise AbftError("dropout stands in front of a ResidualNorm")
+        super().__init__(cfg, device, training)
+
+    def forward(self, x, weight=None, bias=None, lens=None, y=None, saved=None):
+        y = torch.empty_like(x) if y is None else y
+        self._forward(x, None, weight, bias, lens, None, None, y, saved)
+        return y
+
+    def backward(self, dy, x, weight=None, lens=None, dx=None, dweight=None, dbias=None, saved=None):
+        """dx, dweight, dbias."""
+        dx = torch.empty_like(dy) if dx is None else dx
+        dweight, dbias = self._backward(dy, None, x, weight, lens, None, dx, None, dweight, dbias,
+                                        saved)
+        return dx, dweight, dbias
+
+
+class ResidualNorm(_Norm):
+    """h = residual + dropout(x) as it is stored, and its layer norm y, in one pass
+    each way: the same bits as Dropout and LayerNorm one after the other. Records and
+    tensors as of LayerNorm (backward takes h, and raises if it is not the last
+    forward's), rng as of Dropout. In place: h on x or on the residual."""
+
+    def forward(self, x, residual, weight=None, bias=None, rng=None, lens=None, h=None, y=None,
+                saved=None):
+        """h, y."""
+        h = torch.empty_like(x) if h is None else h
+        y = torch.empty_like(x) if y is None else y
+        if residual is None:
+            raise AbftError("residual: LayerNorm is the norm without one")
+        self._forward(x, residual, weight, bias, lens, self._state(rng, self.cfg.dropout >= 2.0 ** -17),
+                      h, y, saved)
+        return h, y
+
+    def backward(self, dy, h, weight=None, dh=None, rng=None, lens=None, dx=None, dresidual=None,
+                 dweight=None, dbias=None, saved=None):
+        """dx, dresidual, dweight, dbias. dh: what comes to h beside its norm's
+        gradient. Without dropout dx and dresidual are alike: one tensor unless both
+        are given."""
+        drops = self.cfg.dropout >= 2.0 ** -17
+        if dx is None:
+            dx = torch.empty_like(dy) if drops or dresidual is None else dresidual
+        if dresidual is None:
+            dresidual = torch.empty_like(dy) if drops else dx
+        second = None if dresidual is dx else dresidual
+        dweight, dbias = self._backward(dy, dh, h, weight, lens, self._state(rng, drops), dx, second,
+                                        dweight, dbias, saved)
+        return dx, dresidual, dweight, dbias
+
+
+@dataclasses.dataclass
+class RotaryConfig:
+    batch: int
+    tokens: int
+    heads: int
+    head_dim: int
+    kv_heads: int = 0            # 0: one key head per query head
+    rotary_dim: int = 0          # 0: the whole head
+    interleaved: bool = False    # pairs of neighbours; else dims k and rotary_dim / 2 + k
+    dtype: str = "bf16"          # "bf16" | "f32"
+    base: float = 10000.0
+    scaling: str = "none"        # "none" | "linear" | "parts" (attn_rotary_frequencies)
+    factor: float = 1.0
+    original_len: float = 2048
+    low_turns: float = 1.0
+    high_turns: float = 32.0
+    magnitude: float = 1.0
+
+    def to_c(self) -> RotaryConfigC:
+        return RotaryConfigC(self.batch, self.tokens, self.heads, self.kv_heads or self.heads,
+                             self.head_dim, self.rotary_dim or self.head_dim, int(self.interleaved),
+                             _dtype_of(self.dtype, "dtype")[0], self.magnitude)
+
+
+def attn_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none",
+                            factor: float = 1.0, original_len: float = 2048,
+                            low_turns: float = 1.0, high_turns: float = 32.0) -> list:
+    """Radians a position of each pair (host only)."""
+    kinds = {"none": 0, "linear": 1, "parts": 2}
+    if scaling not in kinds:
+        raise AbftError(f"scaling: {scaling!r} is none of {sorted(kinds)}")
+    out = (ctypes.c_double * max(1, rotary_dim // 2))()
+    _check(_lib.attn_rotary_frequencies(rotary_dim, base, kinds[scaling], factor, original_len,
+                                        low_turns, high_turns, ctypes.addressof(out)),
+           "attn_rotary_frequencies")
+    return list(out)[:rotary_dim // 2]
+
+
+class Rotary(_Op):
+    """Rotary positions of queries and keys [batch, tokens, heads, head_dim]: holds
+    the frequencies of one configuration on the device (`freqs`, fp64, which may be
+    replaced by others). Token i of sequence b lies at position q_start[b] + i (q_start
+    [batch] int32, None: 0), as CrossAttention has it. Any strides with contiguous
+    dims; results not given are laid out as torch.empty_like of Q or K, and may be Q or
+    K (in place). Calls run on the current stream of the tensors' device."""
+
+    def __init__(self, cfg: RotaryConfig, device="cuda"):
+        self.cfg = cfg
+        self.device = torch.empty(0, device=device).device
+        self._c = cfg.to_c()
+        self._dtype = _DTYPES[cfg.dtype][1]
+        freqs = attn_rotary_frequencies(self._c.rotary_dim, cfg.base, cfg.scaling, cfg.factor,
+                                        cfg.original_len, cfg.low_turns, cfg.high_turns)
+        self.freqs = torch.tensor(freqs, dtype=torch.float64, device=self.device)
+        self._q_shape = (cfg.batch, cfg.tokens, cfg.heads, cfg.head_dim)
+        self._k_shape = (cfg.batch, cfg.tokens, self._c.kv_heads, cfg.head_dim)
+
+    def _at(self, q_start):
+        return (self._vector(self.freqs, "freqs", (self._c.rotary_dim // 2,), torch.float64),
+                self._vector(q_start, "q_start", (self.cfg.batch,), torch.int32))
+
+    def _turn(self, backward, names, Q, K, q_start, Q_out, K_out):
+        Q_out = torch.empty_like(Q) if Q_out is None else Q_out
+        K_out = torch.empty_like(K) if K_out is None else K_out
+        qs, ks = self._q_shape, self._k_shape
+        held, (q, k, qo, ko) = self._records(names, (Q, K, Q_out, K_out), (qs, ks, qs, ks))
+        freqs, start = self._at(q_start)
+        _check(_call(_lib.attn_rotary, self.device, self._c, backward, q, k, freqs, start, qo, ko),
+               "attn_rotary")
+        return Q_out, K_out
+
+    def forward(self, Q, K, q_start=None, Q_out=None, K_out=None):
+        """The turned queries and keys."""
+        return self._turn(0, ("Q", "K", "Q_out", "K_out"), Q, K, q_start, Q_out, K_out)
+
+    def backward(self, dQ, dK, q_start=None, dQ_out=None, dK_out=None):
+        """Gradients of Q and K from those of the turned ones."""
+        return self._turn(1, ("dQ", "dK", "dQ_out", "dK_out"), dQ, dK, q_start, dQ_out, dK_out)
+
+    def append(self, Q, K, V, K_cache, V_cache, q_start=None, Q_out=None):
+        """Returns the turned queries; turned keys and the values go to rows q_start +
+        i of the caches [batch, capacity, kv_heads, head_dim] (left out where the
+        caches have no such row)."""
+        Q_out = torch.empty_like(Q) if Q_out is None else Q_out
+        qs, ks = self._q_shape, self._k_shape
+        capacity = K_cache.shape[1]
+        cs = (ks[0], capacity, ks[2], ks[3])
+        held, (q, k, v, qo, kc, vc) = self._records(
+            ("Q", "K", "V", "Q_out", "K_cache", "V_cache"), (Q, K, V, Q_out, K_cache, V_cache),
+            (qs, ks, ks, qs, cs, cs))
+        freqs, start = self._at(q_start)
+        _check(_call(_lib.attn_rotary_append, self.device, self._c, q, k, v, freqs, start, capacity,
+                     qo, kc, vc), "attn_rotary_append")
+        return Q_out

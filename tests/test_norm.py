@@ -1,0 +1,589 @@
+"""Layer norm, alone and behind a residual with dropout, against its definition in
+64 bits: forward, backward, every width of the kernels' shapes, padded sequences,
+strides, extreme rows; refusals."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import block_reference as R
+from paper_2410_11720_amd import abft
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+RNG = (0x123456789ABCDEF, 77)
+
+
+# ---- host: refusals -----------------------------------------------------------------
+
+def _cfg(**kw):
+    base = dict(batch=2, tokens=3, cols=40)
+    base.update(kw)
+    return abft.NormConfig(**base)
+
+
+@pytest.mark.parametrize("kw", [dict(batch=-1), dict(tokens=-1), dict(cols=0), dict(cols=-5),
+                                dict(cols=16385), dict(batch=2 ** 16, tokens=2 ** 15),
+                                dict(eps=0.0), dict(eps=math.nan), dict(eps=math.inf),
+                                dict(eps=1e-31), dict(dropout=-0.1), dict(dropout=1.5),
+                                dict(dropout=math.nan), dict(site=65536), dict(dtype="f16"),
+                                dict(weight_dtype="int8")])
+def test_config_refusals(kw):
+    with pytest.raises(abft.AbftError):
+        abft.attn_norm_workspace_bytes(_cfg(**kw))
+
+
+def test_workspace_bytes():
+    one = abft.attn_norm_workspace_bytes(_cfg())
+    assert 2 * 40 * 4 <= one <= 2 * 128 * 4
+    # (512 workgroups at most, each with both sums)
+    assert abft.attn_norm_workspace_bytes(_cfg(batch=64, tokens=4096, cols=16384)) <= 512 * 2 * 16384 * 4
+    assert abft.attn_norm_workspace_bytes(_cfg(batch=0)) > 0
+
+
+G = 1 << 30
+
+
+def _t(ptr, stride=(120, 40)):
+    return ctypes.byref(abft.Rows(ptr, *stride))
+
+
+def _forward(cfg=None, x=None, res=None, w=None, b=None, lens=None, rng=None, h=None, y=None,
+             stats=None):
+    c = (cfg or _cfg()).to_c()
+    return abft._lib.attn_norm_forward(c, x or _t(G), res, w, b, lens, rng, h, y or _t(2 * G), stats,
+                                       None)
+
+
+def _passes(status):
+    """Every check of the arguments is passed: what is left is the device (there is
+    none in a run of these tests without a GPU; addresses are never followed)."""
+    return status not in (-1, -2, -4)
+
+
+def test_forward_refuses_before_any_launch():
+    assert _forward(x=_t(0)) == -1 and _forward(y=_t(0)) == -1
+    assert _forward(x=_t(G + 1)) == -1 and _forward(y=_t(2 * G + 1)) == -1
+    assert _forward(x=_t(G, (-120, 40))) == -1 and _forward(y=_t(2 * G, (120, -40))) == -1
+    assert _forward(y=_t(2 * G, (120, 39))) == -1              # rows on one another
+    assert _forward(y=_t(2 * G, (0, 40))) == -1                # sequences on one another
+    assert _forward(y=_t(2 * G, (40, 79))) == -1
+    assert _forward(x=_t(G, (2 ** 60, 40))) == -1
+    assert _forward(w=G + 2 * G + 2) == -1 and _forward(b=3 * G + 2) == -1   # fp32 parameters
+    assert _forward(lens=3 * G + 2) == -1 and _forward(stats=3 * G + 4) == -1
+    # outputs that share memory with other arguments
+    assert _forward(y=_t(G + 80)) == -1                        # x, shifted by a row
+    assert _forward(y=_t(G + 40)) == -1
+    assert _forward(w=2 * G) == -1 and _forward(b=2 * G + 476) == -1
+    assert _forward(lens=2 * G) == -1 and _forward(stats=2 * G) == -1 and _forward(stats=G) == -1
+    # dropout without residual, without state, a sum without a residual
+    drop = _cfg(dropout=0.5)
+    assert _forward(drop, rng=3 * G) == -1
+    assert _forward(drop, res=_t(4 * G)) == -1
+    assert _forward(drop, res=_t(4 * G), rng=3 * G + 4) == -1
+    assert _forward(h=_t(4 * G)) == -1
+    assert _forward(res=_t(4 * G), h=_t(2 * G)) == -1          # h on y
+    assert _forward(drop, res=_t(4 * G), rng=2 * G + 8) == -1  # the state on y
+    # nothing to do
+    assert _forward(_cfg(batch=0)) == 0 and _forward(_cfg(tokens=0), x=_t(0), y=_t(0)) == 0
+
+
+def _backward(cfg=None, dy=None, dh=None, h=None, w=None, stats=5 * G, lens=None, rng=None, dx=None,
+              dres=None, dw=None, db=None, ws=6 * G, ws_bytes=1 << 20):
+    c = (cfg or _cfg()).to_c()
+    return abft._lib.attn_norm_backward(c, dy or _t(G), dh, h or _t(3 * G), w, stats, lens, rng,
+                                        dx or _t(2 * G), dres, dw, db, ws, ws_bytes, None)
+
+
+def test_backward_refuses_before_any_launch():
+    assert _backward(dy=_t(0)) == -1 and _backward(h=_t(0)) == -1 and _backward(stats=None) == -1
+    assert _backward(stats=5 * G + 4) == -1 and _backward(dw=7 * G, ws=None) == -1
+    assert _backward(dw=7 * G, ws=6 * G + 8) == -1 and _backward(dw=7 * G, ws_bytes=64) == -4
+    assert _backward(dw=7 * G + 2) == -1 and _backward(db=7 * G + 1) == -1
+    assert _backward(dw=7 * G, db=7 * G + 156) == -1           # one on the other
+    assert _backward(dw=6 * G) == -1                           # on the workspace
+    assert _backward(dx=_t(6 * G), dw=7 * G) == -1
+    assert _backward(dx=_t(5 * G)) == -1 and _backward(dres=_t(2 * G)) == -1
+    assert _backward(dx=_t(G + 80)) == -1 and _backward(dx=_t(3 * G + 40)) == -1
+    assert _backward(_cfg(dropout=0.1)) == -1                  # no state
+
+
+def test_python_refusals_without_a_gpu():
+    with pytest.raises(abft.AbftError):
+        abft.LayerNorm(_cfg(dropout=0.1), device="cpu")
+    norm = abft.LayerNorm(_cfg(), device="cpu", training=False)
+    x = torch.zeros((2, 3, 40), dtype=torch.bfloat16)
+    with pytest.raises(abft.AbftError):
+        norm.backward(x, x)
+    with pytest.raises(abft.AbftError):
+        norm.forward(x.float())
+    with pytest.raises(abft.AbftError):
+        norm.forward(x[:, :2])
+    with pytest.raises(abft.AbftError):
+        norm.forward(x, weight=torch.ones(40, dtype=torch.bfloat16))
+    with pytest.raises(abft.AbftError):
+        abft.ResidualNorm(_cfg(dropout=0.1), device="cpu").forward(x, x)     # no state
+    with pytest.raises(abft.AbftError):
+        abft.ResidualNorm(_cfg(), device="cpu").forward(x, None)
+
+
+# ---- GPU -------------------------------------------------------------------------------
+
+def _inputs(cfg, seed, lens=None, mean=0.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    dt, wdt = DT[cfg.dtype], DT[cfg.weight_dtype]
+    shape = (cfg.batch, cfg.tokens, cfg.cols)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda")
+    x, res, dy, dh = (rnd(*shape).to(dt) for _ in range(4))
+    x = (x.float() + mean).to(dt)
+    w, b = (1 + 0.3 * rnd(cfg.cols)).to(wdt), rnd(cfg.cols).to(wdt)
+    lens = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    rng = torch.tensor(RNG, dtype=torch.int64, device="cuda") if cfg.dropout else None
+    return dict(x=x, res=res, dy=dy, dh=dh, w=w, b=b, lens=lens, rng=rng)
+
+
+def _check_grads(cfg, d, got, saved, kept=None):
+    dt = DT[cfg.dtype]
+    want = R.norm_backward(d["dy"], d.get("dh"), saved, dt)
+    g, bound = want["dh"]
+    if "dresidual" in got:
+        R.check("dresidual", got["dresidual"], g, R.stored(g, bound, dt))
+    if kept is not None:             # (the factor's rounding, the product's)
+        s = R.scale(cfg.dropout)
+        g, bound = torch.where(kept, g * s, 0.0), torch.where(kept, (bound + 2 * R.U * g.abs()) * s, 0.0)
+        assert (got["dx"][~kept] == 0).all()
+    R.check("dx", got["dx"], g, R.stored(g, bound, dt))
+    for name in ("dweight", "dbias"):
+        R.check(name, got[name], *want[name])
+
+
+def _check_norm(cfg, seed, lens=None, mean=0.0, change=None):
+    print(f"[case] norm {cfg} {lens}", flush=True)
+    d = _inputs(cfg, seed, lens, mean)
+    if change:
+        change(d)
+    d.pop("dh")
+    op = abft.LayerNorm(cfg)
+    op.workspace.fill_(255)        # (NaN patterns: nothing may come from there)
+    y = op.forward(d["x"], d["w"], d["b"], lens=d["lens"])
+    dx, dw, db = op.backward(d["dy"], d["x"], d["w"], lens=d["lens"])
+    want, bound, saved = R.norm(d["x"], d["w"], d["b"], cfg.eps, d["lens"], DT[cfg.dtype])
+    R.check("y", y, want, bound)
+    _check_grads(cfg, d, dict(dx=dx, dweight=dw, dbias=db), saved)
+    return d, y, dx, dw, db
+
+
+# on, one below and one above the widths where the kernels' shapes change
+WIDTHS = [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 130, 255, 257, 511, 512, 515, 767, 768, 769, 1001, 1024,
+          1025, 1530, 2048, 2049, 4095, 4096, 4099, 5120, 8192, 8201, 12289, 16383, 16384]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("dtype,weight_dtype", [("bf16", "f32"), ("f32", "bf16")])
+def test_widths(cols, dtype, weight_dtype):
+    _check_norm(abft.NormConfig(3, 7, cols, dtype=dtype, weight_dtype=weight_dtype), cols)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,tokens", [(1, 1), (1, 2), (64, 1), (1, 5000), (7, 301), (3, 33)])
+@pytest.mark.parametrize("cols", [48, 768, 1001])
+def test_row_counts(batch, tokens, cols):
+    _check_norm(abft.NormConfig(batch, tokens, cols, weight_dtype="bf16"), 3)
+    _check_norm(abft.NormConfig(batch, tokens, cols, dtype="f32"), 4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[5, 0, 9, 3], [0, 0, 0, 0], [9, 9, 9, 9], [-3, 100, 1, 9]])
+@pytest.mark.parametrize("cols", [24, 640, 3000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_behind_a_sequence(lens, cols, dtype):
+    """Not read, whatever they hold; results are 0 there."""
+    def junk(d):
+        for b, n in enumerate(lens):
+            for t in ("x", "dy"):
+                d[t][b, max(0, n):] = math.nan
+                d[t][b, max(0, n):, ::2] = math.inf
+    cfg = abft.NormConfig(4, 9, cols, dtype=dtype)
+    d, y, dx, dw, db = _check_norm(cfg, 5, [min(9, max(0, n)) for n in lens], change=junk)
+    op = abft.LayerNorm(cfg)       # lengths out of range are taken into it
+    raw = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    assert torch.equal(op.forward(d["x"], d["w"], d["b"], lens=raw), y)
+    again = op.backward(d["dy"], d["x"], d["w"], lens=raw)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dw, db)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [40, 768, 5120])
+def test_without_parameters_and_results_left_out(dtype, cols):
+    cfg = abft.NormConfig(2, 5, cols, dtype=dtype)
+    d = _inputs(cfg, 6)
+    op = abft.LayerNorm(cfg)
+    y = op.forward(d["x"])
+    want, bound, saved = R.norm(d["x"], None, None, cfg.eps, None, DT[dtype])
+    R.check("y", y, want, bound)
+    dx, dw, db = op.backward(d["dy"], d["x"])
+    _check_grads(cfg, dict(dy=d["dy"]), dict(dx=dx, dweight=dw, dbias=db), saved)
+    # any result alone, through the C call
+    rows = lambda t: ctypes.byref(abft.Rows(t.data_ptr(), t.stride(0), t.stride(1)))
+    for k in range(4):
+        out = [torch.full_like(t, 7.0) for t in (dx, dx, dw, db)]
+        args = [rows(out[0]), rows(out[1]), out[2].data_ptr(), out[3].data_ptr()]
+        args = [a if i == k else None for i, a in enumerate(args)]
+        ws = op.workspace if k > 1 else None
+        st = abft._lib.attn_norm_backward(cfg.to_c(), rows(d["dy"]), None, rows(d["x"]), None,
+                                          op.stats.data_ptr(), None, None, *args,
+                                          ws.data_ptr() if k > 1 else None,
+                                          ws.numel() if k > 1 else 0,
+                                          torch.cuda.current_stream().cuda_stream)
+        assert st == 0 and torch.equal(out[k], (dx, dx, dw, db)[k])
+        assert all((o == 7.0).all() for i, o in enumerate(out) if i != k)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [5, 64, 129, 768, 2000])
+def test_strides_and_alignment(dtype, cols):
+    """Views with gaps between rows and sequences, at odd elements; what lies between
+    the rows of a result stays as it is."""
+    cfg = abft.NormConfig(3, 4, cols, dtype=dtype)
+    d = _inputs(cfg, 8)
+    op = abft.LayerNorm(cfg)
+    y0 = op.forward(d["x"], d["w"], d["b"])
+    want = op.backward(d["dy"], d["x"], d["w"])
+
+    def view(t, swap):
+        """A copy of t with cols + 3 (and, exchanged, sequences inside tokens)."""
+        shape = (5, 6, cols + 3) if not swap else (6, 5, cols + 3)
+        big = torch.full((1 + math.prod(shape),), 3.0, dtype=t.dtype, device="cuda")[1:].view(shape)
+        v = big[:3, 1:5, 2:2 + cols] if not swap else big.transpose(0, 1)[:3, 1:5, 2:2 + cols]
+        v.copy_(t)
+        return big, v
+    for swap in (False, True):
+        x, dy = view(d["x"], swap)[1], view(d["dy"], not swap)[1]
+        (by, y), (bx, dx) = view(torch.zeros_like(y0), swap), view(torch.zeros_like(y0), not swap)
+        op.forward(x, d["w"], d["b"], y=y)
+        _, dw, db = op.backward(dy, x, d["w"], dx=dx)
+        assert torch.equal(y, y0)
+        assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), want))
+        for big, v in ((by, y), (bx, dx)):
+            v.fill_(3.0)
+            assert (big == 3.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [8, 100, 768, 1025, 16000])
+@pytest.mark.parametrize("value", [0.0, 1.0, 1000.0, -3e4])
+def test_rows_of_one_value(cols, value):
+    """Variance 0: y is the offset (the mean's rounding does not pass for a
+    difference), and the gradient is that of deviation sqrt(eps)."""
+    for dtype in ("bf16", "f32"):
+        cfg = abft.NormConfig(1, 3, cols, dtype=dtype)
+        d = _inputs(cfg, 9)
+        x = torch.full_like(d["x"], value)
+        op = abft.LayerNorm(cfg)
+        assert torch.equal(op.forward(x, d["w"], d["b"]), d["b"].to(x.dtype).expand_as(x).contiguous())
+        assert torch.isfinite(op.backward(d["dy"], x, d["w"])[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [33, 768, 3001])
+@pytest.mark.parametrize("size", [1e-18, 1e10, 1e18, 1e25, 1e30, 1e37])
+def test_extreme_rows(cols, size):
+    """Squares outside of fp32's range: within the same bounds."""
+    for dtype in ("bf16", "f32"):
+        cfg = abft.NormConfig(2, 3, cols, dtype=dtype, eps=1e-30)
+        d = _inputs(cfg, 10)
+        x = (d["x"].float() * size).to(d["x"].dtype)
+        op = abft.LayerNorm(cfg)
+        y = op.forward(x, d["w"], d["b"])
+        want, bound, saved = R.norm(x, d["w"], d["b"], cfg.eps, None, DT[dtype])
+        R.check("y", y, want, bound)
+        dx, dw, db = op.backward(d["dy"], x, d["w"])
+        grads = R.norm_backward(d["dy"], None, saved, DT[dtype])
+        R.check("dweight", dw, *grads["dweight"])
+        # one element near the largest: the others are lost beside it, as they should
+        x = d["x"].clone()
+        x[1, 2, cols // 2] = size
+        want, bound, _ = R.norm(x, d["w"], d["b"], cfg.eps, None, DT[dtype])
+        R.check("y", op.forward(x, d["w"], d["b"]), want, bound)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("cols", [24, 768, 4097])
+def test_values_that_are_not_finite_stay_in_their_row(bad, cols):
+    cfg = abft.NormConfig(2, 9, cols)
+    d = _inputs(cfg, 11)
+    op = abft.LayerNorm(cfg)
+    y0 = op.forward(d["x"], d["w"], d["b"])
+    dx0, _, _ = op.backward(d["dy"], d["x"], d["w"])
+    x = d["x"].clone()
+    x[1, 4, cols - 1] = bad
+    y = op.forward(x, d["w"], d["b"])
+    dx, dw, db = op.backward(d["dy"], x, d["w"])
+    rest = torch.ones((2, 9), dtype=torch.bool, device="cuda")
+    rest[1, 4] = False
+    assert y[1, 4].isnan().all() and dx[1, 4].isnan().all() and dw.isnan().all()
+    assert torch.equal(y[rest], y0[rest]) and torch.equal(dx[rest], dx0[rest])
+    assert torch.isfinite(db).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_means(dtype):
+    """Rows whose mean is 300 deviations: the bound carries the mean's rounding."""
+    for cols in (64, 768, 5000):
+        _check_norm(abft.NormConfig(2, 5, cols, dtype=dtype), 12, mean=300.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [16, 129, 768, 1600])
+def test_gradients_against_differences(cols):
+    """d(sum of dy y) along a direction v, from differences of the definition in 64
+    bits at steps of 1e-6: their error is 1e-10 of third derivatives (below 1e3 here),
+    and the kernel's sums lie within the bounds in fp32."""
+    cfg = abft.NormConfig(2, 3, cols, dtype="f32")
+    d = _inputs(cfg, 13)
+    op = abft.LayerNorm(cfg)
+    op.forward(d["x"], d["w"], d["b"])
+    dx, dw, db = op.backward(d["dy"], d["x"], d["w"])
+
+    def loss(x, w, b):
+        x = x - x.mean(dim=2, keepdim=True)
+        return (d["dy"].double() * (x / (x.square().mean(dim=2, keepdim=True) + cfg.eps).sqrt() * w + b)).sum()
+    at = [d[k].double() for k in ("x", "w", "b")]
+    for k, grad in enumerate((dx, dw, db)):
+        v = torch.randn_like(at[k])
+        up, down = ([a + s * 1e-6 * v if i == k else a for i, a in enumerate(at)] for s in (1, -1))
+        want = (loss(*up) - loss(*down)) / 2e-6
+        assert abs((grad.double() * v).sum() - want) <= 1e-4 * (grad.double() * v).norm()
+
+
+# ---- with a residual and dropout ----------------------------------------------------
+
+def _residual(cfg, d):
+    kept = None
+    x = d["x"].float()
+    if cfg.dropout:
+        kept = R.keep(d["x"].shape, cfg.dropout, RNG, cfg.site)
+        x = R.dropped(d["x"], kept, cfg.dropout)
+    return (d["res"].float() + x).to(d["x"].dtype), kept
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 1.0])
+@pytest.mark.parametrize("cols", [8, 63, 200, 768, 1001, 4096, 16384])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_residual_norm(p, cols, dtype):
+    cfg = abft.NormConfig(3, 11, cols, dtype=dtype, dropout=p, site=9)
+    print(f"[case] residual norm {cfg}", flush=True)
+    lens = [11, 0, 6]
+    d = _inputs(cfg, 20, lens)
+    op = abft.ResidualNorm(cfg)
+    op.workspace.fill_(255)
+    h, y = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"], lens=d["lens"])
+    want_h, kept = _residual(cfg, d)
+    ok = R.valid_rows(d["x"].shape, d["lens"])
+    assert torch.equal(h, torch.where(ok, want_h, torch.zeros_like(want_h)))   # to the bit
+    want, bound, saved = R.norm(h, d["w"], d["b"], cfg.eps, d["lens"], DT[dtype])
+    R.check("y", y, want, bound)
+    dx, dr, dw, db = op.backward(d["dy"], h, d["w"], dh=d["dh"], rng=d["rng"], lens=d["lens"])
+    _check_grads(cfg, d, dict(dx=dx, dresidual=dr, dweight=dw, dbias=db), saved, kept)
+    d.pop("dh")
+    dx, dr, dw, db = op.backward(d["dy"], h, d["w"], rng=d["rng"], lens=d["lens"])
+    _check_grads(cfg, d, dict(dx=dx, dresidual=dr, dweight=dw, dbias=db), saved, kept)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("cols", [40, 64, 500, 768, 1500, 3500, 16384])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_same_bits_as_the_two_calls(p, cols, dtype):
+    cfg = abft.NormConfig(2, 9, cols, dtype=dtype, dropout=p, site=3)
+    d = _inputs(cfg, 21)
+    h, y = abft.ResidualNorm(cfg).forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
+    drop = abft.Dropout(abft.DropoutConfig(2, 9, cols, dtype=dtype, p=p, site=3))
+    h2 = drop.forward(d["x"], d["rng"], residual=d["res"])
+    norm = abft.LayerNorm(abft.NormConfig(2, 9, cols, dtype=dtype))
+    assert torch.equal(h, h2) and torch.equal(y, norm.forward(h2, d["w"], d["b"]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [72, 768, 2500])
+def test_in_place(dtype, cols):
+    cfg = abft.NormConfig(3, 50, cols, dtype=dtype, dropout=0.2)
+    d = _inputs(cfg, 22)
+    op = abft.ResidualNorm(cfg)
+    h, y = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
+    want = op.backward(d["dy"], h, d["w"], dh=d["dh"], rng=d["rng"])
+    x, res, dy, dh = (d[k].clone() for k in ("x", "res", "dy", "dh"))
+    h1, y1 = op.forward(x, res, d["w"], d["b"], rng=d["rng"], h=res, y=x)
+    assert h1 is res and torch.equal(res, h) and torch.equal(x, y)
+    got = op.backward(dy, res, d["w"], dh=dh, rng=d["rng"], dx=dy, dresidual=dh)
+    assert got[0] is dy and all(torch.equal(a, b) for a, b in zip(got, want))
+    x, res = d["x"].clone(), d["res"].clone()
+    op.forward(x, res, d["w"], d["b"], rng=d["rng"], h=x, y=res)
+    assert torch.equal(x, h) and torch.equal(res, y)
+
+
+@pytest.mark.gpu
+def test_a_residual_that_repeats():
+    """One row, or one sequence, for the whole batch (an embedding of positions)."""
+    cfg = abft.NormConfig(4, 6, 100, dropout=0.25)
+    d = _inputs(cfg, 23)
+    op = abft.ResidualNorm(cfg)
+    for part in (d["res"][:1].expand(4, 6, 100), d["res"][:1, :1].expand(4, 6, 100),
+                 d["res"][:, :1].expand(4, 6, 100)):
+        h, y = op.forward(d["x"], part, d["w"], d["b"], rng=d["rng"])
+        h2, y2 = op.forward(d["x"], part.contiguous(), d["w"], d["b"], rng=d["rng"])
+        assert torch.equal(h, h2) and torch.equal(y, y2)
+        assert h.is_contiguous()
+
+
+@pytest.mark.gpu
+def test_serving_without_statistics_or_sum():
+    cfg = abft.NormConfig(32, 1, 4096, weight_dtype="bf16")
+    d = _inputs(cfg, 24)
+    h, y = abft.ResidualNorm(cfg).forward(d["x"], d["res"], d["w"], d["b"])
+    op = abft.ResidualNorm(cfg, training=False)
+    h2, y2 = op.forward(d["x"], d["res"], d["w"], d["b"])
+    assert op.workspace is None and op.stats is None
+    assert torch.equal(h, h2) and torch.equal(y, y2)
+    y3 = torch.empty_like(y)       # the C call without h
+    rows = lambda t: ctypes.byref(abft.Rows(t.data_ptr(), t.stride(0), t.stride(1)))
+    assert abft._lib.attn_norm_forward(cfg.to_c(), rows(d["x"]), rows(d["res"]), d["w"].data_ptr(),
+                                       d["b"].data_ptr(), None, None, None, rows(y3), None,
+                                       torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(y, y3)
+    with pytest.raises(abft.AbftError):
+        op.backward(d["dy"], h, d["w"])
+
+
+@pytest.mark.gpu
+def test_records():
+    """A backward of rows that are not the last forward's is refused; records keep
+    several forwards apart."""
+    cfg = abft.NormConfig(2, 3, 64)
+    d, e = _inputs(cfg, 25), _inputs(cfg, 26)
+    op = abft.LayerNorm(cfg)
+    with pytest.raises(abft.AbftError):
+        op.backward(d["dy"], d["x"], d["w"])
+    op.forward(d["x"], d["w"], d["b"])
+    want = op.backward(d["dy"], d["x"], d["w"])
+    one, two = op.new_saved(), op.new_saved()
+    with pytest.raises(abft.AbftError):
+        op.backward(d["dy"], d["x"], d["w"], saved=one)
+    op.forward(d["x"], d["w"], d["b"], saved=one)
+    op.forward(e["x"], d["w"], d["b"], saved=two)
+    op.forward(e["x"], d["w"], d["b"])
+    with pytest.raises(abft.AbftError):
+        op.backward(d["dy"], d["x"], d["w"])
+    got = op.backward(d["dy"], d["x"], d["w"], saved=one)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(abft.AbftError):
+        op.forward(d["x"], saved=abft.LayerNorm(abft.NormConfig(2, 4, 64)).new_saved())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [64, 768, 5120])
+def test_runs_repeat_and_captured_calls_replay(cols):
+    """A captured step draws anew once its state has advanced, and leaves what the
+    eager calls leave."""
+    cfg = abft.NormConfig(4, 130, cols, dropout=0.1)
+    d = _inputs(cfg, 27)
+    op = abft.ResidualNorm(cfg)
+
+    def step(out):
+        h, y = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"], h=out[0], y=out[1])
+        op.backward(d["dy"], h, d["w"], dh=d["dh"], rng=d["rng"], dx=out[2], dresidual=out[3],
+                    dweight=out[4], dbias=out[5])
+    new = lambda: [torch.empty_like(d["x"]) for _ in range(4)] + [torch.empty(cols, device="cuda")
+                                                                  for _ in range(2)]
+    out, eager = new(), new()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(out)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    last = None
+    for k in range(4):
+        d["rng"][1] += 1
+        d["dy"].copy_(torch.randn_like(d["dy"]))
+        step(eager)
+        step(again := new())
+        for o in out:
+            o.fill_(math.nan)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager))
+        assert all(torch.equal(a, b) for a, b in zip(again, eager))
+        assert last is None or not torch.equal(last, out[0])
+        last = out[0].clone()
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    """Calls that share neither workspace nor outputs may overlap."""
+    cfg = abft.NormConfig(8, 512, 768)
+    d = _inputs(cfg, 28)
+    ops = [abft.LayerNorm(cfg) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in ops]
+    want = [ops[0].forward(d["x"], d["w"], d["b"]), *ops[0].backward(d["dy"], d["x"], d["w"])]
+    got = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for k, (op, s) in enumerate(zip(ops, streams)):
+            with torch.cuda.stream(s):
+                got[k] = [op.forward(d["x"], d["w"], d["b"]), *op.backward(d["dy"], d["x"], d["w"])]
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(got[k], want))
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """Rows of one buffer further than 2^32 bytes apart."""
+    cfg = abft.NormConfig(2, 3, 768, dropout=0.5)
+    d = _inputs(cfg, 29)
+    op = abft.ResidualNorm(cfg)
+    h0, y0 = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
+    want = op.backward(d["dy"], h0, d["w"], dh=d["dh"], rng=d["rng"])
+    big = torch.zeros(5 * 2 ** 30, dtype=torch.bfloat16, device="cuda")   # 10 GiB
+
+    def far(t, at):
+        v = big.as_strided((2, 3, 768), (2 ** 31 + 4096, 2 ** 20, 1), at)
+        if t is not None:
+            v.copy_(t)
+        return v
+    x, res, h, y = far(d["x"], 0), far(d["res"], 768), far(None, 2 * 768), far(None, 3 * 768)
+    op.forward(x, res, d["w"], d["b"], rng=d["rng"], h=h, y=y)
+    assert torch.equal(h, h0) and torch.equal(y, y0)
+    dx, dr = far(None, 4 * 768), far(None, 5 * 768)
+    got = op.backward(far(d["dy"], 6 * 768), h, d["w"], dh=far(d["dh"], 7 * 768), rng=d["rng"], dx=dx,
+                      dresidual=dr)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,most", [("bf16", 2.0 ** -8 / math.sqrt(3)), ("f32", 2.0 ** -21)])
+def test_accuracy_over_whole_tensors(dtype, most):
+    """Relative norms: in bf16 a rounding of at most 2^-8, evenly spread, and nothing
+    beside it; in fp32 eight roundings of at most 2^-24. Parameter gradients are fp32
+    sums of 4000 terms in either."""
+    cfg = abft.NormConfig(4, 1000, 768, dtype=dtype, dropout=0.1)
+    d = _inputs(cfg, 30)
+    op = abft.ResidualNorm(cfg)
+    h, y = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
+    want, _, saved = R.norm(h, d["w"], d["b"], cfg.eps, None, DT[dtype])
+    grads = R.norm_backward(d["dy"], d["dh"], saved, DT[dtype])
+    dx, dr, dw, db = op.backward(d["dy"], h, d["w"], dh=d["dh"], rng=d["rng"])
+    for got, ref, top in ((y, want, most), (dr, grads["dh"][0], most),
+                          (dw, grads["dweight"][0], 2.0 ** -21), (db, grads["dbias"][0], 2.0 ** -21)):
+        assert (got.double() - ref).norm() <= top * ref.norm()
