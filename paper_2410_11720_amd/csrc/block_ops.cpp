@@ -108,6 +108,7 @@ int take_drop(double p, uint32_t site, const uint64_t* rng, DropArgs* d) {
   if (!(p >= 0.0 && p <= 1.0) || site >= MAX_SITE) return ABFT_ERR_INVALID;
   d->threshold = uint32_t(std::floor(65536.0 * p + 0.5));
   d->scale = d->threshold < 65536 ? float(65536.0 / (65536.0 - d->threshold)) : 0.f;
+  d->last = uint32_t((uint64_t(d->threshold) << 16) - 1);
   d->site = site;
   d->rng = rng;
   if (d->threshold && (!rng || reinterpret_cast<uintptr_t>(rng) % 8)) return ABFT_ERR_INVALID;
@@ -141,6 +142,20 @@ int common(const attn_norm_config* c, const void* weight, const void* bias, cons
   a->tokens = Divisor::of(std::max(1, c->tokens));
   a->eps = c->eps;
   return ABFT_OK;
+}
+
+// Whether the kernels for rows of whole chunks take these tensors.
+bool lines_ok(const NormArgs& a, const Operand* rows, int n, int es) {
+  if (a.cols % 8 || a.rows >= (1 << 28)) return false;
+  for (int i = 0; i < n; ++i) {
+    if (!rows[i].p) continue;
+    if (reinterpret_cast<uintptr_t>(rows[i].p) % 16 || rows[i].st[0] % 16 || rows[i].st[1] % 16)
+      return false;
+    // (rows of less than a wave's width: 32-bit offsets from the tensor's start)
+    const int64_t bytes = int64_t(rows[i].area.end - rows[i].area.at);
+    if (a.cols <= NORM_LINE_COLS && bytes > 0x7fffff00) return false;
+  }
+  return a.cols * es % 16 == 0;
 }
 
 int valid_rotary(const attn_rotary_config* c) {
@@ -265,6 +280,8 @@ int attn_norm_forward(const attn_norm_config* cfg, const attn_rows* x, const att
   if (written_overlap(mem, 3, 2, 9)) return ABFT_ERR_INVALID;
   if (a.rows == 0) return ABFT_OK;
   a.stats = reinterpret_cast<float2*>(stats);
+  const Operand rows[] = {mem[0], mem[1], mem[3], mem[4]};
+  a.lines = lines_ok(a, rows, 4, es_of(dt));
   TRY(check_device());
   CK(launch_norm_fwd(a, dt, a.drop.threshold ? NORM_DROPOUT : sum ? NORM_RESIDUAL : NORM_ALONE,
                      static_cast<hipStream_t>(stream)));
@@ -308,6 +325,8 @@ int attn_norm_backward(const attn_norm_config* cfg, const attn_rows* dy, const a
   a.part = static_cast<float*>(workspace);
   a.stride = norm_part_stride(H);
   if (a.rows == 0 && !grads) return ABFT_OK;
+  const Operand rows[] = {mem[0], mem[1], mem[5], mem[6], mem[7]};
+  a.lines = a.rows > 0 && lines_ok(a, rows, 5, es_of(dt));
   TRY(check_device());
   const bool sum = a.dres.p || a.dh.p;
   CK(launch_norm_bwd(a, dt, a.drop.threshold ? NORM_DROPOUT : sum ? NORM_RESIDUAL : NORM_ALONE,

@@ -12,168 +12,202 @@
 namespace abft {
 namespace {
 
-constexpr int MAX_WGS = 512;
+// A row as it is read.
+template <typename T, typename S, int KIND, bool LINES> struct BwdLine {
+  Chunk<T> dy[S::NV], h[S::NV], dh[KIND == NORM_ALONE ? 1 : S::NV];
+  float2 st;
 
-template <typename T, typename S, int KIND>
-__global__ __launch_bounds__(S::NT) void norm_bwd_kernel(NormArgs a) {
-#pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
-  constexpr int LPR = S::LPR, NV = S::NV, R = S::R;
-  __shared__ float2 sh[LPR > 64 ? 2 * LPR / 64 : 1];
-  __shared__ float4 sums[R > 1 ? S::NT * NV * 2 : 1];
-  const int lane = threadIdx.x % LPR;
-  int turn = 0;
-  float w[NV][8], dw[NV][8], db[NV][8];
+  __device__ __forceinline__ void read(const NormArgs& a, const Place<T, S>& p, int row) {
+    const int in = min(row, a.rows - 1);
+    const RowAt at = row_at(a.tokens, in);
+    const bool ok = row < a.rows && (!a.lens || int(at.t) < a.lens[at.b]);
+    const Line<T, S, LINES> pg(a.dy, at, ok, a.cols), ph(a.h, at, ok, a.cols), pd(a.dh, at, ok, a.cols);
+    st = a.stats[in];
+    // (a row that is not read has 0 in dy, dh and h; its statistics may be any row's)
+    st.x = ok ? st.x : 0.f;
+    st.y = ok ? st.y : 0.f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int col = 8 * (lane + j * LPR);
-    load_params(w[j], a.weight, a.weight_bf16, col, a.cols - col, 1.f);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) dw[j][e] = db[j][e] = 0.f;
+    for (int j = 0; j < S::NV; ++j) {
+      pg.load(dy[j], p, j);
+      ph.load(h[j], p, j);
+      if constexpr (KIND != NORM_ALONE) pd.load(dh[j], p, j);
+    }
   }
+};
+
+// The row after the present one is read ahead.
+template <typename T, typename S, int KIND, bool LINES>
+__global__ __launch_bounds__(S::LPR ? 256 : 1024) void norm_bwd_kernel(NormArgs a, ShapeAt shape) {
+#pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
+  constexpr int NV = S::NV;
+  __shared__ float2 sh[2][16];
+  extern __shared__ float4 sums[];   // [rows][lanes NV][2] where there are several rows
+  const Place<T, S> p(shape.lanes, a.cols);
+  const int waves = shape.lanes / 64;
+  const int step = gridDim.x * shape.rows;
+  int row = blockIdx.x * shape.rows + p.slot, turn = 0;
+  BwdLine<T, S, KIND, LINES> cur, next;
+  if (a.rows > 0) cur.read(a, p, row);
   uint64_t seed = 0, offset = 0;
   if constexpr (KIND == NORM_DROPOUT) {
     seed = a.drop.rng[0];
     offset = a.drop.rng[1];
   }
-  const float inv_n = 1.f / float(a.cols);
-  const int step = gridDim.x * R;
-  for (int row = blockIdx.x * R + threadIdx.x / LPR; row < a.rows; row += step) {
-    RowAt at;
-    at.b = a.tokens.quotient(row);
-    at.t = row - at.b * a.tokens.d;
-    T* dx = a.dx.p ? row_of<T>(a.dx, at) : nullptr;
-    T* dres = a.dres.p ? row_of<T>(a.dres, at) : nullptr;
-    if (a.lens && int(at.t) >= a.lens[at.b]) {
-      Chunk<T> zero;
-      zero.clear();
+  float w[NV][8], dw[NV][8], db[NV][8];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int col = 8 * (lane + j * LPR);
-        if (dx) store_chunk(zero, dx + col, a.cols - col);
-        if (KIND != NORM_ALONE && dres) store_chunk(zero, dres + col, a.cols - col);
-      }
-      continue;
-    }
-    const float2 st = a.stats[row];
+  for (int j = 0; j < NV; ++j) {
+    const int col = p.col(j);
+    load_params(w[j], a.weight, a.weight_bf16, col, a.cols - col, 1.f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[j][e] = db[j][e] = 0.f;
+  }
+  const float inv_n = 1.f / float(a.cols);
+  // (the workgroup's waves take as many turns: they meet in the sums)
+  for (int first = blockIdx.x * shape.rows; first < a.rows; first += step, row += step, cur = next) {
+    next.read(a, p, row + step);
+    const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
+    const Line<T, S, LINES> px(a.dx, at, row < a.rows, a.cols);
+    const Line<T, S, LINES> pr(a.dres, at, row < a.rows, a.cols);
+    const float mean = cur.st.x, r = cur.st.y;
     float g[NV][8], xh[NV][8];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int col = 8 * (lane + j * LPR), m = a.cols - col;
-      Chunk<T> c, ch;
-      load_chunk(c, row_of<T>(a.dy, at) + col, m);
-      load_chunk(ch, row_of<T>(a.h, at) + col, m);
+    for (int j = 0; j < NV; ++j)
+      // (what is not in the row is 0 in dy)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = c.get(e);
-        xh[j][e] = (ch.get(e) - st.x) * st.y;
+        const float d = cur.dy[j].get(e);
+        xh[j][e] = (cur.h[j].get(e) - mean) * r;
         g[j][e] = d * w[j][e];
         dw[j][e] = fmaf(d, xh[j][e], dw[j][e]);
         db[j][e] += d;
         s.x += g[j][e];
         s.y = fmaf(g[j][e], xh[j][e], s.y);
       }
-    }
-    s = row_sum<LPR>(s, sh, turn);
+    s = line_sum<S>(s, sh, waves, p.slot, turn);
     const float c1 = s.x * inv_n, c2 = s.y * inv_n;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = 8 * (lane + j * LPR), m = a.cols - col;
       float o[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = st.y * fmaf(-xh[j][e], c2, g[j][e] - c1);
+      for (int e = 0; e < 8; ++e) {
+        o[e] = r * fmaf(-xh[j][e], c2, g[j][e] - c1);
+        if constexpr (KIND != NORM_ALONE) o[e] += cur.dh[j].get(e);
+      }
       Chunk<T> c;
       if constexpr (KIND != NORM_ALONE) {
-        if (a.dh.p) {
-          load_chunk(c, row_of<T>(a.dh, at) + col, m);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += c.get(e);
-        }
-        if (dres) {
-          c.set(o);
-          store_chunk(c, dres + col, m);
-        }
-        if constexpr (KIND == NORM_DROPOUT) drop(o, a.drop, seed, offset, row, lane + j * LPR);
-      }
-      if (dx) {
         c.set(o);
-        store_chunk(c, dx + col, m);
+        pr.store(c, p, j);
       }
+      if constexpr (KIND == NORM_DROPOUT)
+        drop(o, a.drop, seed, offset, row, p.lane + j * p.lanes);
+      if constexpr (KIND != NORM_RESIDUAL) c.set(o);
+      px.store(c, p, j);
     }
   }
   if (!a.dweight && !a.dbias) return;
-  // the workgroup's sums: over its R rows at a time, in their order
+  // the workgroup's sums: over its rows at a time, in their order
   float* out = a.part + int64_t(blockIdx.x) * a.stride;
+  const int padded = norm_padded(a.cols);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     float(&v)[NV][8] = k ? db : dw;
-    if constexpr (R > 1) {
-      if (k) __syncthreads();
-      float4* my = sums + (threadIdx.x / LPR) * (LPR * NV * 2);
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        my[2 * (lane + j * LPR)] = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
-        my[2 * (lane + j * LPR) + 1] = make_float4(v[j][4], v[j][5], v[j][6], v[j][7]);
-      }
-      __syncthreads();
-      const float* f = reinterpret_cast<const float*>(sums);
-      for (int c = threadIdx.x; c < a.cols; c += S::NT) {
-        float t = f[c];
-        for (int q = 1; q < R; ++q) t += f[q * (LPR * NV * 8) + c];
-        out[k * a.cols + c] = t;
-      }
-    } else {
+    if (shape.rows == 1) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = 8 * (lane + j * LPR) + e;
-          if (c < a.cols) out[k * a.cols + c] = v[j][e];
+        if (p.has(j)) {
+          float4* to = reinterpret_cast<float4*>(out + k * padded) + 2 * (p.lane + j * p.lanes);
+          to[0] = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
+          to[1] = make_float4(v[j][4], v[j][5], v[j][6], v[j][7]);
         }
+      continue;
+    }
+    if (k) __syncthreads();
+    const int width = p.lanes * NV * 2;   // (of four columns)
+    float4* my = sums + p.slot * width;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      my[2 * (p.lane + j * p.lanes)] = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
+      my[2 * (p.lane + j * p.lanes) + 1] = make_float4(v[j][4], v[j][5], v[j][6], v[j][7]);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < padded / 4; c += blockDim.x) {
+      float4 t = sums[c];
+      for (int q = 1; q < shape.rows; ++q) {
+        const float4 x = sums[q * width + c];
+        t = make_float4(t.x + x.x, t.y + x.y, t.z + x.z, t.w + x.w);
+      }
+      reinterpret_cast<float4*>(out + k * padded)[c] = t;
     }
   }
 }
 
-// dweight and dbias from the workgroups' sums: 64 columns a workgroup, 16 lanes of
-// four columns, the sums split over 16 such groups.
-__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, int wgs) {
-  __shared__ float4 sh[256];
-  const int c4 = threadIdx.x % 16, k0 = threadIdx.x / 16;
+// dweight and dbias from the workgroups' sums: 32 columns a workgroup, 8 lanes of four
+// columns each, the sums split over 128 such groups: 2 to 8 loads each, all in flight
+// at once, then joined in LDS in their order.
+constexpr int JOIN_NT = 1024, JOIN_COLS = 32, JOIN_GROUPS = JOIN_NT * 4 / JOIN_COLS;
+
+__global__ __launch_bounds__(JOIN_NT) void norm_join_kernel(NormArgs a, int wgs) {
+  __shared__ float sh[JOIN_GROUPS][JOIN_COLS], sh2[16][JOIN_COLS];
+  const int c4 = threadIdx.x % 8, group = threadIdx.x / 8;
   float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float* at = a.part + blockIdx.x * 64 + c4 * 4;
-  for (int k = k0; k < wgs; k += 16) {
+  const float* at = a.part + blockIdx.x * JOIN_COLS + c4 * 4;
+#pragma unroll 4
+  for (int k = group; k < wgs; k += JOIN_GROUPS) {
     const float4 v = *reinterpret_cast<const float4*>(at + int64_t(k) * a.stride);
-    t.x += v.x;
-    t.y += v.y;
-    t.z += v.z;
-    t.w += v.w;
+    t = make_float4(t.x + v.x, t.y + v.y, t.z + v.z, t.w + v.w);
   }
-  sh[threadIdx.x] = t;
+  *reinterpret_cast<float4*>(&sh[group][c4 * 4]) = t;
   __syncthreads();
-  if (threadIdx.x >= 64) return;
-  const int f = blockIdx.x * 64 + threadIdx.x;
-  const float* s = reinterpret_cast<const float*>(sh) + threadIdx.x;
-  float v = s[0];
-  for (int k = 1; k < 16; ++k) v += s[64 * k];
-  if (f < a.cols) {
-    if (a.dweight) a.dweight[f] = v;
-  } else if (f < 2 * a.cols) {
-    if (a.dbias) a.dbias[f - a.cols] = v;
+  const int c = threadIdx.x % JOIN_COLS, q = threadIdx.x / JOIN_COLS;
+  if (q < 16) {
+    float v = sh[8 * q][c];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) v += sh[8 * q + k][c];
+    sh2[q][c] = v;
   }
+  __syncthreads();
+  if (q > 0) return;
+  float v = sh2[0][c];
+#pragma unroll
+  for (int k = 1; k < 16; ++k) v += sh2[k][c];
+  const int f = blockIdx.x * JOIN_COLS + c;
+  const int padded = norm_padded(a.cols);
+  float* to = f < padded ? a.dweight : a.dbias;
+  const int col = f < padded ? f : f - padded;
+  if (to && col < a.cols) to[col] = v;
 }
 
-template <typename S> int wgs_of(int64_t rows) {
-  return int(std::max<int64_t>(1, std::min<int64_t>(MAX_WGS, (rows + S::R - 1) / S::R)));
+// f(shape, its lanes and rows) for rows of whole chunks.
+template <typename F> auto with_lines(int chunks, F f) {
+  if (chunks <= 8) return f(Shape<8, 1>(), ShapeAt{8, 32});
+  if (chunks <= 16) return f(Shape<16, 1>(), ShapeAt{16, 16});
+  if (chunks <= 32) return f(Shape<32, 1>(), ShapeAt{32, 8});
+  if (chunks <= 64) return f(Shape<32, 2>(), ShapeAt{32, 8});
+  if (chunks <= 96) return f(Shape<32, 3>(), ShapeAt{32, 8});
+  const int waves = (chunks + 63) / 64;
+  if (waves <= 16) return f(Shape<0, 1>(), ShapeAt{64 * waves, std::max(1, 8 / waves)});
+  return f(Shape<0, 2>(), ShapeAt{64 * ((chunks + 127) / 128), 1});
+}
+
+// Workgroups: as many as two waves a SIMD make, since each leaves sums of its own.
+int wgs_of(ShapeAt at, int64_t rows) {
+  const int64_t most = std::max(256, 2048 / (at.threads() / 64));
+  return int(std::max<int64_t>(1, std::min<int64_t>(most, (rows + at.rows - 1) / at.rows)));
 }
 
 template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t s) {
-  return with_shape((a.cols + 7) / 8, [&](auto shape) {
+  return with_lines((a.cols + 7) / 8, [&](auto shape, ShapeAt at) {
     using S = decltype(shape);
-    const int grid = wgs_of<S>(a.rows);
-    norm_bwd_kernel<T, S, KIND><<<dim3(grid), S::NT, 0, s>>>(a);
+    const int grid = wgs_of(at, a.rows);
+    const size_t lds = at.rows > 1 ? size_t(at.threads()) * S::NV * 32 : 0;
+    if (a.lines)
+      norm_bwd_kernel<T, S, KIND, true><<<dim3(grid), at.threads(), lds, s>>>(a, at);
+    else
+      norm_bwd_kernel<T, S, KIND, false><<<dim3(grid), at.threads(), lds, s>>>(a, at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
-    norm_join_kernel<<<dim3(a.stride / 64), 256, 0, s>>>(a, grid);
+    norm_join_kernel<<<dim3(a.stride / JOIN_COLS), JOIN_NT, 0, s>>>(a, grid);
     return hipGetLastError();
   });
 }
@@ -187,7 +221,7 @@ template <typename T> hipError_t launch(const NormArgs& a, NormKind kind, hipStr
 }  // namespace
 
 int norm_bwd_wgs(int64_t rows, int cols) {
-  return with_shape((cols + 7) / 8, [&](auto shape) { return wgs_of<decltype(shape)>(rows); });
+  return with_lines((cols + 7) / 8, [&](auto, ShapeAt at) { return wgs_of(at, rows); });
 }
 
 hipError_t launch_norm_bwd(const NormArgs& a, int dtype, NormKind kind, hipStream_t s) {

@@ -3,131 +3,163 @@
 //   h = round(residual + dropout(x)) (or x), y = (h - mean) / sqrt(var + eps) w + b
 // A row is held in the registers of LPR lanes from its one reading to its one
 // writing; mean and variance are two sums over them. Bound by memory.
+#include <algorithm>
+
 #include "rows.hpp"
 
 namespace abft {
 namespace {
 
-template <typename T, typename S, int KIND>
-__global__ __launch_bounds__(S::NT) void norm_fwd_kernel(NormArgs a) {
-#pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
-  constexpr int LPR = S::LPR, NV = S::NV;
-  __shared__ float2 sh[LPR > 64 ? 2 * LPR / 64 : 1];
-  const int lane = threadIdx.x % LPR;
-  int turn = 0;
-  float w[NV][8], bias[NV][8];
+// A row as it is read.
+template <typename T, typename S, int KIND, bool LINES> struct FwdLine {
+  Chunk<T> x[S::NV], res[KIND == NORM_ALONE ? 1 : S::NV];
+  bool ok;
+
+  __device__ __forceinline__ void read(const NormArgs& a, const Place<T, S>& p, int row) {
+    const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
+    ok = row < a.rows && (!a.lens || int(at.t) < a.lens[at.b]);
+    const Line<T, S, LINES> px(a.x, at, ok, a.cols), pr(a.res, at, ok, a.cols);
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int col = 8 * (lane + j * LPR);
-    load_params(w[j], a.weight, a.weight_bf16, col, a.cols - col, 1.f);
-    load_params(bias[j], a.bias, a.weight_bf16, col, a.cols - col, 0.f);
+    for (int j = 0; j < S::NV; ++j) {
+      px.load(x[j], p, j);
+      if constexpr (KIND != NORM_ALONE) pr.load(res[j], p, j);
+    }
   }
+};
+
+// The row after the present one is read ahead.
+template <typename T, typename S, int KIND, bool LINES>
+__global__ __launch_bounds__(S::LPR ? 256 : 1024) void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
+#pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
+  constexpr int NV = S::NV;
+  __shared__ float2 sh[2][16];
+  const Place<T, S> p(shape.lanes, a.cols);
+  const int waves = shape.lanes / 64;
+  const int step = gridDim.x * shape.rows;
+  int row = blockIdx.x * shape.rows + p.slot, turn = 0;
+  FwdLine<T, S, KIND, LINES> cur, next;
+  cur.read(a, p, row);
   uint64_t seed = 0, offset = 0;
   if constexpr (KIND == NORM_DROPOUT) {
     seed = a.drop.rng[0];
     offset = a.drop.rng[1];
   }
-  const float inv_n = 1.f / float(a.cols);
-  const int step = gridDim.x * S::R;
-  for (int row = blockIdx.x * S::R + threadIdx.x / LPR; row < a.rows; row += step) {
-    RowAt at;
-    at.b = a.tokens.quotient(row);
-    at.t = row - at.b * a.tokens.d;
-    T* y = row_of<T>(a.y, at);
-    T* hp = a.h.p ? row_of<T>(a.h, at) : nullptr;
-    if (a.lens && int(at.t) >= a.lens[at.b]) {
-      Chunk<T> zero;
-      zero.clear();
+  float w[NV][8], bias[NV][8];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int col = 8 * (lane + j * LPR);
-        store_chunk(zero, y + col, a.cols - col);
-        if (KIND != NORM_ALONE && hp) store_chunk(zero, hp + col, a.cols - col);
-      }
-      if (a.stats && lane == 0) a.stats[row] = make_float2(0.f, 0.f);
-      continue;
-    }
+  for (int j = 0; j < NV; ++j) {
+    const int col = p.col(j);
+    load_params(w[j], a.weight, a.weight_bf16, col, a.cols - col, 1.f);
+    load_params(bias[j], a.bias, a.weight_bf16, col, a.cols - col, 0.f);
+  }
+  const float inv_n = 1.f / float(a.cols);
+  // (the workgroup's waves take as many turns: they meet in the sums)
+  for (int first = blockIdx.x * shape.rows; first < a.rows; first += step, row += step, cur = next) {
+    next.read(a, p, row + step);
+    const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
+    const Line<T, S, LINES> py(a.y, at, row < a.rows, a.cols);
+    const Line<T, S, LINES> ph(a.h, at, row < a.rows, a.cols);
     float v[NV][8];
-    const T* x = row_of<T>(a.x, at);
+    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = 8 * (lane + j * LPR), m = a.cols - col;
-      Chunk<T> c;
-      load_chunk(c, x + col, m);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] = c.get(e);
+      for (int e = 0; e < 8; ++e) v[j][e] = cur.x[j].get(e);
       if constexpr (KIND != NORM_ALONE) {
-        if constexpr (KIND == NORM_DROPOUT) drop(v[j], a.drop, seed, offset, row, lane + j * LPR);
-        load_chunk(c, row_of<T>(a.res, at) + col, m);
+        if constexpr (KIND == NORM_DROPOUT)
+          drop(v[j], a.drop, seed, offset, row, p.lane + j * p.lanes);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[j][e] = plain_add(c.get(e), v[j][e]);
+        for (int e = 0; e < 8; ++e) v[j][e] = cur.res[j].get(e) + v[j][e];
         // the norm is that of the sum as it is stored, the one the backward and the
         // next layer read
+        Chunk<T> c;
         c.set(v[j]);
-        if (hp) store_chunk(c, hp + col, m);
+        ph.store(c, p, j);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[j][e] = c.get(e);
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s.x += v[j][e];
     }
     // Mean and variance. The first mean's rounding is taken off both by the sum of
     // the differences (a row of one large value has variance 0). Where the squares
     // pass fp32's range the row is scaled by 2^-80 and summed again.
     float mean, var, scale = 1.f;
     while (true) {
-      float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s.x += v[j][e];
-      s = row_sum<LPR>(s, sh, turn);
-      mean = s.x * inv_n;
+      mean = line_sum<S>(s, sh, waves, p.slot, turn).x * inv_n;
       s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int m = a.cols - 8 * (lane + j * LPR);
+        float2 t = make_float2(0.f, 0.f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float d = e < m ? v[j][e] - mean : 0.f;
-          s.x += d;
-          s.y = fmaf(d, d, s.y);
+          float d = v[j][e] - mean;
+          if (!LINES && p.col(j) + e >= a.cols) d = 0.f;
+          t.x += d;
+          t.y = fmaf(d, d, t.y);
         }
+        s.x += p.has(j) ? t.x : 0.f;
+        s.y += p.has(j) ? t.y : 0.f;
       }
-      s = row_sum<LPR>(s, sh, turn);
+      s = line_sum<S>(s, sh, waves, p.slot, turn);
       const float more = s.x * inv_n;
       var = fmaxf(fmaf(-more, more, s.y * inv_n), 0.f);
-      const bool again = !is_finite(s.y) && scale == 1.f;
-      if (!again) {
+      if (is_finite(s.y) || scale != 1.f) {
         mean += more;
         if (is_nan(s.y)) var = s.y;  // (fmaxf takes the number)
         break;
       }
       scale = 0x1p-80f;
+      s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[j][e] *= scale;
+        for (int e = 0; e < 8; ++e) {
+          v[j][e] *= scale;
+          s.x += v[j][e];
+        }
     }
     const float r = 1.f / sqrtf(scale == 1.f ? var + a.eps : var);
-    if (a.stats && lane == 0) a.stats[row] = make_float2(mean / scale, r * scale);
+    const float2 st = cur.ok ? make_float2(mean / scale, r * scale) : make_float2(0.f, 0.f);
+    if constexpr (LINES)
+      __builtin_amdgcn_raw_buffer_store_b64(
+          __builtin_bit_cast(u32x2, st), bytes_at(a.stats, a.stats ? a.rows * 8u : 0u),
+          p.lane == 0 && row < a.rows ? row * 8u : OUTSIDE, 0, 0);
+    else if (a.stats && p.lane == 0 && row < a.rows)
+      a.stats[row] = st;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = 8 * (lane + j * LPR);
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = fmaf((v[j][e] - mean) * r, w[j][e], bias[j][e]);
       Chunk<T> c;
       c.set(o);
-      store_chunk(c, y + col, a.cols - col);
+      c.keep(cur.ok);
+      py.store(c, p, j);
     }
   }
 }
 
+// f(shape, its lanes and rows) for rows of whole chunks.
+template <typename F> auto with_lines(int chunks, F f) {
+  if (chunks <= 8) return f(Shape<8, 1>(), ShapeAt{8, 32});
+  if (chunks <= 16) return f(Shape<16, 1>(), ShapeAt{16, 16});
+  if (chunks <= 32) return f(Shape<32, 1>(), ShapeAt{32, 8});
+  if (chunks <= 64) return f(Shape<32, 2>(), ShapeAt{32, 8});
+  if (chunks <= 96) return f(Shape<32, 3>(), ShapeAt{32, 8});
+  if (chunks <= 128) return f(Shape<64, 2>(), ShapeAt{64, 4});
+  const int waves = (chunks + 127) / 128;
+  return f(Shape<0, 2>(), ShapeAt{64 * waves, 1});
+}
+
 template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t s) {
-  return with_shape((a.cols + 7) / 8, [&](auto shape) {
+  return with_lines((a.cols + 7) / 8, [&](auto shape, ShapeAt at) {
     using S = decltype(shape);
-    const int64_t wgs = (int64_t(a.rows) + S::R - 1) / S::R;
-    const int grid = int(wgs < 2048 ? wgs : 2048);
-    norm_fwd_kernel<T, S, KIND><<<dim3(grid), S::NT, 0, s>>>(a);
+    const int64_t wgs = (int64_t(a.rows) + at.rows - 1) / at.rows;
+    const dim3 grid(int(std::min<int64_t>(wgs, 5120 / (at.threads() / 64))));
+    if (a.lines)
+      norm_fwd_kernel<T, S, KIND, true><<<grid, at.threads(), 0, s>>>(a, at);
+    else
+      norm_fwd_kernel<T, S, KIND, false><<<grid, at.threads(), 0, s>>>(a, at);
     return hipGetLastError();
   });
 }

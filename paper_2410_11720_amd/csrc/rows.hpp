@@ -24,6 +24,7 @@ struct RowTensor {
 struct DropArgs {
   const uint64_t* rng = nullptr;  // seed, offset
   uint32_t threshold = 0, site = 0;
+  uint32_t last = 0;              // (threshold << 16) - 1
   float scale = 1.f;
 };
 
@@ -44,6 +45,9 @@ struct NormArgs {
   float* dweight = nullptr;
   float* dbias = nullptr;
   int32_t stride = 0;
+  // whether every row is whole chunks at multiples of 16 bytes, tensors of rows
+  // below a wave's width are below 2 GiB, and statistics too
+  int32_t lines = 0;
 };
 
 struct DropoutArgs {
@@ -53,6 +57,9 @@ struct DropoutArgs {
   Divisor tokens, chunks;      // chunks: of a row
 };
 
+// Columns up to which less than a wave shares a row of whole chunks.
+constexpr int NORM_LINE_COLS = 768;
+
 // What stands in front of a norm.
 enum NormKind { NORM_ALONE = 0, NORM_RESIDUAL = 1, NORM_DROPOUT = 2 };
 
@@ -60,12 +67,15 @@ hipError_t launch_norm_fwd(const NormArgs& a, int dtype, NormKind kind, hipStrea
 hipError_t launch_norm_bwd(const NormArgs& a, int dtype, NormKind kind, hipStream_t s);
 // Workgroups of the backward for this many rows, and floats of each one's sums.
 int norm_bwd_wgs(int64_t rows, int cols);
-inline int norm_part_stride(int cols) { return (2 * cols + 63) / 64 * 64; }
+// (each sum's columns rounded up to whole chunks, both to whole joining workgroups)
+__host__ __device__ inline int norm_padded(int cols) { return (cols + 7) / 8 * 8; }
+inline int norm_part_stride(int cols) { return (2 * norm_padded(cols) + 31) / 32 * 32; }
 hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
 
 #ifdef __HIPCC__
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // (the loads and stores below are single 16-byte ones at any alignment of the
 // element: global memory is accessed unaligned on this target)
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
@@ -90,6 +100,10 @@ template <> struct Chunk<bf16_t> {
   __device__ __forceinline__ void put(int e, bf16_t x) {
     r[e / 2] = e % 2 ? (r[e / 2] & 0xffffu) | uint32_t(x) << 16 : (r[e / 2] & 0xffff0000u) | x;
   }
+  __device__ __forceinline__ void keep(bool yes) {  // else all 0
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = yes ? r[k] : 0;
+  }
   __device__ __forceinline__ bf16_t at(int e) const { return bf16_t(r[e / 2] >> (e % 2 * 16)); }
 };
 template <> struct Chunk<float> {
@@ -109,6 +123,10 @@ template <> struct Chunk<float> {
     for (int e = 0; e < 8; ++e) r[e / 4][e % 4] = __float_as_uint(v[e]);
   }
   __device__ __forceinline__ void put(int e, float x) { r[e / 4][e % 4] = __float_as_uint(x); }
+  __device__ __forceinline__ void keep(bool yes) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[k / 4][k % 4] = yes ? r[k / 4][k % 4] : 0;
+  }
   __device__ __forceinline__ float at(int e) const { return get(e); }
 };
 
@@ -139,6 +157,12 @@ __device__ __forceinline__ void store_chunk(const Chunk<T>& c, T* p, int m) {
 struct RowAt {
   uint32_t b, t;
 };
+__device__ __forceinline__ RowAt row_at(const Divisor& tokens, uint32_t row) {
+  RowAt at;
+  at.b = tokens.quotient(row);
+  at.t = row - at.b * tokens.d;
+  return at;
+}
 template <typename T>
 __device__ __forceinline__ T* row_of(const RowTensor& x, RowAt at) {
   return reinterpret_cast<T*>(x.p + int64_t(at.b) * x.b + int64_t(at.t) * x.t);
@@ -146,15 +170,16 @@ __device__ __forceinline__ T* row_of(const RowTensor& x, RowAt at) {
 
 // v of the elements that stay, scaled; 0 of the others, whatever they hold. (No
 // fused multiply-add with what follows: the sum with a residual has the same bits
-// wherever it is formed.)
+// wherever it is formed.) The draws are compared in the high halves of words: one is
+// below t exactly if the word is at most (t << 16) - 1.
 __device__ __forceinline__ void drop(float (&v)[8], const DropArgs& d, uint64_t seed, uint64_t offset,
                                      uint32_t row, uint32_t chunk) {
 #pragma clang fp contract(off)
   const Philox u = dropout_draws(seed, offset, d.site, row, chunk);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t draw = e % 2 ? u.w[e / 2] >> 16 : u.w[e / 2] & 0xffffu;
-    v[e] = draw < d.threshold ? 0.f : v[e] * d.scale;
+    const uint32_t word = e % 2 ? u.w[e / 2] : u.w[e / 2] << 16;
+    v[e] = word <= d.last ? 0.f : v[e] * d.scale;
   }
 }
 
@@ -163,28 +188,21 @@ __device__ __forceinline__ float plain_add(float x, float y) {
   return x + y;
 }
 
-// Sums of two values over the LPR lanes that share a row (a power of two from 8;
-// above 64 the workgroup is the row, and `turn` alternates between two places of
-// the exchange: one barrier a sum). Every lane has the same bits.
-template <int LPR>
-__device__ __forceinline__ float2 row_sum(float2 v, float2* sh, int& turn) {
-  constexpr int W = LPR < 64 ? LPR : 64;
-  v.x = group_sum<W>(v.x);
-  v.y = group_sum<W>(v.y);
-  if constexpr (LPR > 64) {
-    constexpr int N = LPR / 64;
-    float2* at = sh + turn * N;
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = at[0];
-#pragma unroll
-    for (int k = 1; k < N; ++k) {
-      v.x += at[k].x;
-      v.y += at[k].y;
-    }
+// Sum over aligned groups of W lanes (a power of two from 8), in every lane of a
+// group: lane moves within 16, swaps of 16 and 32 lanes.
+template <int W> __device__ __forceinline__ float lanes_sum(float x) {
+  x = group_sum<W < 16 ? W : 16>(x);
+  if constexpr (W >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
-  return v;
+  if constexpr (W >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return x;
 }
 
 // A gain or offset's eight entries from column col on (m in range).
@@ -206,25 +224,131 @@ __device__ __forceinline__ void load_params(float (&v)[8], const void* p, int bf
   }
 }
 
-// Lanes that share a row, and chunks each of them holds.
-template <int LPR_, int NV_> struct NormShape {
+// ---- rows by their lanes -------------------------------------------------------------
+// Rows of whole chunks at multiples of 16 bytes (LINES) are read and written through
+// buffer descriptors, which bring 0 from outside of their bytes and drop what is
+// stored there: a lane without a chunk, a row behind a sequence's length or behind
+// the last one, a tensor that is not given need no branch. With branches around them
+// the compiler cannot count what is in flight, and waits for the next row's loads and
+// for all stores where it needs this row's (norm of 8192 x 768: forward 8.2 -> 7.0
+// us). Other rows take those branches; what lies where and the order of sums are the
+// same, and so are the results' bits.
+
+constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset behind every descriptor's bytes
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_at(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(bytes), 0x00020000);
+}
+__device__ __forceinline__ void load_at(Chunk<bf16_t>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  c.r = __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0);
+}
+__device__ __forceinline__ void load_at(Chunk<float>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  c.r[0] = __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0);
+  c.r[1] = __builtin_amdgcn_raw_buffer_load_b128(b, off + 16, 0, 0);
+}
+__device__ __forceinline__ void store_at(const Chunk<bf16_t>& c, __amdgpu_buffer_rsrc_t b,
+                                         uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(c.r, b, off, 0, 0);
+}
+__device__ __forceinline__ void store_at(const Chunk<float>& c, __amdgpu_buffer_rsrc_t b,
+                                         uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(c.r[0], b, off, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(c.r[1], b, off + 16, 0, 0);
+}
+
+// Lanes that share a row and chunks each of them holds (chunk lane + j lanes): LPR
+// lanes, or (LPR = 0) the workgroup's waves divided among its rows.
+template <int LPR_, int NV_> struct Shape {
   static constexpr int LPR = LPR_, NV = NV_;
-  static constexpr int NT = LPR > 64 ? LPR : 256;  // threads of a workgroup
-  static constexpr int R = NT / LPR;                // rows it holds at a time
+};
+struct ShapeAt {        // what the host chose
+  int lanes, rows;      // of a row; of a workgroup
+  int threads() const { return lanes * rows; }
 };
 
-// f(shape) for the smallest shape that holds `chunks` chunks a row.
-template <typename F> auto with_shape(int chunks, F f) {
-  if (chunks <= 8) return f(NormShape<8, 1>());
-  if (chunks <= 16) return f(NormShape<16, 1>());
-  if (chunks <= 32) return f(NormShape<32, 1>());
-  if (chunks <= 64) return f(NormShape<64, 1>());
-  if (chunks <= 96) return f(NormShape<32, 3>());
-  if (chunks <= 128) return f(NormShape<64, 2>());
-  if (chunks <= 256) return f(NormShape<128, 2>());
-  if (chunks <= 512) return f(NormShape<256, 2>());
-  if (chunks <= 1024) return f(NormShape<512, 2>());
-  return f(NormShape<1024, 2>());
+// A thread's place: its row of the workgroup's, its chunks in a row.
+template <typename T, typename S> struct Place {
+  int lanes, lane, slot, cols;
+  uint32_t off[S::NV];  // of its chunks in a row, bytes
+
+  __device__ __forceinline__ Place(int lanes_, int cols_) : cols(cols_) {
+    lanes = S::LPR ? S::LPR : lanes_;
+    if constexpr (S::LPR) {
+      slot = threadIdx.x / S::LPR;
+      lane = threadIdx.x % S::LPR;
+    } else {
+      slot = threadIdx.x / uint32_t(lanes);
+      lane = threadIdx.x - slot * lanes;
+    }
+    if constexpr (S::LPR == 0 || S::LPR >= 64) slot = __builtin_amdgcn_readfirstlane(slot);
+#pragma unroll
+    for (int j = 0; j < S::NV; ++j) off[j] = col(j) < cols ? col(j) * uint32_t(sizeof(T)) : OUTSIDE;
+  }
+  __device__ __forceinline__ int col(int j) const { return 8 * (lane + j * lanes); }
+  __device__ __forceinline__ bool has(int j) const { return off[j] != OUTSIDE; }
+};
+
+// A row of x (ok false: none of it). Rows of one wave or more have a descriptor of
+// their own, of fewer lanes an offset in their tensor's (below 2 GiB).
+template <typename T, typename S, bool LINES> struct Line;
+template <typename T, typename S> struct Line<T, S, true> {
+  static constexpr bool WAVES = S::LPR == 0 || S::LPR >= 64;
+  __amdgpu_buffer_rsrc_t b;
+  uint32_t row;
+
+  __device__ __forceinline__ Line(const RowTensor& x, RowAt at, bool ok, int cols)
+      : b(bytes_at(nullptr, 0)), row(0) {
+    if constexpr (WAVES) {
+      b = bytes_at(x.p + int64_t(at.b) * x.b + int64_t(at.t) * x.t,
+                   ok && x.p ? cols * uint32_t(sizeof(T)) : 0);
+    } else {
+      b = bytes_at(x.p, x.p ? OUTSIDE - 32 : 0);
+      row = ok ? at.b * uint32_t(x.b) + at.t * uint32_t(x.t) : OUTSIDE;
+    }
+  }
+  __device__ __forceinline__ uint32_t at(const Place<T, S>& p, int j) const {
+    if constexpr (WAVES) return p.off[j];
+    return p.has(j) && row != OUTSIDE ? p.off[j] + row : OUTSIDE;
+  }
+  __device__ __forceinline__ void load(Chunk<T>& c, const Place<T, S>& p, int j) const {
+    load_at(c, b, at(p, j));
+  }
+  __device__ __forceinline__ void store(const Chunk<T>& c, const Place<T, S>& p, int j) const {
+    store_at(c, b, at(p, j));
+  }
+};
+template <typename T, typename S> struct Line<T, S, false> {
+  T* row;
+
+  __device__ __forceinline__ Line(const RowTensor& x, RowAt at, bool ok, int)
+      : row(ok && x.p ? row_of<T>(x, at) : nullptr) {}
+  __device__ __forceinline__ void load(Chunk<T>& c, const Place<T, S>& p, int j) const {
+    load_chunk(c, row + p.col(j), row ? p.cols - p.col(j) : 0);
+  }
+  __device__ __forceinline__ void store(const Chunk<T>& c, const Place<T, S>& p, int j) const {
+    store_chunk(c, row + p.col(j), row ? p.cols - p.col(j) : 0);
+  }
+};
+
+// Sums of two values over the lanes of a row. Rows of several waves exchange their
+// waves' sums in LDS, in one of two places by turns (one barrier a sum, which all the
+// workgroup's waves pass).
+template <typename S>
+__device__ __forceinline__ float2 line_sum(float2 v, float2 (*sh)[16], int waves, int slot, int& turn) {
+  constexpr int W = S::LPR && S::LPR < 64 ? S::LPR : 64;
+  v.x = lanes_sum<W>(v.x);
+  v.y = lanes_sum<W>(v.y);
+  if constexpr (S::LPR == 0) {
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 15;
+    float2* at = sh[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) at[wave] = v;
+    __syncthreads();
+    v = l < waves ? at[slot * waves + l] : make_float2(0.f, 0.f);
+    v.x = group_sum<16>(v.x);
+    v.y = group_sum<16>(v.y);
+  }
+  return v;
 }
 
 #endif  // __HIPCC__
