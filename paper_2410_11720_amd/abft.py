@@ -523,10 +523,13 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                       lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _call(fn, device, *args):
     """fn(*args, current stream of the device) with that device current."""
     index = device.index
-    if index == torch.cuda.current_device():
+    if index == _current_device():
         return fn(*args, _raw_stream(index))
     with torch.cuda.device(index):
         return fn(*args, _raw_stream(index))
@@ -758,23 +761,28 @@ class _Op:
     """Marshalling that the classes below share: tensors of one type and device
     as records of address and strides."""
 
-    def _records(self, names, tensors, shapes):
+    def _records(self, names, tensors, shapes, fresh=()):
         """Records (address, all strides but the last) one after the other, None
-        for an absent tensor; returns them and the address of each."""
+        for an absent tensor; `fresh` ones, which a call has just made like one of
+        the others, are not looked over. Returns the records and the address of each."""
         fields, at, dtype, index = [], [], self._dtype, self.device.index
         for name, t, shape in zip(names, tensors, shapes):
-            at.append(None)
             if t is None:
+                at.append(None)
                 continue
             st = t.stride()
-            if t.get_device() != index or t.dtype != dtype or t.shape != shape or (
+            if t.get_device() != index or t.dtype is not dtype or t.shape != shape or (
                     st[-1] != 1 and shape[-1] > 1):
                 raise AbftError(f"{name}: expected {tuple(shape)} {dtype} on {self.device} with a "
                                 f"contiguous last dimension, got {tuple(t.shape)} {t.dtype} on "
                                 f"{t.device}, strides {st}")
-            at[-1] = 8 * len(fields)
+            at.append(8 * len(fields))
             fields.append(t.data_ptr())
             fields += st[:-1]
+        for t in fresh:
+            at.append(8 * len(fields))
+            fields.append(t.data_ptr())
+            fields += t.stride()[:-1]
         held = array.array("q", fields)
         base = held.buffer_info()[0]
         return held, [None if a is None else base + a for a in at]
@@ -831,24 +839,26 @@ class Dropout(_Op):
         self.device = torch.empty(0, device=device).device
         self._c = cfg.to_c()
         self._dtype = _DTYPES[cfg.dtype][1]
-        self._shape = (cfg.batch, cfg.tokens, cfg.cols)
+        self._shapes = ((cfg.batch, cfg.tokens, cfg.cols),) * 3
+        self._drops = cfg.p >= 2.0 ** -17
 
     def _run(self, names, x, residual, rng, y):
-        held, (x, r, y) = self._records(names, (x, residual, y), (self._shape,) * 3)
-        rng = self._state(rng, self.cfg.p >= 2.0 ** -17)
-        _check(_call(_lib.attn_dropout, self.device, self._c, x, r, rng, y), "attn_dropout")
+        if y is None:
+            y = torch.empty_like(x)
+            held, (x, r, o) = self._records(names, (x, residual), self._shapes, (y,))
+        else:
+            held, (x, r, o) = self._records(names, (x, residual, y), self._shapes)
+        rng = self._state(rng, self._drops)
+        _check(_call(_lib.attn_dropout, self.device, self._c, x, r, rng, o), "attn_dropout")
+        return y
 
     def forward(self, x, rng=None, residual=None, y=None):
         """residual + dropout(x)."""
-        y = torch.empty_like(x) if y is None else y
-        self._run(("x", "residual", "y"), x, residual, rng, y)
-        return y
+        return self._run(("x", "residual", "y"), x, residual, rng, y)
 
     def backward(self, dy, rng=None, dx=None):
         """dropout(dy), the gradient of x; that of the residual is dy itself."""
-        dx = torch.empty_like(dy) if dx is None else dx
-        self._run(("dy", "", "dx"), dy, None, rng, dx)
-        return dx
+        return self._run(("dy", "", "dx"), dy, None, rng, dx)
 
 
 @dataclasses.dataclass
@@ -895,7 +905,11 @@ class _Norm(_Op):
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
         self._saved = self.new_saved() if training else None
         self._dtype, self._wdtype = _DTYPES[cfg.dtype][1], _DTYPES[cfg.weight_dtype][1]
-        self._shape = (cfg.batch, cfg.tokens, cfg.cols)
+        self._shape, self._cols = (cfg.batch, cfg.tokens, cfg.cols), (cfg.cols,)
+        self._shapes = (self._shape,) * 5
+        self._drops = cfg.dropout >= 2.0 ** -17
+        if training:
+            self._sums = torch.empty(cfg.cols, dtype=torch.float32, device=self.device)
 
     @property
     def stats(self):
@@ -910,23 +924,23 @@ class _Norm(_Op):
             raise AbftError("saved: made for another shape or device")
         return saved
 
-    def _forward(self, x, residual, weight, bias, lens, rng, h, y, saved):
-        held, (x_, r_, h_, y_) = self._records(("x", "residual", "h", "y"), (x, residual, h, y),
-                                               (self._shape,) * 4)
-        cols = self._shape[2:]
+    def _forward(self, rows, weight, bias, lens, rng, saved, of):
+        """rows: of x, residual, h, y; of: where the norm's rows are."""
+        x, r, h, y = rows
         saved = self._saved if saved is None else self._record(saved)
         stats = None
         if saved is not None:
             stats, saved._of = saved.stats.data_ptr(), None
-        _check(_call(_lib.attn_norm_forward, self.device, self._c, x_, r_,
-                     self._vector(weight, "weight", cols, self._wdtype),
-                     self._vector(bias, "bias", cols, self._wdtype),
-                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, h_, y_, stats),
+        _check(_call(_lib.attn_norm_forward, self.device, self._c, x, r,
+                     self._vector(weight, "weight", self._cols, self._wdtype),
+                     self._vector(bias, "bias", self._cols, self._wdtype),
+                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, h, y, stats),
                "attn_norm_forward")
         if saved is not None:
-            saved._of = (x if residual is None else h).data_ptr()
+            saved._of = of.data_ptr()
 
-    def _backward(self, dy, dh, h, weight, lens, rng, dx, dresidual, dweight, dbias, saved):
+    def _of(self, saved, h):
+        """The record of the rows h."""
         own = saved is None
         saved = self._saved if own else self._record(saved)
         if saved is None or self.workspace is None:
@@ -935,18 +949,22 @@ class _Norm(_Op):
             raise AbftError("backward: the rows are not those of the last forward"
                             if saved._of is not None
                             else "backward: no forward has left its statistics")
-        cols = self._shape[2:]
+        return saved
+
+    def _backward(self, rows, weight, lens, rng, dweight, dbias, saved):
+        """rows: of dy, dh, h, dx, dresidual."""
+        dy, dh, h, dx, dr = rows
+        dw, db = (self._vector(t, name, self._cols, torch.float32)
+                  for t, name in ((dweight, "dweight"), (dbias, "dbias")))
         if dweight is None:
-            dweight = torch.empty(cols, dtype=torch.float32, device=self.device)
+            dweight = torch.empty_like(self._sums)
+            dw = dweight.data_ptr()
         if dbias is None:
-            dbias = torch.empty(cols, dtype=torch.float32, device=self.device)
-        held, (dy_, dh_, h_, dx_, dr_) = self._records(
-            ("dy", "dh", "h", "dx", "dresidual"), (dy, dh, h, dx, dresidual), (self._shape,) * 5)
-        _check(_call(_lib.attn_norm_backward, self.device, self._c, dy_, dh_, h_,
-                     self._vector(weight, "weight", cols, self._wdtype), saved.stats.data_ptr(),
-                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, dx_, dr_,
-                     self._vector(dweight, "dweight", cols, torch.float32),
-                     self._vector(dbias, "dbias", cols, torch.float32),
+            dbias = torch.empty_like(self._sums)
+            db = dbias.data_ptr()
+        _check(_call(_lib.attn_norm_backward, self.device, self._c, dy, dh, h,
+                     self._vector(weight, "weight", self._cols, self._wdtype), saved.stats.data_ptr(),
+                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, dx, dr, dw, db,
                      self.workspace.data_ptr(), self.workspace.numel()), "attn_norm_backward")
         return dweight, dbias
 
@@ -971,14 +989,23 @@ class LayerNorm(_Norm):
         super().__init__(cfg, device, training)
 
     def forward(self, x, weight=None, bias=None, lens=None, y=None, saved=None):
-        y = torch.empty_like(x) if y is None else y
-        self._forward(x, None, weight, bias, lens, None, None, y, saved)
+        if y is None:
+            y = torch.empty_like(x)
+            held, (x_, y_) = self._records(("x",), (x,), self._shapes, (y,))
+        else:
+            held, (x_, y_) = self._records(("x", "y"), (x, y), self._shapes)
+        self._forward((x_, None, None, y_), weight, bias, lens, None, saved, x)
         return y
 
     def backward(self, dy, x, weight=None, lens=None, dx=None, dweight=None, dbias=None, saved=None):
         """dx, dweight, dbias."""
-        dx = torch.empty_like(dy) if dx is None else dx
-        dweight, dbias = self._backward(dy, None, x, weight, lens, None, dx, None, dweight, dbias,
+        saved = self._of(saved, x)
+        if dx is None:
+            dx = torch.empty_like(dy)
+            held, (dy, x, o) = self._records(("dy", "x"), (dy, x), self._shapes, (dx,))
+        else:
+            held, (dy, x, o) = self._records(("dy", "x", "dx"), (dy, x, dx), self._shapes)
+        dweight, dbias = self._backward((dy, None, x, o, None), weight, lens, None, dweight, dbias,
                                         saved)
         return dx, dweight, dbias
 
@@ -992,12 +1019,16 @@ class ResidualNorm(_Norm):
     def forward(self, x, residual, weight=None, bias=None, rng=None, lens=None, h=None, y=None,
                 saved=None):
         """h, y."""
-        h = torch.empty_like(x) if h is None else h
-        y = torch.empty_like(x) if y is None else y
         if residual is None:
             raise AbftError("residual: LayerNorm is the norm without one")
-        self._forward(x, residual, weight, bias, lens, self._state(rng, self.cfg.dropout >= 2.0 ** -17),
-                      h, y, saved)
+        if h is None and y is None:
+            h, y = torch.empty_like(x), torch.empty_like(x)
+            held, rows = self._records(("x", "residual"), (x, residual), self._shapes, (h, y))
+        else:
+            h = torch.empty_like(x) if h is None else h
+            y = torch.empty_like(x) if y is None else y
+            held, rows = self._records(("x", "residual", "h", "y"), (x, residual, h, y), self._shapes)
+        self._forward(rows, weight, bias, lens, self._state(rng, self._drops), saved, h)
         return h, y
 
     def backward(self, dy, h, weight=None, dh=None, rng=None, lens=None, dx=None, dresidual=None,
@@ -1005,14 +1036,26 @@ class ResidualNorm(_Norm):
         """dx, dresidual, dweight, dbias. dh: what comes to h beside its norm's
         gradient. Without dropout dx and dresidual are alike: one tensor unless both
         are given."""
-        drops = self.cfg.dropout >= 2.0 ** -17
-        if dx is None:
-            dx = torch.empty_like(dy) if drops or dresidual is None else dresidual
-        if dresidual is None:
-            dresidual = torch.empty_like(dy) if drops else dx
-        second = None if dresidual is dx else dresidual
-        dweight, dbias = self._backward(dy, dh, h, weight, lens, self._state(rng, drops), dx, second,
-                                        dweight, dbias, saved)
+        saved = self._of(saved, h)
+        drops, names = self._drops, ("dy", "dh", "h", "dx", "dresidual")
+        if dx is None and dresidual is None:
+            dx = dresidual = torch.empty_like(dy)
+            fresh = (dx,)
+            if drops:
+                dresidual = torch.empty_like(dy)
+                fresh = (dx, dresidual)
+            held, rows = self._records(names, (dy, dh, h), self._shapes, fresh)
+        else:
+            if dx is None:
+                dx = torch.empty_like(dy) if drops else dresidual
+            if dresidual is None:
+                dresidual = torch.empty_like(dy) if drops else dx
+            second = () if dresidual is dx else (dresidual,)
+            held, rows = self._records(names, (dy, dh, h, dx, *second), self._shapes)
+        if len(rows) == 4:
+            rows.append(None)
+        dweight, dbias = self._backward(rows, weight, lens, self._state(rng, drops), dweight, dbias,
+                                        saved)
         return dx, dresidual, dweight, dbias
 
 
@@ -1078,10 +1121,14 @@ class Rotary(_Op):
                 self._vector(q_start, "q_start", (self.cfg.batch,), torch.int32))
 
     def _turn(self, backward, names, Q, K, q_start, Q_out, K_out):
-        Q_out = torch.empty_like(Q) if Q_out is None else Q_out
-        K_out = torch.empty_like(K) if K_out is None else K_out
         qs, ks = self._q_shape, self._k_shape
-        held, (q, k, qo, ko) = self._records(names, (Q, K, Q_out, K_out), (qs, ks, qs, ks))
+        if Q_out is None and K_out is None:
+            Q_out, K_out = torch.empty_like(Q), torch.empty_like(K)
+            held, (q, k, qo, ko) = self._records(names, (Q, K), (qs, ks), (Q_out, K_out))
+        else:
+            Q_out = torch.empty_like(Q) if Q_out is None else Q_out
+            K_out = torch.empty_like(K) if K_out is None else K_out
+            held, (q, k, qo, ko) = self._records(names, (Q, K, Q_out, K_out), (qs, ks, qs, ks))
         freqs, start = self._at(q_start)
         _check(_call(_lib.attn_rotary, self.device, self._c, backward, q, k, freqs, start, qo, ko),
                "attn_rotary")
@@ -1099,13 +1146,16 @@ class Rotary(_Op):
         """Returns the turned queries; turned keys and the values go to rows q_start +
         i of the caches [batch, capacity, kv_heads, head_dim] (left out where the
         caches have no such row)."""
-        Q_out = torch.empty_like(Q) if Q_out is None else Q_out
         qs, ks = self._q_shape, self._k_shape
         capacity = K_cache.shape[1]
         cs = (ks[0], capacity, ks[2], ks[3])
-        held, (q, k, v, qo, kc, vc) = self._records(
-            ("Q", "K", "V", "Q_out", "K_cache", "V_cache"), (Q, K, V, Q_out, K_cache, V_cache),
-            (qs, ks, ks, qs, cs, cs))
+        names, tensors = ("Q", "K", "V", "K_cache", "V_cache", "Q_out"), (Q, K, V, K_cache, V_cache)
+        if Q_out is None:
+            Q_out = torch.empty_like(Q)
+            held, at = self._records(names, tensors, (qs, ks, ks, cs, cs), (Q_out,))
+        else:
+            held, at = self._records(names, (*tensors, Q_out), (qs, ks, ks, cs, cs, qs))
+        q, k, v, kc, vc, qo = at
         freqs, start = self._at(q_start)
         _check(_call(_lib.attn_rotary_append, self.device, self._c, q, k, v, freqs, start, capacity,
                      qo, kc, vc), "attn_rotary_append")

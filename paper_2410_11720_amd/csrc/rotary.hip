@@ -1,10 +1,10 @@
 // Rotary positions: pair k of a head at position p is turned by p f_k,
 //   (a, c) -> m (a cos - c sin, a sin + c cos),
-// backward by -p f_k. A workgroup takes some tokens: their angles' cosines and
-// sines go to LDS once, then all heads of the tokens pass through. An angle is
-// formed in 64 bits and reduced to one turn there (position 2^20 at one radian a
-// position has 3 bits left behind the point in 32); its functions in 32. Bound by
-// memory.
+// backward by -p f_k. A wave takes a token, or some heads of one: it forms the angles'
+// cosines and sines once, into its own part of LDS, then its lanes take 16 dims of a
+// head at a time. An angle is formed in 64 bits and reduced to one turn there
+// (position 2^20 at one radian a position has 3 bits left behind the point in 32); its
+// functions in 32. Bound by memory.
 #include <algorithm>
 
 #include "rotary_internal.hpp"
@@ -14,131 +14,167 @@ namespace abft {
 namespace {
 
 constexpr int NT = 256;
-constexpr int LDS_PAIRS = 4096;  // of a workgroup's tokens
+constexpr int MAX_PAIRS = 256;  // of a head
+constexpr int U = 2;            // items of a lane in flight
 
-template <typename T> __device__ __forceinline__ T* head_at(const HeadTensor& x, uint32_t b,
-                                                            int64_t t, uint32_t h) {
-  return reinterpret_cast<T*>(x.p + int64_t(b) * x.b + t * x.t + int64_t(h) * x.h);
-}
+// Item: two chunks of a head, m[0] and m[1] of their elements in it.
+template <typename T> struct Item {
+  Chunk<T> c[2];
+  T* out[2];
+  int m[2];
+  int pair;     // of the first element; below 0: copied
+  bool store;
+};
 
-template <typename T>
-__device__ __forceinline__ void turn_halves(const T* x, T* o, const float2* cs, int half, int k) {
-  const int m = half - k;
-  Chunk<T> a, c;
-  load_chunk(a, x + k, m);
-  load_chunk(c, x + half + k, m);
-  float p[8], q[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float2 f = e < m ? cs[k + e] : make_float2(1.f, 0.f);
-    p[e] = a.get(e) * f.x - c.get(e) * f.y;
-    q[e] = a.get(e) * f.y + c.get(e) * f.x;
-  }
-  a.set(p);
-  c.set(q);
-  store_chunk(a, o + k, m);
-  store_chunk(c, o + half + k, m);
-}
-
-template <typename T>
-__device__ __forceinline__ void turn_neighbours(const T* x, T* o, const float2* cs, int half, int k) {
-  const int m = 2 * (half - k);
-  Chunk<T> a;
-  load_chunk(a, x + 2 * k, m);
-  float p[8];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 f = 2 * e < m ? cs[k + e] : make_float2(1.f, 0.f);
-    p[2 * e] = a.get(2 * e) * f.x - a.get(2 * e + 1) * f.y;
-    p[2 * e + 1] = a.get(2 * e) * f.y + a.get(2 * e + 1) * f.x;
-  }
-  a.set(p);
-  store_chunk(a, o + 2 * k, m);
-}
-
-template <typename T>
+// FULL: every chunk is whole.
+template <typename T, bool INTER, bool FULL>
 __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a) {
-  __shared__ float2 cs[LDS_PAIRS];
-  const int tiles = (a.n_tokens + a.tile - 1) / a.tile;
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int first = tile * a.tile, n = min(a.tile, a.n_tokens - first);
-    __syncthreads();  // (the tile before has been read)
-    for (int i = threadIdx.x; i < n * a.half; i += NT) {
-      const int tok = i / a.half, k = i - tok * a.half;
-      const uint32_t b = a.tokens.quotient(first + tok);
-      const int64_t at = int64_t(a.start ? a.start[b] : 0) + (first + tok - int(b * a.tokens.d));
-      double turns = double(at) * a.freqs[k] * 0.15915494309189533577;  // 1 / (2 pi)
+  __shared__ float2 angles[NT / 64][MAX_PAIRS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  float2* cs = angles[wave];
+  const int jobs = a.n_tokens * int(a.waves.d);
+  for (int64_t job = int64_t(blockIdx.x) * (NT / 64) + wave; job < jobs;
+       job += int64_t(gridDim.x) * (NT / 64)) {
+    const uint32_t n = a.waves.quotient(uint32_t(job));
+    const uint32_t b = a.tokens.quotient(n), t = n - b * a.tokens.d;
+    const int first = int(uint32_t(job) - n * a.waves.d) * a.per;
+    const int end = min(first + a.per, a.items);
+    const int64_t pos = int64_t(a.start ? a.start[b] : 0) + t;
+    const int64_t row = a.append ? pos : t;   // of keys and values
+    const bool there = !a.append || (pos >= 0 && pos < a.capacity);
+    auto at = [&](const HeadTensor& x, int64_t r) { return x.p + int64_t(b) * x.b + r * x.t; };
+    const char* in[3] = {at(a.in[0], t), at(a.in[1], t), at(a.in[2], t)};
+    char* out[3] = {at(a.out[0], t), at(a.out[1], row), at(a.out[2], row)};
+    for (int k = lane; k < a.half; k += 64) {
+      double turns = double(pos) * a.freqs[k] * 0.15915494309189533577;  // 1 / (2 pi)
       turns -= rint(turns);
       float s, c;
       sincospif(2.f * float(turns), &s, &c);
-      cs[i] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
+      cs[k] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
     }
-    __syncthreads();
-    const int items = n * int(a.slots.d * a.parts.d);
-    for (int i = threadIdx.x; i < items; i += NT) {
-      const uint32_t head = a.parts.quotient(i), part = i - head * a.parts.d;
-      const uint32_t tok = a.slots.quotient(head);
-      uint32_t slot = head - tok * a.slots.d;
-      const uint32_t b = a.tokens.quotient(first + tok);
-      const uint32_t t = first + tok - b * a.tokens.d;
-      int which = 0;
-      if (slot >= uint32_t(a.heads[0])) {
-        slot -= a.heads[0];
-        which = 1;
-        if (slot >= uint32_t(a.heads[1])) {
-          slot -= a.heads[1];
-          which = 2;
+    // (a wave's LDS accesses keep their order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    int i = first + lane;
+    int head = a.parts.quotient(i), part = i - head * int(a.parts.d);
+    while (i - lane < end) {
+      Item<T> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        // (behind the last item: the wave's first one again, not stored)
+        const bool ok = i < end;
+        const int h = ok ? head : 0, p = ok ? part : 0;
+        const int which = h < a.heads[0] ? 0 : h < a.heads[0] + a.heads[1] ? 1 : 2;
+        const int64_t slot = h - (which > 0 ? a.heads[0] : 0) - (which > 1 ? a.heads[1] : 0);
+        const int64_t hs = which == 0 ? a.in[0].h : which == 1 ? a.in[1].h : a.in[2].h;
+        const int64_t ho = which == 0 ? a.out[0].h : which == 1 ? a.out[1].h : a.out[2].h;
+        const T* src = reinterpret_cast<const T*>((which == 0 ? in[0] : which == 1 ? in[1] : in[2]) +
+                                                  slot * hs);
+        T* dst = reinterpret_cast<T*>((which == 0 ? out[0] : which == 1 ? out[1] : out[2]) + slot * ho);
+        const bool turn = which < 2 && p < a.turned;
+        int e0, e1;
+        if (turn) {
+          x[u].pair = 8 * p;
+          e0 = INTER ? 16 * p : 8 * p;
+          e1 = INTER ? 16 * p + 8 : a.half + 8 * p;
+          x[u].m[0] = INTER ? 2 * a.half - e0 : a.half - 8 * p;
+          x[u].m[1] = INTER ? 2 * a.half - e1 : a.half - 8 * p;
+        } else {
+          x[u].pair = -1;
+          e0 = 16 * p + (which < 2 ? 2 * a.half - 16 * a.turned : 0);
+          e1 = e0 + 8;
+          x[u].m[0] = a.head_dim - e0;
+          x[u].m[1] = a.head_dim - e1;
+        }
+        x[u].out[0] = dst + e0;
+        x[u].out[1] = dst + e1;
+        x[u].store = ok && (which == 0 || there);
+        if constexpr (FULL) {
+          x[u].c[0].load(src + e0);
+          x[u].c[1].load(src + e1);
+        } else {
+          load_chunk(x[u].c[0], src + e0, x[u].m[0]);
+          load_chunk(x[u].c[1], src + e1, x[u].m[1]);
+        }
+        i += 64;
+        head += a.dq;
+        part += a.dr;
+        if (part >= int(a.parts.d)) {
+          part -= a.parts.d;
+          ++head;
         }
       }
-      int64_t to = t;
-      if (a.append && which > 0) {
-        to += a.start ? a.start[b] : 0;
-        if (to < 0 || to >= a.capacity) continue;
-      }
-      const HeadTensor& src = which == 0 ? a.in[0] : which == 1 ? a.in[1] : a.in[2];
-      const HeadTensor& dst = which == 0 ? a.out[0] : which == 1 ? a.out[1] : a.out[2];
-      const T* x = head_at<T>(src, b, t, slot);
-      T* o = head_at<T>(dst, b, to, slot);
-      const float2* f = cs + tok * a.half;
-      if (which < 2 && part < uint32_t(a.turned)) {
-        if (a.interleaved)
-          turn_neighbours(x, o, f, a.half, 4 * part);
-        else
-          turn_halves(x, o, f, a.half, 8 * part);
-        continue;
-      }
-      // dims that stay as they are: behind the turned ones, or all of a value's
-      const int p0 = which < 2 ? 2 * a.half + 8 * (part - a.turned) : 8 * part;
-      const int step = which < 2 ? a.head_dim : 8 * a.parts.d;
-      for (int p = p0; p < a.head_dim; p += step) {
-        Chunk<T> c;
-        load_chunk(c, x + p, a.head_dim - p);
-        store_chunk(c, o + p, a.head_dim - p);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (x[u].pair >= 0) {
+          float p[8], q[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int k = x[u].pair + e;
+            const float2 f = FULL ? cs[k] : cs[min(k, a.half - 1)];
+            // elements of pair e: of both chunks, or neighbours in one
+            Chunk<T>&ca = x[u].c[INTER ? e / 4 : 0], &cc = x[u].c[INTER ? e / 4 : 1];
+            const int ia = INTER ? 2 * e % 8 : e, ic = INTER ? 2 * e % 8 + 1 : e;
+            const float va = ca.get(ia), vc = cc.get(ic);
+            p[e] = va * f.x - vc * f.y;
+            q[e] = va * f.y + vc * f.x;
+          }
+          if constexpr (INTER) {
+            const float lo[8] = {p[0], q[0], p[1], q[1], p[2], q[2], p[3], q[3]};
+            const float hi[8] = {p[4], q[4], p[5], q[5], p[6], q[6], p[7], q[7]};
+            x[u].c[0].set(lo);
+            x[u].c[1].set(hi);
+          } else {
+            x[u].c[0].set(p);
+            x[u].c[1].set(q);
+          }
+        }
+        if (!x[u].store) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if constexpr (FULL)
+            x[u].c[k].store(x[u].out[k]);
+          else
+            store_chunk(x[u].c[k], x[u].out[k], x[u].m[k]);
+        }
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <typename T> hipError_t launch(const RotaryArgs& a, bool full, int grid, hipStream_t s) {
+  if (a.interleaved && full)
+    rotary_kernel<T, true, true><<<dim3(grid), NT, 0, s>>>(a);
+  else if (a.interleaved)
+    rotary_kernel<T, true, false><<<dim3(grid), NT, 0, s>>>(a);
+  else if (full)
+    rotary_kernel<T, false, true><<<dim3(grid), NT, 0, s>>>(a);
+  else
+    rotary_kernel<T, false, false><<<dim3(grid), NT, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_rotary(RotaryArgs a, int dtype, hipStream_t s) {
-  a.turned = a.interleaved ? (a.half + 3) / 4 : (a.half + 7) / 8;
-  const int parts = a.turned + (a.head_dim - 2 * a.half + 7) / 8;
-  const int slots = a.heads[0] + a.heads[1] + a.heads[2];
+  a.turned = (a.half + 7) / 8;
+  const int copied = a.head_dim - 2 * a.half;
+  const int parts = a.turned + (copied + 15) / 16;
   a.parts = Divisor::of(parts);
-  a.slots = Divisor::of(slots);
-  // tokens of a workgroup: four items a thread, but no fewer than 1024 workgroups
-  const int64_t items = int64_t(parts) * slots;
-  int64_t tile = std::max<int64_t>(1, 4 * NT / items);
-  tile = std::min<int64_t>(tile, std::max(1, a.n_tokens / 1024));
-  a.tile = int(std::min<int64_t>(tile, LDS_PAIRS / std::max(1, a.half)));
-  const int tiles = (a.n_tokens + a.tile - 1) / a.tile;
-  const int grid = std::min(tiles, 1 << 20);
-  if (dtype == ABFT_BF16)
-    rotary_kernel<bf16_t><<<dim3(grid), NT, 0, s>>>(a);
-  else
-    rotary_kernel<float><<<dim3(grid), NT, 0, s>>>(a);
-  return hipGetLastError();
+  a.items = parts * (a.heads[0] + a.heads[1] + a.heads[2]);
+  a.dq = 64 / parts;
+  a.dr = 64 % parts;
+  // few tokens: several waves share one, down to 64 items each
+  const int steps = (a.items + 63) / 64;
+  const int waves = std::max(1, std::min(steps, 4096 / std::min(4096, a.n_tokens)));
+  a.per = 64 * ((steps + waves - 1) / waves);
+  a.waves = Divisor::of((a.items + a.per - 1) / a.per);
+  const int64_t jobs = int64_t(a.n_tokens) * a.waves.d;
+  const int grid = int(std::min<int64_t>((jobs + 3) / 4, 1 << 20));
+  const bool full = a.half % 8 == 0 && copied % 16 == 0;
+  return dtype == ABFT_BF16 ? launch<bf16_t>(a, full, grid, s) : launch<float>(a, full, grid, s);
 }
 
 }  // namespace abft

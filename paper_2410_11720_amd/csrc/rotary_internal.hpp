@@ -26,10 +26,10 @@ struct RotaryArgs {
   float sign = 1.f, magnitude = 1.f;
   int32_t append = 0;             // keys and values go to their positions ...
   int32_t capacity = 0;           // ... below this one
-  // work: parts of a head (turned, then copied ones), heads, tokens of a workgroup
-  int32_t turned = 0;
-  Divisor parts, slots;
-  int32_t tile = 1;
+  // work: items of a token are parts (16 dims) of heads, `turned` ones in front; a
+  // wave takes `per` of them, `waves` waves a token; 64 items are dq heads and dr parts
+  int32_t turned = 0, items = 0, per = 0, dq = 0, dr = 0;
+  Divisor parts, waves;
 };
 
 hipError_t launch_rotary(RotaryArgs a, int dtype, hipStream_t s);
