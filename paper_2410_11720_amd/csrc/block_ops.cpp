@@ -246,6 +246,14 @@ int attn_dropout(const attn_dropout_config* cfg, const attn_rows* x, const attn_
   if (a.rows == 0) return ABFT_OK;
   a.tokens = Divisor::of(S);
   a.chunks = Divisor::of((H + 7) / 8);
+  a.flat = H % 8 == 0;
+  for (int i = 0; i < 3; ++i) {
+    if (!mem[i].p) continue;
+    const int64_t row = int64_t(H) * es_of(dt);
+    if (reinterpret_cast<uintptr_t>(mem[i].p) % 16 || (S > 1 && mem[i].st[1] != row) ||
+        (B > 1 && mem[i].st[0] != row * S))
+      a.flat = 0;
+  }
   TRY(check_device());
   CK(launch_dropout(a, dt, static_cast<hipStream_t>(stream)));
   return ABFT_OK;

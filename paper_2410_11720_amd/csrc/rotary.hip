@@ -1,8 +1,8 @@
 // Rotary positions: pair k of a head at position p is turned by p f_k,
 //   (a, c) -> m (a cos - c sin, a sin + c cos),
-// backward by -p f_k. A wave takes a token, or some heads of one: it forms the angles'
-// cosines and sines once, into its own part of LDS, then its lanes take 16 dims of a
-// head at a time. An angle is formed in 64 bits and reduced to one turn there
+// backward by -p f_k. A wave, or 32 or 16 lanes of one, takes a token, or some heads of
+// one: it forms the angles' cosines and sines once, into its own part of LDS, then its
+// lanes take 16 dims of a head at a time. An angle is formed in 64 bits and reduced to one turn there
 // (position 2^20 at one radian a position has 3 bits left behind the point in 32); its
 // functions in 32. Bound by memory.
 #include <algorithm>
@@ -15,7 +15,6 @@ namespace {
 
 constexpr int NT = 256;
 constexpr int MAX_PAIRS = 256;  // of a head
-constexpr int U = 2;            // items of a lane in flight
 
 // Item: two chunks of a head, m[0] and m[1] of their elements in it.
 template <typename T> struct Item {
@@ -26,15 +25,17 @@ template <typename T> struct Item {
   bool store;
 };
 
-// FULL: every chunk is whole.
-template <typename T, bool INTER, bool FULL>
+// L lanes a token, U items of a lane in flight. FULL: every chunk is whole.
+template <typename T, int L, int U, bool INTER, bool FULL>
 __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a) {
-  __shared__ float2 angles[NT / 64][MAX_PAIRS];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  float2* cs = angles[wave];
+  __shared__ float2 angles[NT / L][MAX_PAIRS * L / 64];
+  const int lane = threadIdx.x % L;
+  int group = threadIdx.x / L;
+  if constexpr (L == 64) group = __builtin_amdgcn_readfirstlane(group);
+  float2* cs = angles[group];
   const int jobs = a.n_tokens * int(a.waves.d);
-  for (int64_t job = int64_t(blockIdx.x) * (NT / 64) + wave; job < jobs;
-       job += int64_t(gridDim.x) * (NT / 64)) {
+  for (int64_t job = int64_t(blockIdx.x) * (NT / L) + group; job < jobs;
+       job += int64_t(gridDim.x) * (NT / L)) {
     const uint32_t n = a.waves.quotient(uint32_t(job));
     const uint32_t b = a.tokens.quotient(n), t = n - b * a.tokens.d;
     const int first = int(uint32_t(job) - n * a.waves.d) * a.per;
@@ -43,9 +44,9 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a) {
     const int64_t row = a.append ? pos : t;   // of keys and values
     const bool there = !a.append || (pos >= 0 && pos < a.capacity);
     auto at = [&](const HeadTensor& x, int64_t r) { return x.p + int64_t(b) * x.b + r * x.t; };
-    const char* in[3] = {at(a.in[0], t), at(a.in[1], t), at(a.in[2], t)};
-    char* out[3] = {at(a.out[0], t), at(a.out[1], row), at(a.out[2], row)};
-    for (int k = lane; k < a.half; k += 64) {
+    const char *in0 = at(a.in[0], t), *in1 = at(a.in[1], t), *in2 = at(a.in[2], t);
+    char *out0 = at(a.out[0], t), *out1 = at(a.out[1], row), *out2 = at(a.out[2], row);
+    for (int k = lane; k < a.half; k += L) {
       double turns = double(pos) * a.freqs[k] * 0.15915494309189533577;  // 1 / (2 pi)
       turns -= rint(turns);
       float s, c;
@@ -61,16 +62,16 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a) {
       Item<T> x[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        // (behind the last item: the wave's first one again, not stored)
+        // (behind the last item: a first one again, not stored)
         const bool ok = i < end;
         const int h = ok ? head : 0, p = ok ? part : 0;
         const int which = h < a.heads[0] ? 0 : h < a.heads[0] + a.heads[1] ? 1 : 2;
         const int64_t slot = h - (which > 0 ? a.heads[0] : 0) - (which > 1 ? a.heads[1] : 0);
         const int64_t hs = which == 0 ? a.in[0].h : which == 1 ? a.in[1].h : a.in[2].h;
         const int64_t ho = which == 0 ? a.out[0].h : which == 1 ? a.out[1].h : a.out[2].h;
-        const T* src = reinterpret_cast<const T*>((which == 0 ? in[0] : which == 1 ? in[1] : in[2]) +
+        const T* src = reinterpret_cast<const T*>((which == 0 ? in0 : which == 1 ? in1 : in2) +
                                                   slot * hs);
-        T* dst = reinterpret_cast<T*>((which == 0 ? out[0] : which == 1 ? out[1] : out[2]) + slot * ho);
+        T* dst = reinterpret_cast<T*>((which == 0 ? out0 : which == 1 ? out1 : out2) + slot * ho);
         const bool turn = which < 2 && p < a.turned;
         int e0, e1;
         if (turn) {
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a) {
           load_chunk(x[u].c[0], src + e0, x[u].m[0]);
           load_chunk(x[u].c[1], src + e1, x[u].m[1]);
         }
-        i += 64;
+        i += L;
         head += a.dq;
         part += a.dr;
         if (part >= int(a.parts.d)) {
@@ -144,16 +145,35 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a) {
   }
 }
 
-template <typename T> hipError_t launch(const RotaryArgs& a, bool full, int grid, hipStream_t s) {
+template <typename T, int L, int U> hipError_t launch(RotaryArgs a, bool full, hipStream_t s) {
+  a.dq = L / int(a.parts.d);
+  a.dr = L % int(a.parts.d);
+  // few tokens: several groups share one, down to an item a lane
+  const int steps = (a.items + L - 1) / L, few = 4096 * (64 / L);
+  const int waves = std::max(1, std::min(steps, few / std::min(few, a.n_tokens)));
+  a.per = L * ((steps + waves - 1) / waves);
+  a.waves = Divisor::of((a.items + a.per - 1) / a.per);
+  const int64_t jobs = int64_t(a.n_tokens) * a.waves.d;
+  const dim3 grid(int(std::min<int64_t>((jobs + NT / L - 1) / (NT / L), 1 << 20)));
   if (a.interleaved && full)
-    rotary_kernel<T, true, true><<<dim3(grid), NT, 0, s>>>(a);
+    rotary_kernel<T, L, U, true, true><<<grid, NT, 0, s>>>(a);
   else if (a.interleaved)
-    rotary_kernel<T, true, false><<<dim3(grid), NT, 0, s>>>(a);
+    rotary_kernel<T, L, U, true, false><<<grid, NT, 0, s>>>(a);
   else if (full)
-    rotary_kernel<T, false, true><<<dim3(grid), NT, 0, s>>>(a);
+    rotary_kernel<T, L, U, false, true><<<grid, NT, 0, s>>>(a);
   else
-    rotary_kernel<T, false, false><<<dim3(grid), NT, 0, s>>>(a);
+    rotary_kernel<T, L, U, false, false><<<grid, NT, 0, s>>>(a);
   return hipGetLastError();
+}
+
+// Lanes a token: as many as it has items for (57 x 1257 tokens, three heads and three
+// key heads of 80 dims, 30 items: a pass of both directions with 64 lanes 120, with 32
+// 63 us).
+template <typename T> hipError_t launch(const RotaryArgs& a, bool full, hipStream_t s) {
+  if (a.items > 64) return launch<T, 64, 2>(a, full, s);
+  if (a.items > 32 || a.half > MAX_PAIRS / 2) return launch<T, 64, 1>(a, full, s);
+  if (a.items > 16 || a.half > MAX_PAIRS / 4) return launch<T, 32, 1>(a, full, s);
+  return launch<T, 16, 1>(a, full, s);
 }
 
 }  // namespace
@@ -164,17 +184,8 @@ hipError_t launch_rotary(RotaryArgs a, int dtype, hipStream_t s) {
   const int parts = a.turned + (copied + 15) / 16;
   a.parts = Divisor::of(parts);
   a.items = parts * (a.heads[0] + a.heads[1] + a.heads[2]);
-  a.dq = 64 / parts;
-  a.dr = 64 % parts;
-  // few tokens: several waves share one, down to 64 items each
-  const int steps = (a.items + 63) / 64;
-  const int waves = std::max(1, std::min(steps, 4096 / std::min(4096, a.n_tokens)));
-  a.per = 64 * ((steps + waves - 1) / waves);
-  a.waves = Divisor::of((a.items + a.per - 1) / a.per);
-  const int64_t jobs = int64_t(a.n_tokens) * a.waves.d;
-  const int grid = int(std::min<int64_t>((jobs + 3) / 4, 1 << 20));
   const bool full = a.half % 8 == 0 && copied % 16 == 0;
-  return dtype == ABFT_BF16 ? launch<bf16_t>(a, full, grid, s) : launch<float>(a, full, grid, s);
+  return dtype == ABFT_BF16 ? launch<bf16_t>(a, full, s) : launch<float>(a, full, s);
 }
 
 }  // namespace abft

@@ -27,7 +27,8 @@ struct RotaryArgs {
   int32_t append = 0;             // keys and values go to their positions ...
   int32_t capacity = 0;           // ... below this one
   // work: items of a token are parts (16 dims) of heads, `turned` ones in front; a
-  // wave takes `per` of them, `waves` waves a token; 64 items are dq heads and dr parts
+  // group of lanes takes `per` of them, `waves` groups a token; as many items as it has
+  // lanes are dq heads and dr parts
   int32_t turned = 0, items = 0, per = 0, dq = 0, dr = 0;
   Divisor parts, waves;
 };

@@ -55,6 +55,8 @@ struct DropoutArgs {
   DropArgs drop;
   int32_t rows = 0, cols = 0;
   Divisor tokens, chunks;      // chunks: of a row
+  int32_t flat = 0;            // all tensors are whole chunks, one behind the other, at
+                               // multiples of 16 bytes
 };
 
 // Columns up to which less than a wave shares a row of whole chunks.
@@ -90,6 +92,9 @@ template <> struct Chunk<bf16_t> {
     r = *reinterpret_cast<const u32x4_at2*>(p);
   }
   __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<u32x4_at2*>(p) = r; }
+  __device__ __forceinline__ void store_past(bf16_t* p) const {  // past the cache, aligned
+    __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(p));
+  }
   __device__ __forceinline__ float get(int e) const {
     return __uint_as_float(e % 2 ? r[e / 2] & 0xffff0000u : r[e / 2] << 16);
   }
@@ -116,6 +121,10 @@ template <> struct Chunk<float> {
   __device__ __forceinline__ void store(float* p) const {
     reinterpret_cast<u32x4_at4*>(p)[0] = r[0];
     reinterpret_cast<u32x4_at4*>(p)[1] = r[1];
+  }
+  __device__ __forceinline__ void store_past(float* p) const {
+    __builtin_nontemporal_store(r[0], reinterpret_cast<u32x4*>(p));
+    __builtin_nontemporal_store(r[1], reinterpret_cast<u32x4*>(p) + 1);
   }
   __device__ __forceinline__ float get(int e) const { return __uint_as_float(r[e / 4][e % 4]); }
   __device__ __forceinline__ void set(const float (&v)[8]) {
