@@ -155,12 +155,12 @@ template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t
   return with_lines((a.cols + 7) / 8, [&](auto shape, ShapeAt at) {
     using S = decltype(shape);
     const int64_t wgs = (int64_t(a.rows) + at.rows - 1) / at.rows;
-    // Waves at a time, by what a lane holds (8192 x 768, three chunks: in 512 workgroups
-    // 7.4, in 1024 7.9 us; 8192 x 2048, two: in 2048 14.8, in 1024 17.2 us), and the
-    // same number of rows for each workgroup.
-    constexpr int WAVES[] = {8192, 5120, 2048};
-    const int64_t most = WAVES[S::NV - 1] / (at.threads() / 64), turns = (wgs + most - 1) / most;
-    const dim3 grid(int((wgs + turns - 1) / turns));
+    // Waves of a CU, by what a lane holds (8192 x 768, three chunks: 8 waves 7.4, 16 7.9
+    // us; 8192 x 2048, two: 16 waves 14.8, 8 17.2 us), in whole workgroups: every CU has
+    // the same number (8192 x 11072, 11 waves a row: 512 workgroups 73.5, 465 80.8 us).
+    constexpr int WAVES[] = {32, 20, 8};
+    const int waves = at.threads() / 64, each = std::max(1, (WAVES[S::NV - 1] + waves / 2) / waves);
+    const dim3 grid(int(std::min<int64_t>(wgs, 256 * each)));
     if (a.lines)
       norm_fwd_kernel<T, S, KIND, true><<<grid, at.threads(), 0, s>>>(a, at);
     else
