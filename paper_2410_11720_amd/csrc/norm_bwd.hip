@@ -35,11 +35,15 @@ template <typename T, typename S, int KIND, bool LINES> struct BwdLine {
   }
 };
 
-// The row after the present one is read ahead.
+// The row after the present one is read ahead. Rows above 8192 columns take up to 1024
+// lanes of two chunks, 128 registers each: there g and xh are formed twice from what
+// was read, and only bf16 rows without a residual are read ahead (4096 x 16384, with
+// spills before: bf16 with residual and dropout 253 -> 144, fp32 alone 243 -> 162 us).
 template <typename T, typename S, int KIND, bool LINES>
 __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
   constexpr int NV = S::NV;
+  constexpr bool WIDE = S::LPR == 0 && NV > 1, AHEAD = !WIDE || (sizeof(T) == 2 && KIND == NORM_ALONE);
   __shared__ float2 sh[2][16];
   extern __shared__ float4 sums[];   // [rows][lanes NV][2] where there are several rows
   const Place<T, S> p(shape.lanes, a.cols);
@@ -47,7 +51,7 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
   const int step = gridDim.x * shape.rows;
   int row = blockIdx.x * shape.rows + p.slot, turn = 0;
   BwdLine<T, S, KIND, LINES> cur, next;
-  if (a.rows > 0) cur.read(a, p, row);
+  if (AHEAD && a.rows > 0) cur.read(a, p, row);
   uint64_t seed = 0, offset = 0;
   if constexpr (KIND == NORM_DROPOUT) {
     seed = a.drop.rng[0];
@@ -63,35 +67,46 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
   }
   const float inv_n = 1.f / float(a.cols);
   // (the workgroup's waves take as many turns: they meet in the sums)
-  for (int first = blockIdx.x * shape.rows; first < a.rows; first += step, row += step, cur = next) {
-    next.read(a, p, row + step);
+  for (int first = blockIdx.x * shape.rows; first < a.rows; first += step, row += step) {
+    if constexpr (AHEAD)
+      next.read(a, p, row + step);
+    else
+      cur.read(a, p, row);
     const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
     const Line<T, S, LINES> px(a.dx, at, row < a.rows, a.cols);
     const Line<T, S, LINES> pr(a.dres, at, row < a.rows, a.cols);
     const float mean = cur.st.x, r = cur.st.y;
-    float g[NV][8], xh[NV][8];
+    float g[WIDE ? 1 : NV][8], xh[WIDE ? 1 : NV][8];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       // (what is not in the row is 0 in dy)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = cur.dy[j].get(e);
-        xh[j][e] = (cur.h[j].get(e) - mean) * r;
-        g[j][e] = d * w[j][e];
-        dw[j][e] = fmaf(d, xh[j][e], dw[j][e]);
+        const float d = cur.dy[j].get(e), x = (cur.h[j].get(e) - mean) * r, gw = d * w[j][e];
+        dw[j][e] = fmaf(d, x, dw[j][e]);
         db[j][e] += d;
-        s.x += g[j][e];
-        s.y = fmaf(g[j][e], xh[j][e], s.y);
+        s.x += gw;
+        s.y = fmaf(gw, x, s.y);
+        if constexpr (!WIDE) {
+          xh[j][e] = x;
+          g[j][e] = gw;
+        }
       }
     s = line_sum<S>(s, sh, waves, p.slot, turn);
     const float c1 = s.x * inv_n, c2 = s.y * inv_n;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      if constexpr (WIDE) {
+        cur.dy[j].anew();
+        cur.h[j].anew();
+      }
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        o[e] = r * fmaf(-xh[j][e], c2, g[j][e] - c1);
+        const float x = WIDE ? (cur.h[j].get(e) - mean) * r : xh[j][e];
+        const float gw = WIDE ? cur.dy[j].get(e) * w[j][e] : g[j][e];
+        o[e] = r * fmaf(-x, c2, gw - c1);
         if constexpr (KIND != NORM_ALONE) o[e] += cur.dh[j].get(e);
       }
       Chunk<T> c;
@@ -104,6 +119,7 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
       if constexpr (KIND != NORM_RESIDUAL) c.set(o);
       px.store(c, p, j);
     }
+    if constexpr (AHEAD) cur = next;
   }
   if (!a.dweight && !a.dbias) return;
   // the workgroup's sums: over its rows at a time, in their order

@@ -109,6 +109,11 @@ template <> struct Chunk<bf16_t> {
 #pragma unroll
     for (int k = 0; k < 4; ++k) r[k] = yes ? r[k] : 0;
   }
+  // What is computed from it anew is not kept from before.
+  __device__ __forceinline__ void anew() {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(r[k]));
+  }
   __device__ __forceinline__ bf16_t at(int e) const { return bf16_t(r[e / 2] >> (e % 2 * 16)); }
 };
 template <> struct Chunk<float> {
@@ -135,6 +140,10 @@ template <> struct Chunk<float> {
   __device__ __forceinline__ void keep(bool yes) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) r[k / 4][k % 4] = yes ? r[k / 4][k % 4] : 0;
+  }
+  __device__ __forceinline__ void anew() {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(r[k / 4][k % 4]));
   }
   __device__ __forceinline__ float at(int e) const { return get(e); }
 };

@@ -210,6 +210,22 @@ def test_strides_in_place_and_alignment():
 
 
 @pytest.mark.gpu
+def test_python_refusals():
+    op = abft.Dropout(abft.DropoutConfig(2, 3, 40))
+    x, rng = _rows((2, 3, 40), "bf16", 7), _rng(1, 2)
+    wide = torch.zeros((2, 3, 80), dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: op.forward(x), lambda: op.forward(x, rng.int()), lambda: op.forward(x, rng[:1]),
+                 lambda: op.forward(x, rng.cpu()), lambda: op.forward(x.float(), rng),
+                 lambda: op.forward(x.cpu(), rng), lambda: op.forward(x[:, :, :39], rng),
+                 lambda: op.forward(x, rng, residual=x.float()), lambda: op.forward(wide[:, :, ::2], rng),
+                 lambda: op.forward(x, rng, y=x.float()), lambda: op.backward(x),
+                 lambda: op.forward(wide[:, :, :40], rng, y=wide[:, :, 8:48]),
+                 lambda: op.forward(x, rng, y=x[:1].expand(2, 3, 40))):
+        with pytest.raises(abft.AbftError):
+            call()
+
+
+@pytest.mark.gpu
 def test_what_tells_draws_apart():
     """Other seeds, offsets (high words too), sites and rows draw other masks, whose
     agreement is that of independent ones; a share of t / 65536 is dropped. Bounds of

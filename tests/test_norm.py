@@ -488,6 +488,39 @@ def test_records():
 
 
 @pytest.mark.gpu
+def test_python_refusals():
+    """Other types, shapes, devices and layouts than the configuration's, and results on
+    arguments."""
+    cfg = abft.NormConfig(2, 3, 64, dropout=0.25)
+    d = _inputs(cfg, 31)
+    op, plain = abft.ResidualNorm(cfg), abft.LayerNorm(abft.NormConfig(2, 3, 64))
+    x, res, w, b, rng = (d[k] for k in ("x", "res", "w", "b", "rng"))
+    h, _ = op.forward(x, res, w, b, rng=rng)
+    wide = torch.zeros((2, 3, 128), dtype=x.dtype, device="cuda")
+    bad = [lambda: op.forward(x.float(), res, w, b, rng=rng), lambda: op.forward(x, res.cpu(), w, b, rng=rng),
+           lambda: op.forward(x[:, :2], res, w, b, rng=rng), lambda: op.forward(x, None, w, b, rng=rng),
+           lambda: op.forward(x, res, w[:63], b, rng=rng), lambda: op.forward(x, res, w.bfloat16(), b, rng=rng),
+           lambda: op.forward(x, res, w, b), lambda: op.forward(x, res, w, b, rng=rng.int()),
+           lambda: op.forward(x, res, w, b, rng=rng.cpu()),
+           lambda: op.forward(wide[:, :, ::2], res, w, b, rng=rng),
+           lambda: op.forward(x, res, w, b, rng=rng, lens=torch.ones(3, dtype=torch.int32, device="cuda")),
+           lambda: op.forward(x, res, w, b, rng=rng, lens=torch.ones(2, device="cuda")),
+           lambda: op.forward(x, res, w, b, rng=rng, h=wide[:, :, :64], y=wide[:, :, 32:96]),
+           lambda: op.forward(wide[:, :, :64], res, w, b, rng=rng, y=wide[:, :, 8:72]),
+           lambda: op.backward(d["dy"], h, w), lambda: op.backward(d["dy"].float(), h, w, rng=rng),
+           lambda: op.backward(d["dy"], h, w, rng=rng, dweight=w.bfloat16()),
+           lambda: op.backward(d["dy"], h, w, rng=rng, dbias=op.stats.view(-1)[:64]),
+           lambda: op.backward(d["dy"], x, w, rng=rng), lambda: plain.backward(d["dy"], x, w),
+           lambda: plain.forward(x, w, y=x[:, :, :0])]
+    for call in bad:
+        with pytest.raises(abft.AbftError):
+            call()
+    # an output that a call refused is no record of a forward
+    with pytest.raises(abft.AbftError):
+        plain.backward(d["dy"], x, w)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("cols", [64, 768, 5120])
 def test_runs_repeat_and_captured_calls_replay(cols):
     """A captured step draws anew once its state has advanced, and leaves what the

@@ -270,6 +270,24 @@ def test_append(tokens, starts, dtype, interleaved):
 
 
 @pytest.mark.gpu
+def test_python_refusals():
+    rot = abft.Rotary(C(2, 3, 4, 16, kv_heads=2))
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+    q, k, kc, vc = z(2, 3, 4, 16), z(2, 3, 2, 16), z(2, 9, 2, 16), z(2, 9, 2, 16)
+    for call in (lambda: rot.forward(q, q), lambda: rot.forward(q.float(), k), lambda: rot.forward(q.cpu(), k),
+                 lambda: rot.forward(q[:, :2], k), lambda: rot.forward(q.transpose(2, 3), k),
+                 lambda: rot.forward(z(2, 3, 4, 32)[..., ::2], k),
+                 lambda: rot.forward(q, k, q_start=_start([1, 2, 3])),
+                 lambda: rot.forward(q, k, q_start=_start([1, 2]).long()),
+                 lambda: rot.forward(q, k, Q_out=q[:, :1].expand(2, 3, 4, 16)),
+                 lambda: rot.forward(q, q[:, :, :2], Q_out=q),                 # keys in what is written
+                 lambda: rot.append(q, k, k, kc, kc), lambda: rot.append(q, k, k, kc, vc[:, :8]),
+                 lambda: rot.append(q, kc[:, :3], k, kc, vc), lambda: rot.append(q, k, k, kc.float(), vc)):
+        with pytest.raises(abft.AbftError):
+            call()
+
+
+@pytest.mark.gpu
 def test_a_long_cache():
     """Rows further than 2^32 bytes into a cache."""
     cfg = C(1, 2, 4, 128, kv_heads=2, dtype="f32")
