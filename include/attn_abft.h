@@ -474,7 +474,8 @@ int clip_gradients(const abft_grad* grads, int32_t n, double max_norm, abft_grad
  * pass the extent of the one before. An output may be one of the call's inputs of
  * this type (same data and strides), and shares no memory with any other argument
  * (ABFT_ERR_INVALID). Strides of dimensions of extent 1 and tensors without
- * elements are not looked at. batch * tokens < 2^31. */
+ * elements are not looked at. batch * tokens is at most 2^31 - 2^20, here and for
+ * rotary positions (ABFT_ERR_UNSUPPORTED). */
 typedef struct {
   const void* data;
   int64_t batch_stride, token_stride;

@@ -925,7 +925,8 @@ class _Norm(_Op):
         return saved
 
     def _forward(self, rows, weight, bias, lens, rng, saved, of):
-        """rows: of x, residual, h, y; of: where the norm's rows are."""
+        """rows: of x, residual, h, y; of: what holds the norm's rows (None: y does not
+        leave them)."""
         x, r, h, y = rows
         saved = self._saved if saved is None else self._record(saved)
         stats = None
@@ -936,7 +937,7 @@ class _Norm(_Op):
                      self._vector(bias, "bias", self._cols, self._wdtype),
                      self._vector(lens, "lens", self._shape[:1], torch.int32), rng, h, y, stats),
                "attn_norm_forward")
-        if saved is not None:
+        if saved is not None and of is not None:
             saved._of = of.data_ptr()
 
     def _of(self, saved, h):
@@ -981,7 +982,7 @@ class LayerNorm(_Norm):
     weight and bias [cols] may be None (1 and 0); lens [batch] int32: tokens of
     each sequence, behind them nothing is read and results are 0. Any strides with
     contiguous columns; results not given are laid out as torch.empty_like of x or
-    dy, and may be an input (in place; y on x only where no backward follows)."""
+    dy, and may be an input (in place; y on x leaves no record for a backward)."""
 
     def __init__(self, cfg: NormConfig, device="cuda", training=True):
         if cfg.dropout != 0.0:
@@ -994,7 +995,8 @@ class LayerNorm(_Norm):
             held, (x_, y_) = self._records(("x",), (x,), self._shapes, (y,))
         else:
             held, (x_, y_) = self._records(("x", "y"), (x, y), self._shapes)
-        self._forward((x_, None, None, y_), weight, bias, lens, None, saved, x)
+        kept = x if y.data_ptr() != x.data_ptr() else None
+        self._forward((x_, None, None, y_), weight, bias, lens, None, saved, kept)
         return y
 
     def backward(self, dy, x, weight=None, lens=None, dx=None, dweight=None, dbias=None, saved=None):

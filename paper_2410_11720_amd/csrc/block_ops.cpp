@@ -13,6 +13,7 @@ namespace {
 
 constexpr int MAX_NORM_COLS = 16384;      // a row fits a workgroup's registers
 constexpr int MAX_DROP_COLS = 65536;      // a chunk's number fits the counter's 13 bits
+constexpr int64_t MAX_ROWS = 0x7ff00000;  // a row's number and one turn of a grid fit 31 bits
 constexpr int MAX_SITE = 65536;
 constexpr int MAX_HEAD_DIM = 512;
 constexpr int MAX_HEADS = 65536;          // of queries, keys and values together
@@ -100,7 +101,7 @@ int take_rows(int batch, int tokens, int cols, int dtype, const attn_rows* t, bo
 
 int sizes_ok(int batch, int tokens, int cols, int most_cols) {
   if (batch < 0 || tokens < 0 || cols < 1) return ABFT_ERR_INVALID;
-  if (cols > most_cols || int64_t(batch) * tokens > 0x7fffffff) return ABFT_ERR_UNSUPPORTED;
+  if (cols > most_cols || int64_t(batch) * tokens > MAX_ROWS) return ABFT_ERR_UNSUPPORTED;
   return ABFT_OK;
 }
 
@@ -166,7 +167,7 @@ int valid_rotary(const attn_rotary_config* c) {
   if (c->interleaved != 0 && c->interleaved != 1) return ABFT_ERR_INVALID;
   if (!std::isfinite(c->magnitude)) return ABFT_ERR_INVALID;
   if (c->head_dim > MAX_HEAD_DIM || int64_t(c->heads) + 2 * int64_t(c->kv_heads) > MAX_HEADS ||
-      int64_t(c->batch) * c->tokens > 0x7fffffff)
+      int64_t(c->batch) * c->tokens > MAX_ROWS)
     return ABFT_ERR_UNSUPPORTED;
   return ABFT_OK;
 }

@@ -24,6 +24,7 @@ def _cfg(**kw):
 
 @pytest.mark.parametrize("kw", [dict(batch=-1), dict(tokens=-1), dict(cols=0), dict(cols=-5),
                                 dict(cols=16385), dict(batch=2 ** 16, tokens=2 ** 15),
+                                dict(batch=2 ** 11 - 1, tokens=2 ** 20 + 1),
                                 dict(eps=0.0), dict(eps=math.nan), dict(eps=math.inf),
                                 dict(eps=1e-31), dict(dropout=-0.1), dict(dropout=1.5),
                                 dict(dropout=math.nan), dict(site=65536), dict(dtype="f16"),
@@ -39,6 +40,7 @@ def test_workspace_bytes():
     # (512 workgroups at most, each with both sums)
     assert abft.attn_norm_workspace_bytes(_cfg(batch=64, tokens=4096, cols=16384)) <= 512 * 2 * 16384 * 4
     assert abft.attn_norm_workspace_bytes(_cfg(batch=0)) > 0
+    assert abft.attn_norm_workspace_bytes(_cfg(batch=2 ** 11 - 1, tokens=2 ** 20)) > 0
 
 
 G = 1 << 30
@@ -483,6 +485,11 @@ def test_records():
         op.backward(d["dy"], d["x"], d["w"])
     got = op.backward(d["dy"], d["x"], d["w"], saved=one)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+    x = d["x"].clone()             # y on x: its rows are gone, and so is the record
+    assert torch.equal(op.forward(x, d["w"], d["b"], y=x), op.forward(d["x"], d["w"], d["b"]))
+    op.forward(x, d["w"], d["b"], y=x)
+    with pytest.raises(abft.AbftError):
+        op.backward(d["dy"], x, d["w"])
     with pytest.raises(abft.AbftError):
         op.forward(d["x"], saved=abft.LayerNorm(abft.NormConfig(2, 4, 64)).new_saved())
 

@@ -270,6 +270,35 @@ def test_append(tokens, starts, dtype, interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("heads,kv_heads,rotary_dim", [(3, 0, 32), (0, 2, 32), (3, 2, 0), (0, 2, 0)])
+def test_c_calls_without_queries_keys_or_turned_dims(heads, kv_heads, rotary_dim):
+    cfg = C(2, 5, 3, 40, kv_heads=2)
+    q, k, v = _inputs(cfg, 13)
+    c = abft.RotaryConfigC(2, 5, heads, kv_heads, 40, rotary_dim, 0, 0, 1.0)
+    rot = abft.Rotary(C(2, 5, 3, 40, kv_heads=2, rotary_dim=32))
+    tq, tk = rot.forward(q, k)
+    if rotary_dim == 0:
+        tq, tk = q, k
+    at = lambda t: ctypes.byref(abft.CrossTensor(t.data_ptr(), *t.stride()[:3]))
+    null = ctypes.byref(abft.CrossTensor(None, 0, 0, 0))
+    freqs = rot.freqs.data_ptr() if rotary_dim else None
+    qo, ko, vo = (torch.full_like(t, 7.0) for t in (q, k, v))
+    stream = torch.cuda.current_stream().cuda_stream
+    args = [at(t) if n else null for t, n in ((q, heads), (k, kv_heads))]
+    outs = [at(t) if n else null for t, n in ((qo, heads), (ko, kv_heads))]
+    assert abft._lib.attn_rotary(c, 0, *args, freqs, None, *outs, stream) == 0
+    assert torch.equal(qo, tq if heads else torch.full_like(q, 7.0))
+    assert torch.equal(ko, tk if kv_heads else torch.full_like(k, 7.0))
+    qo.fill_(7.0), ko.fill_(7.0)
+    args.append(at(v) if kv_heads else null)
+    outs.append(at(vo) if kv_heads else null)
+    assert abft._lib.attn_rotary_append(c, *args, freqs, None, 5, *outs, stream) == 0
+    assert torch.equal(qo, tq if heads else torch.full_like(q, 7.0))
+    assert torch.equal(ko, tk if kv_heads else torch.full_like(k, 7.0))
+    assert torch.equal(vo, v if kv_heads else torch.full_like(v, 7.0))
+
+
+@pytest.mark.gpu
 def test_python_refusals():
     rot = abft.Rotary(C(2, 3, 4, 16, kv_heads=2))
     z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
