@@ -270,8 +270,8 @@ int attn_norm_forward(const attn_norm_config* cfg, const attn_rows* x, const att
   TRY(valid_norm(cfg));
   NormArgs a;
   TRY(take_drop(cfg->dropout, cfg->site, rng, &a.drop));
-  const bool sum = residual && residual->data;
-  if (!sum && (a.drop.threshold || (h && h->data))) return ABFT_ERR_INVALID;
+  const bool sum = residual && residual->data, none = cfg->batch == 0 || cfg->tokens == 0;
+  if (!none && !sum && (a.drop.threshold || (h && h->data))) return ABFT_ERR_INVALID;
   TRY(common(cfg, weight, bias, lens, &a));
   if (reinterpret_cast<uintptr_t>(stats) % 8) return ABFT_ERR_INVALID;
   const int B = cfg->batch, S = cfg->tokens, H = cfg->cols, dt = cfg->dtype;

@@ -79,11 +79,14 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
     float g[WIDE ? 1 : NV][8], xh[WIDE ? 1 : NV][8];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      // (what is not in the row is 0 in dy)
+    for (int j = 0; j < NV; ++j) {
+      // (what is not in the row is 0 in dy, and must not be INF in xh)
+      const float from = p.has(j) ? mean : 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = cur.dy[j].get(e), x = (cur.h[j].get(e) - mean) * r, gw = d * w[j][e];
+        const float d = cur.dy[j].get(e), gw = d * w[j][e];
+        float x = (cur.h[j].get(e) - from) * r;
+        if (!LINES && p.col(j) + e >= a.cols) x = 0.f;
         dw[j][e] = fmaf(d, x, dw[j][e]);
         db[j][e] += d;
         s.x += gw;
@@ -93,6 +96,7 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
           g[j][e] = gw;
         }
       }
+    }
     s = line_sum<S>(s, sh, waves, p.slot, turn);
     const float c1 = s.x * inv_n, c2 = s.y * inv_n;
 #pragma unroll

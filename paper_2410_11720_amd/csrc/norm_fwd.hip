@@ -118,8 +118,11 @@ __global__ __launch_bounds__(S::LPR ? 256 : 1024) void norm_fwd_kernel(NormArgs 
           s.x += v[j][e];
         }
     }
-    const float r = 1.f / sqrtf(scale == 1.f ? var + a.eps : var);
-    const float2 st = cur.ok ? make_float2(mean / scale, r * scale) : make_float2(0.f, 0.f);
+    // (a scaled row has a variance far above eps, or is one value throughout: 0 there)
+    const bool one = scale != 1.f && var == 0.f;
+    const float r = one ? 0.f : 1.f / sqrtf(scale == 1.f ? var + a.eps : var);
+    const float inv = one ? 1.f / sqrtf(a.eps) : r * scale;
+    const float2 st = cur.ok ? make_float2(mean / scale, inv) : make_float2(0.f, 0.f);
     if constexpr (LINES)
       __builtin_amdgcn_raw_buffer_store_b64(
           __builtin_bit_cast(u32x2, st), bytes_at(a.stats, a.stats ? a.rows * 8u : 0u),

@@ -14,8 +14,8 @@ READELF = shutil.which("llvm-readelf", path=PATH)
 # bytes of scratch a lane: type (f: fp32, t: bf16), what stands in front of the norm, whole
 # chunks. All of rows above 8192 columns, whose lanes hold the sums of two chunks in 128
 # registers
-SPILLS = {("t", 0, 1): 8, ("t", 0, 0): 36, ("t", 2, 0): 44, ("f", 1, 1): 12, ("f", 1, 0): 40,
-          ("f", 2, 1): 76, ("f", 2, 0): 108}
+SPILLS = {("t", 0, 1): 8, ("t", 0, 0): 36, ("t", 2, 0): 52, ("f", 1, 1): 20, ("f", 1, 0): 60,
+          ("f", 2, 1): 76, ("f", 2, 0): 124}
 
 
 @pytest.fixture(scope="module")

@@ -276,7 +276,7 @@ def test_strides_and_alignment(dtype, cols):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("cols", [8, 100, 768, 1025, 16000])
-@pytest.mark.parametrize("value", [0.0, 1.0, 1000.0, -3e4])
+@pytest.mark.parametrize("value", [0.0, 1.0, 1000.0, -3e4, 1e20, -1e30, 2.0 ** 125, -2.0 ** 127])
 def test_rows_of_one_value(cols, value):
     """Variance 0: y is the offset (the mean's rounding does not pass for a
     difference), and the gradient is that of deviation sqrt(eps)."""
@@ -286,7 +286,12 @@ def test_rows_of_one_value(cols, value):
         x = torch.full_like(d["x"], value)
         op = abft.LayerNorm(cfg)
         assert torch.equal(op.forward(x, d["w"], d["b"]), d["b"].to(x.dtype).expand_as(x).contiguous())
-        assert torch.isfinite(op.backward(d["dy"], x, d["w"])[0]).all()
+        dx, dw, db = op.backward(d["dy"], x, d["w"])
+        g = d["dy"].double() * d["w"].double()
+        want = (g - g.mean(dim=2, keepdim=True)) / math.sqrt(cfg.eps)
+        size = g.abs() + g.abs().mean(dim=2, keepdim=True)
+        R.check("dx", dx, want, R.stored(want, (R.K + 8) * R.U * size / math.sqrt(cfg.eps), x.dtype))
+        assert (dw == 0).all()
 
 
 @pytest.mark.gpu
@@ -330,6 +335,22 @@ def test_values_that_are_not_finite_stay_in_their_row(bad, cols):
     assert y[1, 4].isnan().all() and dx[1, 4].isnan().all() and dw.isnan().all()
     assert torch.equal(y[rest], y0[rest]) and torch.equal(dx[rest], dx0[rest])
     assert torch.isfinite(db).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,tokens", [(0, 3), (2, 0), (0, 0)])
+def test_no_rows(batch, tokens):
+    """Parameter gradients of nothing are 0."""
+    cfg = abft.NormConfig(batch, tokens, 100, dropout=0.5)
+    d = _inputs(cfg, 14)
+    op = abft.ResidualNorm(cfg)
+    op.workspace.fill_(255)
+    h, y = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
+    dx, dr, dw, db = op.backward(d["dy"], h, d["w"], dh=d["dh"], rng=d["rng"])
+    assert h.shape == y.shape == dx.shape == dr.shape == (batch, tokens, 100)
+    assert (dw == 0).all() and (db == 0).all()
+    drop = abft.Dropout(abft.DropoutConfig(batch, tokens, 100))
+    assert drop.forward(d["x"], d["rng"], residual=d["res"]).numel() == 0
 
 
 @pytest.mark.gpu
