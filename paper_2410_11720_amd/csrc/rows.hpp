@@ -248,7 +248,7 @@ __device__ __forceinline__ void load_params(float (&v)[8], const void* p, int bf
 // stored there: a lane without a chunk, a row behind a sequence's length or behind
 // the last one, a tensor that is not given need no branch. With branches around them
 // the compiler cannot count what is in flight, and waits for the next row's loads and
-// for all stores where it needs this row's (norm of 8192 x 768: forward 8.2 -> 7.0
+// for all stores where it needs this row's (norm of 8192 x 768: forward 8.2 -> 7.4
 // us). Other rows take those branches; what lies where and the order of sums are the
 // same, and so are the results' bits.
 

@@ -609,27 +609,51 @@ def test_two_streams_at_once():
 
 
 @pytest.mark.gpu
-def test_offsets_past_32_bits():
-    """Rows of one buffer further than 2^32 bytes apart."""
-    cfg = abft.NormConfig(2, 3, 768, dropout=0.5)
+@pytest.mark.parametrize("cols", [768, 1024, 1001])
+def test_offsets_past_32_bits(cols):
+    """Sequences of one buffer further than 2^32 bytes apart."""
+    cfg = abft.NormConfig(2, 3, cols, dropout=0.5)
     d = _inputs(cfg, 29)
     op = abft.ResidualNorm(cfg)
     h0, y0 = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
     want = op.backward(d["dy"], h0, d["w"], dh=d["dh"], rng=d["rng"])
-    big = torch.zeros(5 * 2 ** 30, dtype=torch.bfloat16, device="cuda")   # 10 GiB
+    big = torch.zeros(2 ** 31 + 2 ** 23, dtype=torch.bfloat16, device="cuda")
 
-    def far(t, at):
-        v = big.as_strided((2, 3, 768), (2 ** 31 + 4096, 2 ** 20, 1), at)
+    def far(k, t=None):
+        v = big.as_strided((2, 3, cols), (2 ** 31 + 4096, 2 ** 20, 1), 1024 * k)
         if t is not None:
             v.copy_(t)
         return v
-    x, res, h, y = far(d["x"], 0), far(d["res"], 768), far(None, 2 * 768), far(None, 3 * 768)
-    op.forward(x, res, d["w"], d["b"], rng=d["rng"], h=h, y=y)
+    h, y = far(2), far(3)
+    op.forward(far(0, d["x"]), far(1, d["res"]), d["w"], d["b"], rng=d["rng"], h=h, y=y)
     assert torch.equal(h, h0) and torch.equal(y, y0)
-    dx, dr = far(None, 4 * 768), far(None, 5 * 768)
-    got = op.backward(far(d["dy"], 6 * 768), h, d["w"], dh=far(d["dh"], 7 * 768), rng=d["rng"], dx=dx,
-                      dresidual=dr)
+    got = op.backward(far(6, d["dy"]), h, d["w"], dh=far(7, d["dh"]), rng=d["rng"], dx=far(4),
+                      dresidual=far(5))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_many_rows():
+    """More rows than offsets of statistics have 31 bits for, and the most there may be."""
+    rows = 2 ** 28 + 5
+    cfg = abft.NormConfig(1, rows, 4)
+    x = torch.randn((1, 4096, 4), device="cuda").bfloat16().repeat(1, rows // 4096 + 1, 1)[:, :rows]
+    op = abft.LayerNorm(cfg)
+    y = op.forward(x)
+    want, bound, _ = R.norm(x[:, -4096:], None, None, cfg.eps, None, torch.bfloat16)
+    R.check("y", y[:, -4096:], want, bound)
+    assert torch.equal(y[:, :4096], y[:, 4096:8192]) and torch.equal(y[:, :rows - 4096], y[:, 4096:])
+    assert torch.equal(op.stats[:, :rows - 4096], op.stats[:, 4096:])
+    dx, dw, db = op.backward(y, x)
+    assert torch.equal(dx[:, :rows - 4096], dx[:, 4096:])
+    # (a lane adds 2^28 / 512 / 32 rows: 2^14 roundings)
+    assert (db - y.double().sum(dim=(0, 1))).abs().max() <= 2 ** -10 * y.double().abs().sum() / 4
+    del x, y, dx, op
+    most = 0x7ff00000
+    x = torch.ones((1, most, 1), dtype=torch.bfloat16, device="cuda")
+    op = abft.LayerNorm(abft.NormConfig(1, most, 1), training=False)
+    op.forward(x, y=x)
+    assert not x.any()
 
 
 @pytest.mark.gpu
