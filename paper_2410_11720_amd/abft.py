@@ -797,8 +797,10 @@ class _Op:
         return t.data_ptr()
 
     def _state(self, rng, used):
-        if rng is None and used:
-            raise AbftError("rng: dropout needs its seed and offset")
+        if rng is None:
+            if used:
+                raise AbftError("rng: dropout needs its seed and offset")
+            return None
         return self._vector(rng, "rng", (2,), torch.int64)
 
 
@@ -928,6 +930,8 @@ class _Norm(_Op):
         """rows: of x, residual, h, y; of: what holds the norm's rows (None: y does not
         leave them)."""
         x, r, h, y = rows
+        if lens is not None:
+            lens = self._vector(lens, "lens", self._shape[:1], torch.int32)
         saved = self._saved if saved is None else self._record(saved)
         stats = None
         if saved is not None:
@@ -935,7 +939,7 @@ class _Norm(_Op):
         _check(_call(_lib.attn_norm_forward, self.device, self._c, x, r,
                      self._vector(weight, "weight", self._cols, self._wdtype),
                      self._vector(bias, "bias", self._cols, self._wdtype),
-                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, h, y, stats),
+                     lens, rng, h, y, stats),
                "attn_norm_forward")
         if saved is not None and of is not None:
             saved._of = of.data_ptr()
@@ -955,17 +959,21 @@ class _Norm(_Op):
     def _backward(self, rows, weight, lens, rng, dweight, dbias, saved):
         """rows: of dy, dh, h, dx, dresidual."""
         dy, dh, h, dx, dr = rows
-        dw, db = (self._vector(t, name, self._cols, torch.float32)
-                  for t, name in ((dweight, "dweight"), (dbias, "dbias")))
+        if lens is not None:
+            lens = self._vector(lens, "lens", self._shape[:1], torch.int32)
         if dweight is None:
             dweight = torch.empty_like(self._sums)
             dw = dweight.data_ptr()
+        else:
+            dw = self._vector(dweight, "dweight", self._cols, torch.float32)
         if dbias is None:
             dbias = torch.empty_like(self._sums)
             db = dbias.data_ptr()
+        else:
+            db = self._vector(dbias, "dbias", self._cols, torch.float32)
         _check(_call(_lib.attn_norm_backward, self.device, self._c, dy, dh, h,
                      self._vector(weight, "weight", self._cols, self._wdtype), saved.stats.data_ptr(),
-                     self._vector(lens, "lens", self._shape[:1], torch.int32), rng, dx, dr, dw, db,
+                     lens, rng, dx, dr, dw, db,
                      self.workspace.data_ptr(), self.workspace.numel()), "attn_norm_backward")
         return dweight, dbias
 

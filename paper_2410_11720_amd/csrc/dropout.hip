@@ -93,13 +93,10 @@ template <typename T, bool RES> hipError_t launch(const DropoutArgs& a, hipStrea
   const int64_t chunks = int64_t(a.rows) * a.chunks.d;
   const int64_t per = a.flat ? NT * U : NT, tiles = (chunks + per - 1) / per;
   const dim3 grid(int(std::min<int64_t>(tiles, 1 << 20)));
-  if (!a.flat)
-    dropout_rows<T, RES><<<grid, NT, 0, s>>>(a, tiles);
-  else if (chunks * 8 * int64_t(sizeof(T)) < PAST_BYTES)
-    dropout_flat<T, RES, false><<<grid, NT, 0, s>>>(a, chunks, tiles);
-  else
-    dropout_flat<T, RES, true><<<grid, NT, 0, s>>>(a, chunks, tiles);
-  return hipGetLastError();
+  if (!a.flat) return start(dropout_rows<T, RES>, grid, NT, 0, s, a, tiles);
+  const bool past = chunks * 8 * int64_t(sizeof(T)) >= PAST_BYTES;
+  return start(past ? dropout_flat<T, RES, true> : dropout_flat<T, RES, false>, grid, NT, 0, s, a,
+               chunks, tiles);
 }
 
 }  // namespace

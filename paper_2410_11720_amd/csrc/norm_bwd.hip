@@ -230,14 +230,11 @@ template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t
     using S = decltype(shape);
     const int grid = wgs_of(at, a.rows);
     const size_t lds = at.rows > 1 ? size_t(at.threads()) * S::NV * 32 : 0;
-    if (a.lines)
-      norm_bwd_kernel<T, S, KIND, true><<<dim3(grid), at.threads(), lds, s>>>(a, at);
-    else
-      norm_bwd_kernel<T, S, KIND, false><<<dim3(grid), at.threads(), lds, s>>>(a, at);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e =
+        start(a.lines ? norm_bwd_kernel<T, S, KIND, true> : norm_bwd_kernel<T, S, KIND, false>,
+              dim3(grid), at.threads(), lds, s, a, at);
     if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
-    norm_join_kernel<<<dim3(a.stride / JOIN_COLS), JOIN_NT, 0, s>>>(a, grid);
-    return hipGetLastError();
+    return start(norm_join_kernel, dim3(a.stride / JOIN_COLS), JOIN_NT, 0, s, a, grid);
   });
 }
 

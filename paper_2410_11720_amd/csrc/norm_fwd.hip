@@ -166,11 +166,8 @@ template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t
     constexpr int WAVES[] = {32, 20, 8};
     const int waves = at.threads() / 64, each = std::max(1, (WAVES[S::NV - 1] + waves / 2) / waves);
     const dim3 grid(int(std::min<int64_t>(wgs, 256 * each)));
-    if (a.lines)
-      norm_fwd_kernel<T, S, KIND, true><<<grid, at.threads(), 0, s>>>(a, at);
-    else
-      norm_fwd_kernel<T, S, KIND, false><<<grid, at.threads(), 0, s>>>(a, at);
-    return hipGetLastError();
+    return start(a.lines ? norm_fwd_kernel<T, S, KIND, true> : norm_fwd_kernel<T, S, KIND, false>, grid,
+                 at.threads(), 0, s, a, at);
   });
 }
 

@@ -156,15 +156,10 @@ template <typename T, int L, int U> hipError_t launch(RotaryArgs a, bool full, h
   a.waves = Divisor::of((a.items + a.per - 1) / a.per);
   const int64_t jobs = int64_t(a.n_tokens) * a.waves.d;
   const dim3 grid(int(std::min<int64_t>((jobs + NT / L - 1) / (NT / L), 1 << 20)));
-  if (a.interleaved && full)
-    rotary_kernel<T, L, U, true, true><<<grid, NT, 0, s>>>(a);
-  else if (a.interleaved)
-    rotary_kernel<T, L, U, true, false><<<grid, NT, 0, s>>>(a);
-  else if (full)
-    rotary_kernel<T, L, U, false, true><<<grid, NT, 0, s>>>(a);
-  else
-    rotary_kernel<T, L, U, false, false><<<grid, NT, 0, s>>>(a);
-  return hipGetLastError();
+  auto* kernel = a.interleaved ? full ? rotary_kernel<T, L, U, true, true> : rotary_kernel<T, L, U, true, false>
+                 : full        ? rotary_kernel<T, L, U, false, true>
+                               : rotary_kernel<T, L, U, false, false>;
+  return start(kernel, grid, NT, 0, s, a);
 }
 
 // Lanes a token: as many as it has items for (57 x 1257 tokens, three heads and three

@@ -76,6 +76,14 @@ hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
 
 #ifdef __HIPCC__
 
+// A launch without the configuration's detour through the runtime (2.2 instead of 2.5
+// us, of calls that take 8).
+template <typename... A>
+hipError_t start(void (*kernel)(A...), dim3 grid, int threads, size_t lds, hipStream_t s, A... args) {
+  void* at[] = {&args...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, lds, s);
+}
+
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // (the loads and stores below are single 16-byte ones at any alignment of the
