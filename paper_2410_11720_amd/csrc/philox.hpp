@@ -18,13 +18,21 @@ struct Philox {
   uint32_t w[4];
 };
 
+ABFT_BOTH uint32_t xor3(uint32_t x, uint32_t y, uint32_t z) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_amdgcn_bitop3_b32(x, y, z, 0x96);  // one instruction; the table of x ^ y ^ z
+#else
+  return x ^ y ^ z;
+#endif
+}
+
 ABFT_BOTH Philox philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0,
                         uint32_t k1) {
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint64_t p0 = uint64_t(0xD2511F53u) * c0, p1 = uint64_t(0xCD9E8D57u) * c2;
-    c0 = uint32_t(p1 >> 32) ^ c1 ^ k0;
-    c2 = uint32_t(p0 >> 32) ^ c3 ^ k1;
+    c0 = xor3(uint32_t(p1 >> 32), c1, k0);
+    c2 = xor3(uint32_t(p0 >> 32), c3, k1);
     c1 = uint32_t(p1);
     c3 = uint32_t(p0);
     k0 += 0x9E3779B9u;

@@ -86,6 +86,8 @@ hipError_t start(void (*kernel)(A...), dim3 grid, int threads, size_t lds, hipSt
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // (the loads and stores below are single 16-byte ones at any alignment of the
 // element: global memory is accessed unaligned on this target)
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
@@ -108,7 +110,10 @@ template <> struct Chunk<bf16_t> {
   }
   __device__ __forceinline__ void set(const float (&v)[8]) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = uint32_t(f2bf(v[2 * k])) | uint32_t(f2bf(v[2 * k + 1])) << 16;
+    for (int k = 0; k < 4; ++k) {  // (two in one conversion)
+      const f32x2 f = {v[2 * k], v[2 * k + 1]};
+      r[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+    }
   }
   __device__ __forceinline__ void put(int e, bf16_t x) {
     r[e / 2] = e % 2 ? (r[e / 2] & 0xffffu) | uint32_t(x) << 16 : (r[e / 2] & 0xffff0000u) | x;

@@ -11,11 +11,12 @@ PATH = "/opt/rocm/llvm/bin:" + os.environ.get("PATH", "")
 OBJDUMP = shutil.which("llvm-objdump", path=PATH)
 READELF = shutil.which("llvm-readelf", path=PATH)
 
-# bytes of scratch a lane: type (f: fp32, t: bf16), what stands in front of the norm, whole
-# chunks. All of rows above 8192 columns, whose lanes hold the sums of two chunks in 128
-# registers
+# backward, bytes of scratch a lane: type (f: fp32, t: bf16), what stands in front of the
+# norm, whole chunks. All of rows above 8192 columns, whose lanes hold the sums of two
+# chunks in 128 registers. Forward: the same rows in fp32 with dropout by branches
+SPILLS_FORWARD = {("f", 2, 0): 12}
 SPILLS = {("t", 0, 1): 8, ("t", 0, 0): 36, ("t", 2, 0): 52, ("f", 1, 1): 20, ("f", 1, 0): 60,
-          ("f", 2, 1): 76, ("f", 2, 0): 124}
+          ("f", 2, 1): 76, ("f", 2, 0): 136}
 
 
 @pytest.fixture(scope="module")
@@ -55,6 +56,6 @@ def test_every_form_is_there(kernels):
 
 def test_no_form_spills_but_the_widest(kernels):
     for name, dtype, numbers, scratch in kernels:
-        wide = name == "norm_bwd_kernel" and numbers[:2] == (0, 2)
-        most = SPILLS.get((dtype, *numbers[2:]), 0) if wide else 0
+        known = {"norm_bwd_kernel": SPILLS, "norm_fwd_kernel": SPILLS_FORWARD}.get(name, {})
+        most = known.get((dtype, *numbers[2:]), 0) if numbers[:2] == (0, 2) else 0
         assert scratch <= most, (name, dtype, numbers, scratch)
