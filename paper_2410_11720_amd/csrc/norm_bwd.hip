@@ -18,11 +18,12 @@ namespace {
 template <typename T, typename S, int KIND, bool LINES> struct BwdLine {
   Chunk<T> dy[S::NV], h[S::NV], dh[KIND == NORM_ALONE ? 1 : S::NV];
   float2 st;
+  bool ok;
 
   __device__ __forceinline__ void read(const NormArgs& a, const Place<T, S>& p, int row) {
     const int in = min(row, a.rows - 1);
     const RowAt at = row_at(a.tokens, in);
-    const bool ok = row < a.rows && (!a.lens || int(at.t) < a.lens[at.b]);
+    ok = row < a.rows && (!a.lens || int(at.t) < a.lens[at.b]);
     const Line<T, S, LINES> pg(a.dy, at, ok, a.cols), ph(a.h, at, ok, a.cols), pd(a.dh, at, ok, a.cols);
     st = a.stats[in];
     // (a row that is not read has 0 in dy, dh and h; its statistics may be any row's)
@@ -82,6 +83,8 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      settle<LINES>(cur.dy[j], p, j, cur.ok);
+      settle<LINES>(cur.h[j], p, j, cur.ok);
       // (what is not in the row is 0 in dy, and must not be INF in xh)
       const float from = p.has(j) ? mean : 0.f;
 #pragma unroll
@@ -107,6 +110,7 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
         cur.dy[j].anew();
         cur.h[j].anew();
       }
+      if constexpr (KIND != NORM_ALONE) settle<LINES>(cur.dh[j], p, j, cur.ok && a.dh.p);
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {

@@ -67,11 +67,13 @@ __global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (LINES ? FIVE<T> 
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      settle<LINES>(cur.x[j], p, j, cur.ok);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[j][e] = cur.x[j].get(e);
       if constexpr (KIND != NORM_ALONE) {
         if constexpr (KIND == NORM_DROPOUT)
           drop(v[j], a.drop, seed, offset, row, p.lane + j * p.lanes);
+        settle<LINES>(cur.res[j], p, j, cur.ok);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[j][e] = cur.res[j].get(e) + v[j][e];
         // the norm is that of the sum as it is stored, the one the backward and the

@@ -92,6 +92,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // element: global memory is accessed unaligned on this target)
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
+typedef u32x2 u32x2_at4 __attribute__((aligned(4)));
+typedef uint32_t u32_at2 __attribute__((aligned(2)));
 
 // Eight elements as they are stored.
 template <typename T> struct Chunk;
@@ -127,7 +130,18 @@ template <> struct Chunk<bf16_t> {
 #pragma unroll
     for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(r[k]));
   }
-  __device__ __forceinline__ bf16_t at(int e) const { return bf16_t(r[e / 2] >> (e % 2 * 16)); }
+  __device__ __forceinline__ void down(int n) {  // element e + n to e, 0 behind; n in 0 .. 7
+    u32x4 t = n & 4 ? u32x4{r[2], r[3], 0, 0} : r;
+    t = n & 2 ? u32x4{t[1], t[2], t[3], 0} : t;
+    const u32x4 next = {t[1], t[2], t[3], 0};
+    r = n & 1 ? t >> 16 | next << 16 : t;
+  }
+  // its first 4, 2 or 1 elements
+  __device__ __forceinline__ void store4(bf16_t* p) const {
+    *reinterpret_cast<u32x2_at2*>(p) = u32x2{r[0], r[1]};
+  }
+  __device__ __forceinline__ void store2(bf16_t* p) const { *reinterpret_cast<u32_at2*>(p) = r[0]; }
+  __device__ __forceinline__ void store1(bf16_t* p) const { *p = bf16_t(r[0]); }
 };
 template <> struct Chunk<float> {
   u32x4 r[2];
@@ -158,10 +172,23 @@ template <> struct Chunk<float> {
 #pragma unroll
     for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(r[k / 4][k % 4]));
   }
-  __device__ __forceinline__ float at(int e) const { return get(e); }
+  __device__ __forceinline__ void down(int n) {
+    const u32x4 z = {0, 0, 0, 0};
+    u32x4 a = n & 4 ? r[1] : r[0], b = n & 4 ? z : r[1];
+    a = n & 2 ? u32x4{a[2], a[3], b[0], b[1]} : a;
+    b = n & 2 ? u32x4{b[2], b[3], 0, 0} : b;
+    r[0] = n & 1 ? u32x4{a[1], a[2], a[3], b[0]} : a;
+    r[1] = n & 1 ? u32x4{b[1], b[2], b[3], 0} : b;
+  }
+  __device__ __forceinline__ void store4(float* p) const { *reinterpret_cast<u32x4_at4*>(p) = r[0]; }
+  __device__ __forceinline__ void store2(float* p) const {
+    *reinterpret_cast<u32x2_at4*>(p) = u32x2{r[0][0], r[0][1]};
+  }
+  __device__ __forceinline__ void store1(float* p) const { *p = __uint_as_float(r[0][0]); }
 };
 
-// The chunk at p, of which m elements are in the row (at most 0: none).
+// The chunk at p, of which m elements are in the row (at most 0: none). The loads of a
+// part are all in flight at once (the last element's in the place of those behind it).
 template <typename T>
 __device__ __forceinline__ void load_chunk(Chunk<T>& c, const T* p, int m) {
   if (m >= 8) {
@@ -169,19 +196,31 @@ __device__ __forceinline__ void load_chunk(Chunk<T>& c, const T* p, int m) {
     return;
   }
   c.clear();
+  if (m <= 0) return;
+  T t[7];
 #pragma unroll
-  for (int e = 0; e < 7; ++e)
-    if (e < m) c.put(e, p[e]);
+  for (int e = 0; e < 7; ++e) t[e] = p[min(e, m - 1)];
+#pragma unroll
+  for (int e = 0; e < 7; ++e) c.put(e, e < m ? t[e] : T(0));
 }
 template <typename T>
-__device__ __forceinline__ void store_chunk(const Chunk<T>& c, T* p, int m) {
+__device__ __forceinline__ void store_chunk(Chunk<T> c, T* p, int m) {
   if (m >= 8) {
     c.store(p);
     return;
   }
-#pragma unroll
-  for (int e = 0; e < 7; ++e)
-    if (e < m) p[e] = c.at(e);
+  if (m <= 0) return;
+  if (m & 4) {
+    c.store4(p);
+    c.down(4);
+    p += 4;
+  }
+  if (m & 2) {
+    c.store2(p);
+    c.down(2);
+    p += 2;
+  }
+  if (m & 1) c.store1(p);
 }
 
 // Where a row lies: its tensor's start plus (sequence, token).
@@ -353,13 +392,29 @@ template <typename T, typename S> struct Line<T, S, false> {
 
   __device__ __forceinline__ Line(const RowTensor& x, RowAt at, bool ok, int)
       : row(ok && x.p ? row_of<T>(x, at) : nullptr) {}
+  // One load whatever a lane has of the row: where less than a chunk is left, of the
+  // row's last eight elements. `settle` sets it right when it is used.
   __device__ __forceinline__ void load(Chunk<T>& c, const Place<T, S>& p, int j) const {
-    load_chunk(c, row + p.col(j), row ? p.cols - p.col(j) : 0);
+    const int m = row ? p.cols - p.col(j) : 0;
+    if (p.cols < 8)
+      load_chunk(c, row + p.col(j), m);
+    else if (m > 0)
+      c.load(row + p.col(j) + min(0, m - 8));
   }
   __device__ __forceinline__ void store(const Chunk<T>& c, const Place<T, S>& p, int j) const {
     store_chunk(c, row + p.col(j), row ? p.cols - p.col(j) : 0);
   }
 };
+
+// A chunk as Line::load left it, with 0 for what is not in the row.
+template <bool LINES, typename T, typename S>
+__device__ __forceinline__ void settle(Chunk<T>& c, const Place<T, S>& p, int j, bool ok) {
+  if constexpr (!LINES) {
+    const int m = p.cols - p.col(j);
+    if (!__all(m >= 8) && p.cols >= 8) c.down(max(0, min(8 - m, 7)));
+    c.keep(ok && m > 0);
+  }
+}
 
 // Sums of two values over the lanes of a row. Rows of several waves exchange their
 // waves' sums in LDS, in one of two places by turns (one barrier a sum, which all the
