@@ -145,18 +145,19 @@ int common(const attn_norm_config* c, const void* weight, const void* bias, cons
   return ABFT_OK;
 }
 
-// Whether the kernels for rows of whole chunks take these tensors.
-bool lines_ok(const NormArgs& a, const Operand* rows, int n, int es) {
-  if (a.cols % 8 || a.rows >= (1 << 28)) return false;
+// How the rows of these tensors lie.
+RowMode mode_of(const NormArgs& a, const Operand* rows, int n, int es) {
+  if (a.rows == 0 || a.rows >= (1 << 28)) return ROWS_ANY;
+  uintptr_t bits = uintptr_t(a.cols) * es;
   for (int i = 0; i < n; ++i) {
     if (!rows[i].p) continue;
-    if (reinterpret_cast<uintptr_t>(rows[i].p) % 16 || rows[i].st[0] % 16 || rows[i].st[1] % 16)
-      return false;
+    bits |= reinterpret_cast<uintptr_t>(rows[i].p) | uintptr_t(rows[i].st[0]) | uintptr_t(rows[i].st[1]);
     // (rows of less than a wave's width: 32-bit offsets from the tensor's start)
     const int64_t bytes = int64_t(rows[i].area.end - rows[i].area.at);
-    if (a.cols <= NORM_LINE_COLS && bytes > 0x7fffff00) return false;
+    if (a.cols <= NORM_LINE_COLS && bytes > 0x7fffff00) return ROWS_ANY;
   }
-  return a.cols * es % 16 == 0;
+  if (a.cols % 8 == 0 && bits % 16 == 0) return ROWS_CHUNKS;
+  return a.cols >= 8 && bits % 4 == 0 ? ROWS_WORDS : ROWS_ANY;
 }
 
 int valid_rotary(const attn_rotary_config* c) {
@@ -290,7 +291,7 @@ int attn_norm_forward(const attn_norm_config* cfg, const attn_rows* x, const att
   if (a.rows == 0) return ABFT_OK;
   a.stats = reinterpret_cast<float2*>(stats);
   const Operand rows[] = {mem[0], mem[1], mem[3], mem[4]};
-  a.lines = lines_ok(a, rows, 4, es_of(dt));
+  a.mode = mode_of(a, rows, 4, es_of(dt));
   TRY(check_device());
   CK(launch_norm_fwd(a, dt, a.drop.threshold ? NORM_DROPOUT : sum ? NORM_RESIDUAL : NORM_ALONE,
                      static_cast<hipStream_t>(stream)));
@@ -335,7 +336,7 @@ int attn_norm_backward(const attn_norm_config* cfg, const attn_rows* dy, const a
   a.stride = norm_part_stride(H);
   if (a.rows == 0 && !grads) return ABFT_OK;
   const Operand rows[] = {mem[0], mem[1], mem[5], mem[6], mem[7]};
-  a.lines = a.rows > 0 && lines_ok(a, rows, 5, es_of(dt));
+  a.mode = mode_of(a, rows, 5, es_of(dt));
   TRY(check_device());
   const bool sum = a.dres.p || a.dh.p;
   CK(launch_norm_bwd(a, dt, a.drop.threshold ? NORM_DROPOUT : sum ? NORM_RESIDUAL : NORM_ALONE,

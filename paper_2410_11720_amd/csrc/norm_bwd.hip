@@ -15,7 +15,7 @@ namespace abft {
 namespace {
 
 // A row as it is read.
-template <typename T, typename S, int KIND, bool LINES> struct BwdLine {
+template <typename T, typename S, int KIND, int MODE> struct BwdLine {
   Chunk<T> dy[S::NV], h[S::NV], dh[KIND == NORM_ALONE ? 1 : S::NV];
   float2 st;
   bool ok;
@@ -24,7 +24,7 @@ template <typename T, typename S, int KIND, bool LINES> struct BwdLine {
     const int in = min(row, a.rows - 1);
     const RowAt at = row_at(a.tokens, in);
     ok = row < a.rows && (!a.lens || int(at.t) < a.lens[at.b]);
-    const Line<T, S, LINES> pg(a.dy, at, ok, a.cols), ph(a.h, at, ok, a.cols), pd(a.dh, at, ok, a.cols);
+    const Line<T, S, MODE> pg(a.dy, at, ok, a.cols), ph(a.h, at, ok, a.cols), pd(a.dh, at, ok, a.cols);
     st = a.stats[in];
     // (a row that is not read has 0 in dy, dh and h; its statistics may be any row's)
     st.x = ok ? st.x : 0.f;
@@ -42,7 +42,7 @@ template <typename T, typename S, int KIND, bool LINES> struct BwdLine {
 // lanes of two chunks, 128 registers each: there g and xh are formed twice from what
 // was read, and only bf16 rows without a residual are read ahead (4096 x 16384, with
 // spills before: bf16 with residual and dropout 253 -> 144, fp32 alone 243 -> 162 us).
-template <typename T, typename S, int KIND, bool LINES>
+template <typename T, typename S, int KIND, int MODE>
 __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
   constexpr int NV = S::NV;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
   const int waves = shape.lanes / 64;
   const int step = gridDim.x * shape.rows;
   int row = blockIdx.x * shape.rows + p.slot, turn = 0;
-  BwdLine<T, S, KIND, LINES> cur, next;
+  BwdLine<T, S, KIND, MODE> cur, next;
   if (AHEAD && a.rows > 0) cur.read(a, p, row);
   uint64_t seed = 0, offset = 0;
   if constexpr (KIND == NORM_DROPOUT) {
@@ -76,22 +76,22 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
     else
       cur.read(a, p, row);
     const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
-    const Line<T, S, LINES> px(a.dx, at, row < a.rows, a.cols);
-    const Line<T, S, LINES> pr(a.dres, at, row < a.rows, a.cols);
+    const Line<T, S, MODE> px(a.dx, at, row < a.rows, a.cols);
+    const Line<T, S, MODE> pr(a.dres, at, row < a.rows, a.cols);
     const float mean = cur.st.x, r = cur.st.y;
     float g[WIDE ? 1 : NV][8], xh[WIDE ? 1 : NV][8];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      settle<LINES>(cur.dy[j], p, j, cur.ok);
-      settle<LINES>(cur.h[j], p, j, cur.ok);
+      settle<MODE>(cur.dy[j], p, j, cur.ok);
+      settle<MODE>(cur.h[j], p, j, cur.ok);
       // (what is not in the row is 0 in dy, and must not be INF in xh)
       const float from = p.has(j) ? mean : 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float d = cur.dy[j].get(e), gw = d * w[j][e];
         float x = (cur.h[j].get(e) - from) * r;
-        if (!LINES && p.col(j) + e >= a.cols) x = 0.f;
+        if (MODE != ROWS_CHUNKS && p.col(j) + e >= a.cols) x = 0.f;
         dw[j][e] = fmaf(d, x, dw[j][e]);
         db[j][e] += d;
         s.x += gw;
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
         cur.dy[j].anew();
         cur.h[j].anew();
       }
-      if constexpr (KIND != NORM_ALONE) settle<LINES>(cur.dh[j], p, j, cur.ok && a.dh.p);
+      if constexpr (KIND != NORM_ALONE) settle<MODE>(cur.dh[j], p, j, cur.ok && a.dh.p);
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -235,7 +235,9 @@ template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t
     const int grid = wgs_of(at, a.rows);
     const size_t lds = at.rows > 1 ? size_t(at.threads()) * S::NV * 32 : 0;
     const hipError_t e =
-        start(a.lines ? norm_bwd_kernel<T, S, KIND, true> : norm_bwd_kernel<T, S, KIND, false>,
+        start(a.mode == ROWS_CHUNKS  ? norm_bwd_kernel<T, S, KIND, ROWS_CHUNKS>
+              : a.mode == ROWS_WORDS ? norm_bwd_kernel<T, S, KIND, ROWS_WORDS>
+                                     : norm_bwd_kernel<T, S, KIND, ROWS_ANY>,
               dim3(grid), at.threads(), lds, s, a, at);
     if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
     return start(norm_join_kernel, dim3(a.stride / JOIN_COLS), JOIN_NT, 0, s, a, grid);

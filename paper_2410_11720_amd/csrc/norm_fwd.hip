@@ -13,14 +13,14 @@ namespace abft {
 namespace {
 
 // A row as it is read.
-template <typename T, typename S, int KIND, bool LINES> struct FwdLine {
+template <typename T, typename S, int KIND, int MODE> struct FwdLine {
   Chunk<T> x[S::NV], res[KIND == NORM_ALONE ? 1 : S::NV];
   bool ok;
 
   __device__ __forceinline__ void read(const NormArgs& a, const Place<T, S>& p, int row) {
     const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
     ok = row < a.rows && (!a.lens || int(at.t) < a.lens[at.b]);
-    const Line<T, S, LINES> px(a.x, at, ok, a.cols), pr(a.res, at, ok, a.cols);
+    const Line<T, S, MODE> px(a.x, at, ok, a.cols), pr(a.res, at, ok, a.cols);
 #pragma unroll
     for (int j = 0; j < S::NV; ++j) {
       px.load(x[j], p, j);
@@ -33,8 +33,8 @@ template <typename T, typename S, int KIND, bool LINES> struct FwdLine {
 // (rows of several waves in bf16: five waves a SIMD, as many as a CU is given, which 96
 // registers allow; 4096 x 5120 with residual and dropout 43 us with 104, 36 with 96)
 template <typename T> constexpr int FIVE = sizeof(T) == 2 ? 5 : 4;
-template <typename T, typename S, int KIND, bool LINES>
-__global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (LINES ? FIVE<T> : 4)) void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
+template <typename T, typename S, int KIND, int MODE>
+__global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (MODE == ROWS_CHUNKS ? FIVE<T> : 4)) void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
   constexpr int NV = S::NV;
   __shared__ float2 sh[2][16];
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (LINES ? FIVE<T> 
   const int waves = shape.lanes / 64;
   const int step = gridDim.x * shape.rows;
   int row = blockIdx.x * shape.rows + p.slot, turn = 0;
-  FwdLine<T, S, KIND, LINES> cur, next;
+  FwdLine<T, S, KIND, MODE> cur, next;
   cur.read(a, p, row);
   uint64_t seed = 0, offset = 0;
   if constexpr (KIND == NORM_DROPOUT) {
@@ -61,19 +61,19 @@ __global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (LINES ? FIVE<T> 
   for (int first = blockIdx.x * shape.rows; first < a.rows; first += step, row += step, cur = next) {
     next.read(a, p, row + step);
     const RowAt at = row_at(a.tokens, min(row, a.rows - 1));
-    const Line<T, S, LINES> py(a.y, at, row < a.rows, a.cols);
-    const Line<T, S, LINES> ph(a.h, at, row < a.rows, a.cols);
+    const Line<T, S, MODE> py(a.y, at, row < a.rows, a.cols);
+    const Line<T, S, MODE> ph(a.h, at, row < a.rows, a.cols);
     float v[NV][8];
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      settle<LINES>(cur.x[j], p, j, cur.ok);
+      settle<MODE>(cur.x[j], p, j, cur.ok);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[j][e] = cur.x[j].get(e);
       if constexpr (KIND != NORM_ALONE) {
         if constexpr (KIND == NORM_DROPOUT)
           drop(v[j], a.drop, seed, offset, row, p.lane + j * p.lanes);
-        settle<LINES>(cur.res[j], p, j, cur.ok);
+        settle<MODE>(cur.res[j], p, j, cur.ok);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[j][e] = cur.res[j].get(e) + v[j][e];
         // the norm is that of the sum as it is stored, the one the backward and the
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (LINES ? FIVE<T> 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float d = v[j][e] - mean;
-          if (!LINES && p.col(j) + e >= a.cols) d = 0.f;
+          if (MODE != ROWS_CHUNKS && p.col(j) + e >= a.cols) d = 0.f;
           t.x += d;
           t.y = fmaf(d, d, t.y);
         }
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (LINES ? FIVE<T> 
     const float r = one ? 0.f : 1.f / sqrtf(scale == 1.f ? var + a.eps : var);
     const float inv = one ? 1.f / sqrtf(a.eps) : r * scale;
     const float2 st = cur.ok ? make_float2(mean / scale, inv) : make_float2(0.f, 0.f);
-    if constexpr (LINES)
+    if constexpr (MODE != ROWS_ANY)
       __builtin_amdgcn_raw_buffer_store_b64(
           __builtin_bit_cast(u32x2, st), bytes_at(a.stats, a.stats ? a.rows * 8u : 0u),
           p.lane == 0 && row < a.rows ? row * 8u : OUTSIDE, 0, 0);
@@ -171,8 +171,10 @@ template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t
     constexpr int WAVES[] = {32, 20, 8};
     const int waves = at.threads() / 64, each = std::max(1, (WAVES[S::NV - 1] + waves / 2) / waves);
     const dim3 grid(int(std::min<int64_t>(wgs, 256 * each)));
-    return start(a.lines ? norm_fwd_kernel<T, S, KIND, true> : norm_fwd_kernel<T, S, KIND, false>, grid,
-                 at.threads(), 0, s, a, at);
+    return start(a.mode == ROWS_CHUNKS  ? norm_fwd_kernel<T, S, KIND, ROWS_CHUNKS>
+                 : a.mode == ROWS_WORDS ? norm_fwd_kernel<T, S, KIND, ROWS_WORDS>
+                                        : norm_fwd_kernel<T, S, KIND, ROWS_ANY>,
+                 grid, at.threads(), 0, s, a, at);
   });
 }
 

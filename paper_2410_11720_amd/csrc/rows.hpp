@@ -45,10 +45,13 @@ struct NormArgs {
   float* dweight = nullptr;
   float* dbias = nullptr;
   int32_t stride = 0;
-  // whether every row is whole chunks at multiples of 16 bytes, tensors of rows
-  // below a wave's width are below 2 GiB, and statistics too
-  int32_t lines = 0;
+  int32_t mode = 0;            // ROWS_...
 };
+
+// How rows lie: of whole chunks at multiples of 16 bytes; of at least a chunk at
+// multiples of 4; any other. For the first two, tensors of rows below a wave's width are
+// below 2 GiB, and statistics too.
+enum RowMode { ROWS_ANY = 0, ROWS_CHUNKS = 1, ROWS_WORDS = 2 };
 
 struct DropoutArgs {
   RowTensor x, res, y;         // res may be null
@@ -295,14 +298,16 @@ __device__ __forceinline__ void load_params(float (&v)[8], const void* p, int bf
 }
 
 // ---- rows by their lanes -------------------------------------------------------------
-// Rows of whole chunks at multiples of 16 bytes (LINES) are read and written through
-// buffer descriptors, which bring 0 from outside of their bytes and drop what is
-// stored there: a lane without a chunk, a row behind a sequence's length or behind
-// the last one, a tensor that is not given need no branch. With branches around them
-// the compiler cannot count what is in flight, and waits for the next row's loads and
-// for all stores where it needs this row's (norm of 8192 x 768: forward 8.2 -> 7.4
-// us). Other rows take those branches; what lies where and the order of sums are the
-// same, and so are the results' bits.
+// Rows at multiples of 4 bytes are read and written through buffer descriptors, which
+// bring 0 from outside of their bytes and drop what is stored there: a lane without a
+// chunk, a row behind a sequence's length or behind the last one, a tensor that is not
+// given need no branch. With branches around them the compiler cannot count what is in
+// flight, and waits for the next row's loads and for all stores where it needs this
+// row's (norm of 8192 x 768: forward 8.2 -> 7.4 us). Rows of bf16 at odd elements take
+// those branches (14500 x 1092 with residual and dropout: WORDS_US us, by branches 55). What
+// lies where and the order of sums are the same, and so are the results' bits.
+// Where less than a chunk is left of a row, its lane reads the row's last eight elements
+// and `settle` moves what is its own to the front.
 
 constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset behind every descriptor's bytes
 
@@ -324,6 +329,23 @@ __device__ __forceinline__ void store_at(const Chunk<float>& c, __amdgpu_buffer_
                                          uint32_t off) {
   __builtin_amdgcn_raw_buffer_store_b128(c.r[0], b, off, 0, 0);
   __builtin_amdgcn_raw_buffer_store_b128(c.r[1], b, off + 16, 0, 0);
+}
+
+// its first 4, 2 or 1 elements
+__device__ __forceinline__ void store4_at(const Chunk<bf16_t>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2{c.r[0], c.r[1]}, b, off, 0, 0);
+}
+__device__ __forceinline__ void store2_at(const Chunk<bf16_t>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b32(c.r[0], b, off, 0, 0);
+}
+__device__ __forceinline__ void store4_at(const Chunk<float>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(c.r[0], b, off, 0, 0);
+}
+__device__ __forceinline__ void store2_at(const Chunk<float>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2{c.r[0][0], c.r[0][1]}, b, off, 0, 0);
+}
+__device__ __forceinline__ void store1_at(const Chunk<float>& c, __amdgpu_buffer_rsrc_t b, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b32(c.r[0][0], b, off, 0, 0);
 }
 
 // Lanes that share a row and chunks each of them holds (chunk lane + j lanes): LPR
@@ -356,12 +378,12 @@ template <typename T, typename S> struct Place {
   }
   __device__ __forceinline__ int col(int j) const { return 8 * (lane + j * lanes); }
   __device__ __forceinline__ bool has(int j) const { return off[j] != OUTSIDE; }
+  __device__ __forceinline__ int left(int j) const { return cols - col(j); }
 };
 
 // A row of x (ok false: none of it). Rows of one wave or more have a descriptor of
 // their own, of fewer lanes an offset in their tensor's (below 2 GiB).
-template <typename T, typename S, bool LINES> struct Line;
-template <typename T, typename S> struct Line<T, S, true> {
+template <typename T, typename S, int MODE> struct Line {
   static constexpr bool WAVES = S::LPR == 0 || S::LPR >= 64;
   __amdgpu_buffer_rsrc_t b;
   uint32_t row;
@@ -376,24 +398,44 @@ template <typename T, typename S> struct Line<T, S, true> {
       row = ok ? at.b * uint32_t(x.b) + at.t * uint32_t(x.t) : OUTSIDE;
     }
   }
-  __device__ __forceinline__ uint32_t at(const Place<T, S>& p, int j) const {
-    if constexpr (WAVES) return p.off[j];
-    return p.has(j) && row != OUTSIDE ? p.off[j] + row : OUTSIDE;
+  __device__ __forceinline__ uint32_t at(uint32_t off) const {
+    if constexpr (WAVES) return off;
+    return off != OUTSIDE && row != OUTSIDE ? off + row : OUTSIDE;
   }
   __device__ __forceinline__ void load(Chunk<T>& c, const Place<T, S>& p, int j) const {
-    load_at(c, b, at(p, j));
+    uint32_t off = p.off[j];
+    if constexpr (MODE == ROWS_WORDS)
+      off = p.has(j) ? min(off, uint32_t(p.cols - 8) * uint32_t(sizeof(T))) : OUTSIDE;
+    load_at(c, b, at(off));
   }
   __device__ __forceinline__ void store(const Chunk<T>& c, const Place<T, S>& p, int j) const {
-    store_at(c, b, at(p, j));
+    if constexpr (MODE == ROWS_CHUNKS) {
+      store_at(c, b, at(p.off[j]));
+    } else {
+      const int m = p.left(j);
+      uint32_t off = p.off[j];
+      store_at(c, b, at(m >= 8 ? off : OUTSIDE));
+      if (__all(m >= 8 || m <= 0)) return;
+      // (four, two and one of the elements that are left, if these are)
+      const bool part = m > 0 && m < 8;
+      Chunk<T> t = c;
+      store4_at(t, b, at(part && (m & 4) ? off : OUTSIDE));
+      off += m & 4 ? 4 * sizeof(T) : 0;
+      t.down(m & 4);
+      store2_at(t, b, at(part && (m & 2) ? off : OUTSIDE));
+      if constexpr (sizeof(T) == 4) {
+        off += m & 2 ? 2 * sizeof(T) : 0;
+        t.down(m & 2);
+        store1_at(t, b, at(part && (m & 1) ? off : OUTSIDE));
+      }
+    }
   }
 };
-template <typename T, typename S> struct Line<T, S, false> {
+template <typename T, typename S> struct Line<T, S, ROWS_ANY> {
   T* row;
 
   __device__ __forceinline__ Line(const RowTensor& x, RowAt at, bool ok, int)
       : row(ok && x.p ? row_of<T>(x, at) : nullptr) {}
-  // One load whatever a lane has of the row: where less than a chunk is left, of the
-  // row's last eight elements. `settle` sets it right when it is used.
   __device__ __forceinline__ void load(Chunk<T>& c, const Place<T, S>& p, int j) const {
     const int m = row ? p.cols - p.col(j) : 0;
     if (p.cols < 8)
@@ -407,12 +449,12 @@ template <typename T, typename S> struct Line<T, S, false> {
 };
 
 // A chunk as Line::load left it, with 0 for what is not in the row.
-template <bool LINES, typename T, typename S>
+template <int MODE, typename T, typename S>
 __device__ __forceinline__ void settle(Chunk<T>& c, const Place<T, S>& p, int j, bool ok) {
-  if constexpr (!LINES) {
-    const int m = p.cols - p.col(j);
+  if constexpr (MODE != ROWS_CHUNKS) {
+    const int m = p.left(j);
     if (!__all(m >= 8) && p.cols >= 8) c.down(max(0, min(8 - m, 7)));
-    c.keep(ok && m > 0);
+    if constexpr (MODE == ROWS_ANY) c.keep(ok && m > 0);
   }
 }
 

@@ -11,12 +11,13 @@ PATH = "/opt/rocm/llvm/bin:" + os.environ.get("PATH", "")
 OBJDUMP = shutil.which("llvm-objdump", path=PATH)
 READELF = shutil.which("llvm-readelf", path=PATH)
 
-# backward, bytes of scratch a lane: type (f: fp32, t: bf16), what stands in front of the
-# norm, whole chunks. All of rows above 8192 columns, whose lanes hold the sums of two
-# chunks in 128 registers. Forward: the same rows in fp32 with dropout by branches
-SPILLS_FORWARD = {("f", 2, 0): 12}
-SPILLS = {("t", 0, 1): 8, ("t", 0, 0): 36, ("t", 2, 0): 52, ("f", 1, 1): 20, ("f", 1, 0): 60,
-          ("f", 2, 1): 76, ("f", 2, 0): 136}
+# bytes of scratch a lane: type (f: fp32, t: bf16), what stands in front of the norm, how
+# rows lie (1: whole chunks). All of rows above 8192 columns, whose lanes hold the sums of
+# two chunks in 128 registers; forward, the same rows in fp32 with dropout
+SPILLS_FORWARD = {("f", 2, 2): 24}
+SPILLS = {("t", 0, 1): 8, ("t", 0, 2): 56, ("t", 0, 0): 52, ("t", 1, 2): 20, ("t", 1, 0): 40,
+          ("t", 2, 2): 68, ("t", 2, 0): 140, ("f", 0, 2): 12, ("f", 0, 0): 72, ("f", 1, 1): 20,
+          ("f", 1, 2): 132, ("f", 1, 0): 160, ("f", 2, 1): 76, ("f", 2, 2): 180, ("f", 2, 0): 216}
 
 
 @pytest.fixture(scope="module")
@@ -47,8 +48,8 @@ def kernels(tmp_path_factory):
 
 def test_every_form_is_there(kernels):
     count = lambda name: sum(k[0] == name for k in kernels)
-    # (seven widths, three things in front, whole chunks or not, two types)
-    assert count("norm_fwd_kernel") == count("norm_bwd_kernel") == 7 * 3 * 2 * 2
+    # (seven widths, three things in front, three ways of rows, two types)
+    assert count("norm_fwd_kernel") == count("norm_bwd_kernel") == 7 * 3 * 3 * 2
     assert count("norm_join_kernel") == 1
     assert (count("dropout_flat"), count("dropout_rows")) == (8, 4)
     assert count("rotary_kernel") == 4 * 2 * 2 * 2

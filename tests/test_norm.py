@@ -245,10 +245,12 @@ def test_without_parameters_and_results_left_out(dtype, cols):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("cols", [5, 64, 129, 768, 2000])
-def test_strides_and_alignment(dtype, cols):
-    """Views with gaps between rows and sequences, at odd elements; what lies between
-    the rows of a result stays as it is."""
+@pytest.mark.parametrize("cols", [5, 64, 129, 130, 768, 998, 2000, 9002])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_strides_and_alignment(dtype, cols, odd):
+    """Views with gaps between rows and sequences, at odd elements and at even ones;
+    what lies between the rows of a result stays as it is, and the results' bits are those
+    of rows without gaps."""
     cfg = abft.NormConfig(3, 4, cols, dtype=dtype)
     d = _inputs(cfg, 8)
     op = abft.LayerNorm(cfg)
@@ -256,9 +258,10 @@ def test_strides_and_alignment(dtype, cols):
     want = op.backward(d["dy"], d["x"], d["w"])
 
     def view(t, swap):
-        """A copy of t with cols + 3 (and, exchanged, sequences inside tokens)."""
-        shape = (5, 6, cols + 3) if not swap else (6, 5, cols + 3)
-        big = torch.full((1 + math.prod(shape),), 3.0, dtype=t.dtype, device="cuda")[1:].view(shape)
+        """A copy of t with wider rows (and, exchanged, sequences inside tokens)."""
+        wide = cols + 4 - (cols + odd) % 2
+        shape = (5, 6, wide) if not swap else (6, 5, wide)
+        big = torch.full((odd + math.prod(shape),), 3.0, dtype=t.dtype, device="cuda")[odd:].view(shape)
         v = big[:3, 1:5, 2:2 + cols] if not swap else big.transpose(0, 1)[:3, 1:5, 2:2 + cols]
         v.copy_(t)
         return big, v
