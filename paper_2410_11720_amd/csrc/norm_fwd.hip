@@ -34,7 +34,9 @@ template <typename T, typename S, int KIND, int MODE> struct FwdLine {
 // registers allow; 4096 x 5120 with residual and dropout 43 us with 104, 36 with 96)
 template <typename T> constexpr int FIVE = sizeof(T) == 2 ? 5 : 4;
 template <typename T, typename S, int KIND, int MODE>
-__global__ __launch_bounds__(S::LPR ? 256 : 1024, S::LPR ? 1 : (MODE == ROWS_CHUNKS ? FIVE<T> : 4)) void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
+__global__ __launch_bounds__(S::LPR ? 256 : 1024,
+                             S::LPR ? 1 : (MODE == ROWS_CHUNKS ? FIVE<T> : 4))
+void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
   constexpr int NV = S::NV;
   __shared__ float2 sh[2][16];
