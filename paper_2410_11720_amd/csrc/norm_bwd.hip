@@ -4,8 +4,8 @@
 // over rows. A workgroup takes rows in turn, holds its columns' sums over them in
 // registers and leaves them in the workspace; a second launch joins the
 // workgroups' sums in one order (no atomics: results do not depend on
-// scheduling). Bound by memory (bf16, alone: 8192 x 768 10.5 us, 3.6 TB/s; 4096 x 4096
-// 24.6 us, 4.1 TB/s; with residual and dropout 4096 x 5120 45 us, 4.7 TB/s; the join 2 to 4
+// scheduling). Bound by memory (bf16, alone: 8192 x 768 11.0 us, 3.4 TB/s; 4096 x 4096
+// 21.2 us, 4.7 TB/s; with residual and dropout 4096 x 5120 45.6 us, 4.6 TB/s; the join 2 to 5
 // us. Two rows read ahead gain nothing: 10.4 -> 11, 24.6 -> 25.7 us).
 #include <algorithm>
 
@@ -41,7 +41,7 @@ template <typename T, typename S, int KIND, int MODE> struct BwdLine {
 // The row after the present one is read ahead. Rows above 8192 columns take up to 1024
 // lanes of two chunks, 128 registers each: there g and xh are formed twice from what
 // was read, and only bf16 rows without a residual are read ahead (4096 x 16384, with
-// spills before: bf16 with residual and dropout 253 -> 144, fp32 alone 243 -> 162 us).
+// spills before: bf16 with residual and dropout 253 -> 143, fp32 alone 243 -> 162 us).
 template <typename T, typename S, int KIND, int MODE>
 __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)

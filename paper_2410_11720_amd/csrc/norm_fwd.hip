@@ -3,7 +3,7 @@
 //   h = round(residual + dropout(x)) (or x), y = (h - mean) / sqrt(var + eps) w + b
 // A row is held in the registers of LPR lanes from its one reading to its one
 // writing; mean and variance are two sums over them. Bound by memory (bf16, alone: 8192
-// x 768 7.5 us, 3.4 TB/s; 4096 x 4096 14.9 us, 4.5 TB/s; with residual and dropout 4096 x
+// x 768 8.1 us, 3.1 TB/s; 4096 x 4096 15.3 us, 4.4 TB/s; with residual and dropout 4096 x
 // 5120 36 us, 4.7 TB/s).
 #include <algorithm>
 
