@@ -119,14 +119,20 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
         o[e] = r * fmaf(-x, c2, gw - c1);
         if constexpr (KIND != NORM_ALONE) o[e] += cur.dh[j].get(e);
       }
+      // (a row that is not read has 0 in g only if the gain is finite: it is cleared)
       Chunk<T> c;
-      if constexpr (KIND != NORM_ALONE) {
-        c.set(o);
-        pr.store(c, p, j);
-      }
-      if constexpr (KIND == NORM_DROPOUT)
+      c.set(o);
+      if (!cur.ok) c.clear();
+      if constexpr (KIND != NORM_ALONE) pr.store(c, p, j);
+      if constexpr (KIND == NORM_DROPOUT) {
+        // (in fp32 of what is stored: 4 bytes less of scratch in the widest form)
+        if constexpr (sizeof(T) == 4)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = c.get(e);
         drop(o, a.drop, seed, offset, row, p.lane + j * p.lanes);
-      if constexpr (KIND != NORM_RESIDUAL) c.set(o);
+        c.set(o);
+        if (sizeof(T) == 2 && !cur.ok) c.clear();
+      }
       px.store(c, p, j);
     }
     if constexpr (AHEAD) cur = next;

@@ -675,3 +675,36 @@ def test_accuracy_over_whole_tensors(dtype, most):
     for got, ref, top in ((y, want, most), (dr, grads["dh"][0], most),
                           (dw, grads["dweight"][0], 2.0 ** -21), (db, grads["dbias"][0], 2.0 ** -21)):
         assert (got.double() - ref).norm() <= top * ref.norm()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [5, 24, 200, 768, 770, 771, 2000, 5121, 8200, 16381])
+def test_gains_that_are_not_finite_leave_rows_behind_a_sequence_zero(cols, dtype, bad):
+    """Gradients of rows behind a sequence are 0, not 0 times the gain, in each width and
+    layout of rows; what does not depend on the gain keeps its bits."""
+    shape, lens = (4, 6), [6, 0, 2, 5]
+    for p in (None, 0.0, 0.3):
+        cfg = abft.NormConfig(*shape, cols, dtype=dtype, dropout=p or 0.0)
+        print(f"[case] gain {bad} {cfg}", flush=True)
+        d = _inputs(cfg, 40, lens)
+        w = d["w"].clone()
+        w[cols // 2], w[-1] = bad, 1.0 if cols > 8 else bad
+        runs = []
+        for gain in (d["w"], w):
+            if p is None:
+                op = abft.LayerNorm(cfg)
+                y = op.forward(d["x"], gain, d["b"], lens=d["lens"])
+                dx, dw, db = op.backward(d["dy"], d["x"], gain, lens=d["lens"])
+                rows, kept = (y, dx), (dw, db)
+            else:
+                op = abft.ResidualNorm(cfg)
+                h, y = op.forward(d["x"], d["res"], gain, d["b"], rng=d["rng"], lens=d["lens"])
+                dx, dr, dw, db = op.backward(d["dy"], h, gain, dh=d["dh"], rng=d["rng"], lens=d["lens"])
+                rows, kept = (h, y, dx, dr), (h, dw, db)
+            runs.append(kept)
+            behind = ~R.valid_rows((*shape, cols), d["lens"])[..., 0]
+            for t in rows:
+                assert (t[behind] == 0).all()
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
