@@ -29,13 +29,20 @@ template <typename T, typename S, int KIND, int MODE> struct FwdLine {
   }
 };
 
+// A value that a wave's lanes share, in a scalar register.
+template <typename S> __device__ __forceinline__ float scalar(float x) {
+  if constexpr (S::LPR == 0 || S::LPR >= 64)
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+  return x;
+}
+
 // The row after the present one is read ahead.
-// (rows of several waves in bf16: five waves a SIMD, as many as a CU is given, which 96
-// registers allow; 4096 x 5120 with residual and dropout 43 us with 104, 36 with 96)
+// (rows of several waves in bf16, or alone: five waves a SIMD, as many as a CU is given,
+// which 96 registers allow; 4096 x 5120 with residual and dropout 43 us with 104, 36 with 96)
 template <typename T> constexpr int FIVE = sizeof(T) == 2 ? 5 : 4;
 template <typename T, typename S, int KIND, int MODE>
 __global__ __launch_bounds__(S::LPR ? 256 : 1024,
-                             S::LPR ? 1 : (MODE == ROWS_CHUNKS ? FIVE<T> : 4))
+                             S::LPR ? 1 : (MODE == ROWS_CHUNKS ? FIVE<T> : KIND == NORM_ALONE ? 5 : 4))
 void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
   constexpr int NV = S::NV;
@@ -89,10 +96,13 @@ void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) s.x += v[j][e];
     }
-    // Mean and variance. The first mean's rounding is taken off both by the sum of
-    // the differences (a row of one large value has variance 0). Where the squares
-    // pass fp32's range the row is scaled by 2^-80 and summed again.
-    float mean, var, scale = 1.f;
+    // Mean and variance. The first mean's rounding is taken off both by the sum of the
+    // differences. Where its square is above what that leaves of the variance, too few
+    // bits are left: the row is taken less the corrected mean (a difference without
+    // rounding, as its elements are then close to it; 0 throughout for a row of one value)
+    // and summed again, once. Where the squares pass fp32's range the row is scaled by
+    // 2^-80 and summed again.
+    float mean, var, scale = 1.f, base = 0.f, by = 0.f;
     while (true) {
       mean = line_sum<S>(s, sh, waves, p.slot, turn).x * inv_n;
       s = make_float2(0.f, 0.f);
@@ -112,26 +122,33 @@ void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
       s = line_sum<S>(s, sh, waves, p.slot, turn);
       const float more = s.x * inv_n;
       var = fmaxf(fmaf(-more, more, s.y * inv_n), 0.f);
+      float less = 0.f;
       if (is_finite(s.y) || scale != 1.f) {
         mean += more;
         if (is_nan(s.y)) var = s.y;  // (fmaxf takes the number)
-        break;
+        if (by == 1.f || !(more * more > (scale == 1.f ? var + a.eps : var))) break;
+        base = less = scalar<S>(mean);
+        by = 1.f;
+      } else {
+        by = 0x1p-80f;
       }
-      scale = 0x1p-80f;
+      scale *= by;
       s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          v[j][e] *= scale;
+          float d = v[j][e] - less;
+          if (MODE != ROWS_CHUNKS && p.col(j) + e >= a.cols) d = 0.f;
+          v[j][e] = p.has(j) ? d * by : 0.f;
           s.x += v[j][e];
         }
     }
     // (a scaled row has a variance far above eps, or is one value throughout: 0 there)
     const bool one = scale != 1.f && var == 0.f;
-    const float r = one ? 0.f : 1.f / sqrtf(scale == 1.f ? var + a.eps : var);
-    const float inv = one ? 1.f / sqrtf(a.eps) : r * scale;
-    const float2 st = cur.ok ? make_float2(mean / scale, inv) : make_float2(0.f, 0.f);
+    const float r = 1.f / sqrtf(scale == 1.f || one ? var + a.eps : var);
+    const float2 st = cur.ok ? make_float2((base + mean) * (scale == 1.f ? 1.f : 0x1p80f), one ? r : r * scale)
+                             : make_float2(0.f, 0.f);
     if constexpr (MODE != ROWS_ANY)
       __builtin_amdgcn_raw_buffer_store_b64(
           __builtin_bit_cast(u32x2, st), bytes_at(a.stats, a.stats ? a.rows * 8u : 0u),

@@ -708,3 +708,54 @@ def test_gains_that_are_not_finite_leave_rows_behind_a_sequence_zero(cols, dtype
             for t in rows:
                 assert (t[behind] == 0).all()
         assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [5, 61, 107, 242, 474, 752, 887, 1090, 3001, 11000])
+def test_each_row_of_a_value_of_its_own(cols, dtype):
+    """Rows of one value, from 1 to 2^125: the mean is that value, 1 / deviation is 1 /
+    sqrt(eps), however the sums round. The variance is a difference of two sums over the
+    distance to the first mean, whose square is at most variance + eps: (K + 4) roundings of
+    each, half of that in the root, and three more; y is the offset, and the gradient is
+    that of deviation sqrt(eps)."""
+    cfg = abft.NormConfig(1, 2000, cols, dtype=dtype)
+    d = _inputs(cfg, 41)
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    value = torch.exp2(125 * torch.rand(2000, generator=gen, device="cuda"))
+    value[:6] = torch.tensor([191323200.0, 19710781440.0, 15300820992.0, 1.83e20, -1e8, 3e9])
+    value = value.to(DT[dtype])
+    x = value.view(1, -1, 1).expand_as(d["x"]).contiguous()
+    op = abft.LayerNorm(cfg)
+    y = op.forward(x, d["w"], d["b"])
+    mean, inv = op.stats.double().unbind(dim=2)
+    assert torch.equal(mean[0], value.double())
+    want = 1 / math.sqrt(cfg.eps)
+    assert ((inv - want).abs() <= (R.K + 8) * R.U * want).all(), (inv.min(), inv.max())
+    assert torch.equal(y, d["b"].to(x.dtype).expand_as(x).contiguous())
+    dx, dw, db = op.backward(d["dy"], x, d["w"])
+    g = d["dy"].double() * d["w"].double()
+    ref = (g - g.mean(dim=2, keepdim=True)) * want
+    size = g.abs() + g.abs().mean(dim=2, keepdim=True)
+    R.check("dx", dx, ref, R.stored(ref, (2 * R.K + 16) * R.U * size * want, x.dtype))
+    assert (dw == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [8, 61, 242, 752, 1090, 3001, 11000])
+def test_rows_of_two_neighbouring_values(cols):
+    """fp32 values v and the next one: the deviation is a part of the values' last place.
+    The square of the mean's last correction is at most the variance, so this is a
+    difference of at most three to one: 1.5 (K + 4) roundings in the root, and four."""
+    cfg = abft.NormConfig(1, 500, cols, dtype="f32")
+    gen = torch.Generator(device="cuda").manual_seed(43)
+    rand = lambda *s: torch.rand(s, generator=gen, device="cuda")
+    low = torch.exp2(30 + 80 * rand(1, 500, 1))
+    high = torch.nextafter(low, torch.full_like(low, math.inf))
+    x = torch.where(rand(1, 500, cols) < rand(1, 500, 1), high, low)
+    op = abft.LayerNorm(cfg)
+    op.forward(x)
+    inv = op.stats[..., 1].double()
+    t = x.double()
+    want = 1 / (t.var(dim=2, correction=0) + cfg.eps).sqrt()
+    assert ((inv - want).abs() <= (1.5 * (R.K + 4) + 4) * R.U * want).all()
