@@ -522,7 +522,7 @@ typedef struct {
   int32_t weight_dtype;         /* of weight and bias; their gradients are fp32   */
   uint32_t site;                /* dropout, as above: p > 0 needs a residual      */
   double  dropout;
-  double  eps;                  /* >= 1e-30                                       */
+  double  eps;                  /* 1e-30 .. 1e37                                  */
 } attn_norm_config;
 
 /* Forward.

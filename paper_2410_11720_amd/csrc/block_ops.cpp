@@ -18,6 +18,7 @@ constexpr int MAX_SITE = 65536;
 constexpr int MAX_HEAD_DIM = 512;
 constexpr int MAX_HEADS = 65536;          // of queries, keys and values together
 constexpr double MIN_EPS = 1e-30;         // squares below fp32's range stay far below it
+constexpr double MAX_EPS = 1e37;          // variances of fp32's range and it have a sum there
 constexpr int64_t MAX_EXTENT = int64_t(1) << 56;  // bytes between a dimension's ends
 
 int es_of(int dtype) { return dtype == ABFT_FP32 ? 4 : 2; }
@@ -118,7 +119,7 @@ int take_drop(double p, uint32_t site, const uint64_t* rng, DropArgs* d) {
 
 int valid_norm(const attn_norm_config* c) {
   if (!c || !dtype_ok(c->dtype) || !dtype_ok(c->weight_dtype)) return ABFT_ERR_INVALID;
-  if (!(c->eps >= MIN_EPS) || !std::isfinite(c->eps)) return ABFT_ERR_INVALID;
+  if (!(c->eps >= MIN_EPS && c->eps <= MAX_EPS)) return ABFT_ERR_INVALID;
   if (!(c->dropout >= 0.0 && c->dropout <= 1.0) || c->site >= MAX_SITE) return ABFT_ERR_INVALID;
   return sizes_ok(c->batch, c->tokens, c->cols, MAX_NORM_COLS);
 }
@@ -142,6 +143,7 @@ int common(const attn_norm_config* c, const void* weight, const void* bias, cons
   a->cols = c->cols;
   a->tokens = Divisor::of(std::max(1, c->tokens));
   a->eps = c->eps;
+  a->eps_scaled = c->eps * 0x1p-160;
   return ABFT_OK;
 }
 

@@ -126,7 +126,7 @@ void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
       if (is_finite(s.y) || scale != 1.f) {
         mean += more;
         if (is_nan(s.y)) var = s.y;  // (fmaxf takes the number)
-        if (by == 1.f || !(more * more > (scale == 1.f ? var + a.eps : var))) break;
+        if (by == 1.f || !(more * more > var + (scale == 1.f ? a.eps : a.eps_scaled))) break;
         base = less = scalar<S>(mean);
         by = 1.f;
       } else {
@@ -144,9 +144,9 @@ void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
           s.x += v[j][e];
         }
     }
-    // (a scaled row has a variance far above eps, or is one value throughout: 0 there)
+    // (a scaled row of variance 0 is one value throughout)
     const bool one = scale != 1.f && var == 0.f;
-    const float r = 1.f / sqrtf(scale == 1.f || one ? var + a.eps : var);
+    const float r = 1.f / sqrtf(var + (scale == 1.f || one ? a.eps : a.eps_scaled));
     const float2 st = cur.ok ? make_float2((base + mean) * (scale == 1.f ? 1.f : 0x1p80f), one ? r : r * scale)
                              : make_float2(0.f, 0.f);
     if constexpr (MODE != ROWS_ANY)

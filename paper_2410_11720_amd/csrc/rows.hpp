@@ -39,7 +39,7 @@ struct NormArgs {
   DropArgs drop;
   int32_t rows = 0, cols = 0;
   Divisor tokens;
-  float eps = 0.f;
+  float eps = 0.f, eps_scaled = 0.f;  // the second: of a row scaled by 2^-80
   // backward: sums of each workgroup [wgs][stride] (dweight, then dbias), joined
   float* part = nullptr;
   float* dweight = nullptr;

@@ -759,3 +759,30 @@ def test_rows_of_two_neighbouring_values(cols):
     t = x.double()
     want = 1 / (t.var(dim=2, correction=0) + cfg.eps).sqrt()
     assert ((inv - want).abs() <= (1.5 * (R.K + 4) + 4) * R.U * want).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [33, 768, 3001])
+@pytest.mark.parametrize("eps", [1e-3, 2.0 ** 100, 2.0 ** 118, 2.0 ** 122])
+def test_large_eps_beside_large_rows(cols, eps):
+    """Squares past fp32's range with an eps of their size: it counts there too."""
+    for dtype in ("bf16", "f32"):
+        cfg = abft.NormConfig(2, 9, cols, dtype=dtype, eps=eps)
+        d = _inputs(cfg, 44)
+        x = (d["x"].float() * 2.0 ** 60).to(d["x"].dtype)
+        op = abft.LayerNorm(cfg)
+        y = op.forward(x, d["w"], d["b"])
+        want, bound, saved = R.norm(x, d["w"], d["b"], cfg.eps, None, DT[dtype])
+        R.check("y", y, want, bound)
+        dx, dw, db = op.backward(d["dy"], x, d["w"])
+        grads = R.norm_backward(d["dy"], None, saved, DT[dtype])
+        R.check("dweight", dw, *grads["dweight"])
+        # (gradients of 2^-60 lie in fp32's range)
+        R.check("dx", dx, grads["dh"][0], R.stored(*grads["dh"], DT[dtype]))
+
+
+@pytest.mark.parametrize("eps", [1.1e37, 1e39, 1e300])
+def test_eps_past_the_range_of_its_sums(eps):
+    with pytest.raises(abft.AbftError):
+        abft.attn_norm_workspace_bytes(_cfg(eps=eps))
+    assert abft.attn_norm_workspace_bytes(_cfg(eps=1e37)) > 0
