@@ -926,9 +926,9 @@ class _Norm(_Op):
             raise AbftError("saved: made for another shape or device")
         return saved
 
-    def _forward(self, rows, weight, bias, lens, rng, saved, of):
+    def _forward(self, rows, weight, bias, lens, rng, saved, of, written):
         """rows: of x, residual, h, y; of: what holds the norm's rows (None: y does not
-        leave them)."""
+        leave them); written: the caller's h and y."""
         x, r, h, y = rows
         if lens is not None:
             lens = self._vector(lens, "lens", self._shape[:1], torch.int32)
@@ -936,6 +936,8 @@ class _Norm(_Op):
         stats = None
         if saved is not None:
             stats, saved._of = saved.stats.data_ptr(), None
+            if written is not None and saved is not self._saved:
+                self._gone(written)
         _check(_call(_lib.attn_norm_forward, self.device, self._c, x, r,
                      self._vector(weight, "weight", self._cols, self._wdtype),
                      self._vector(bias, "bias", self._cols, self._wdtype),
@@ -956,8 +958,9 @@ class _Norm(_Op):
                             else "backward: no forward has left its statistics")
         return saved
 
-    def _backward(self, rows, weight, lens, rng, dweight, dbias, saved):
-        """rows: of dy, dh, h, dx, dresidual."""
+    def _backward(self, rows, weight, lens, rng, dweight, dbias, saved, of, written):
+        """rows: of dy, dh, h, dx, dresidual; of: h itself; written: the caller's dx and
+        dresidual, which may be on it."""
         dy, dh, h, dx, dr = rows
         if lens is not None:
             lens = self._vector(lens, "lens", self._shape[:1], torch.int32)
@@ -975,7 +978,17 @@ class _Norm(_Op):
                      self._vector(weight, "weight", self._cols, self._wdtype), saved.stats.data_ptr(),
                      lens, rng, dx, dr, dw, db,
                      self.workspace.data_ptr(), self.workspace.numel()), "attn_norm_backward")
+        if written is not None and self._gone(written, of):
+            saved._of = None
         return dweight, dbias
+
+    def _gone(self, written, rows=None):
+        """The caller's results `written` end the object's record if they are on its rows.
+        Returns whether they are on `rows`."""
+        at = [t.data_ptr() for t in written if t is not None]
+        if self._saved is not None and self._saved._of in at:
+            self._saved._of = None
+        return rows is not None and rows.data_ptr() in at
 
 
 class LayerNorm(_Norm):
@@ -990,7 +1003,7 @@ class LayerNorm(_Norm):
     weight and bias [cols] may be None (1 and 0); lens [batch] int32: tokens of
     each sequence, behind them nothing is read and results are 0. Any strides with
     contiguous columns; results not given are laid out as torch.empty_like of x or
-    dy, and may be an input (in place; y on x leaves no record for a backward)."""
+    dy, and may be an input (in place; y or dx on x leaves no record for a backward)."""
 
     def __init__(self, cfg: NormConfig, device="cuda", training=True):
         if cfg.dropout != 0.0:
@@ -998,25 +1011,28 @@ class LayerNorm(_Norm):
         super().__init__(cfg, device, training)
 
     def forward(self, x, weight=None, bias=None, lens=None, y=None, saved=None):
+        kept, written = x, None
         if y is None:
             y = torch.empty_like(x)
             held, (x_, y_) = self._records(("x",), (x,), self._shapes, (y,))
         else:
+            written = (y,)
             held, (x_, y_) = self._records(("x", "y"), (x, y), self._shapes)
-        kept = x if y.data_ptr() != x.data_ptr() else None
-        self._forward((x_, None, None, y_), weight, bias, lens, None, saved, kept)
+            kept = x if y.data_ptr() != x.data_ptr() else None
+        self._forward((x_, None, None, y_), weight, bias, lens, None, saved, kept, written)
         return y
 
     def backward(self, dy, x, weight=None, lens=None, dx=None, dweight=None, dbias=None, saved=None):
         """dx, dweight, dbias."""
-        saved = self._of(saved, x)
+        saved, written = self._of(saved, x), None
         if dx is None:
             dx = torch.empty_like(dy)
-            held, (dy, x, o) = self._records(("dy", "x"), (dy, x), self._shapes, (dx,))
+            held, (dy, x_, o) = self._records(("dy", "x"), (dy, x), self._shapes, (dx,))
         else:
-            held, (dy, x, o) = self._records(("dy", "x", "dx"), (dy, x, dx), self._shapes)
-        dweight, dbias = self._backward((dy, None, x, o, None), weight, lens, None, dweight, dbias,
-                                        saved)
+            written = (dx,)
+            held, (dy, x_, o) = self._records(("dy", "x", "dx"), (dy, x, dx), self._shapes)
+        dweight, dbias = self._backward((dy, None, x_, o, None), weight, lens, None, dweight, dbias,
+                                        saved, x, written)
         return dx, dweight, dbias
 
 
@@ -1024,21 +1040,24 @@ class ResidualNorm(_Norm):
     """h = residual + dropout(x) as it is stored, and its layer norm y, in one pass
     each way: the same bits as Dropout and LayerNorm one after the other. Records and
     tensors as of LayerNorm (backward takes h, and raises if it is not the last
-    forward's), rng as of Dropout. In place: h on x or on the residual."""
+    forward's), rng as of Dropout. In place: h on x or on the residual; dx or dresidual on
+    h leaves no record."""
 
     def forward(self, x, residual, weight=None, bias=None, rng=None, lens=None, h=None, y=None,
                 saved=None):
         """h, y."""
         if residual is None:
             raise AbftError("residual: LayerNorm is the norm without one")
+        written = None
         if h is None and y is None:
             h, y = torch.empty_like(x), torch.empty_like(x)
             held, rows = self._records(("x", "residual"), (x, residual), self._shapes, (h, y))
         else:
+            written = (h, y)
             h = torch.empty_like(x) if h is None else h
             y = torch.empty_like(x) if y is None else y
             held, rows = self._records(("x", "residual", "h", "y"), (x, residual, h, y), self._shapes)
-        self._forward(rows, weight, bias, lens, self._state(rng, self._drops), saved, h)
+        self._forward(rows, weight, bias, lens, self._state(rng, self._drops), saved, h, written)
         return h, y
 
     def backward(self, dy, h, weight=None, dh=None, rng=None, lens=None, dx=None, dresidual=None,
@@ -1047,7 +1066,7 @@ class ResidualNorm(_Norm):
         gradient. Without dropout dx and dresidual are alike: one tensor unless both
         are given."""
         saved = self._of(saved, h)
-        drops, names = self._drops, ("dy", "dh", "h", "dx", "dresidual")
+        drops, names, written = self._drops, ("dy", "dh", "h", "dx", "dresidual"), None
         if dx is None and dresidual is None:
             dx = dresidual = torch.empty_like(dy)
             fresh = (dx,)
@@ -1056,6 +1075,7 @@ class ResidualNorm(_Norm):
                 fresh = (dx, dresidual)
             held, rows = self._records(names, (dy, dh, h), self._shapes, fresh)
         else:
+            written = (dx, dresidual)
             if dx is None:
                 dx = torch.empty_like(dy) if drops else dresidual
             if dresidual is None:
@@ -1065,7 +1085,7 @@ class ResidualNorm(_Norm):
         if len(rows) == 4:
             rows.append(None)
         dweight, dbias = self._backward(rows, weight, lens, self._state(rng, drops), dweight, dbias,
-                                        saved)
+                                        saved, h, written)
         return dx, dresidual, dweight, dbias
 
 

@@ -1,0 +1,94 @@
+"""What the classes of layer norm, dropout and rotary positions do on the host around
+their C calls, on CPU tensors: records of a forward, references, arguments. The
+library's calls are replaced by one that notes what it is given."""
+import pytest
+import torch
+
+from paper_2410_11720_amd import abft
+
+
+class Host:
+    """Stands for the device: CPU tensors are on it."""
+    index = -1
+
+    def __eq__(self, other):
+        return other == torch.device("cpu")
+
+    def __str__(self):
+        return "cpu"
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """(function, arguments) of each call of the library."""
+    made = []
+    monkeypatch.setattr(abft, "_call", lambda fn, device, *args: made.append((fn, args)) or 0)
+    return made
+
+
+def _host(kind, cfg, **kw):
+    op = kind(cfg, device="cpu", **kw)
+    op.device = Host()
+    return op
+
+
+def _rows(n=1, shape=(2, 3, 40), dtype=torch.bfloat16):
+    out = [torch.zeros(shape, dtype=dtype) for _ in range(n)]
+    return out if n > 1 else out[0]
+
+
+def _norm(kind=abft.LayerNorm, batch=2, **kw):
+    return _host(kind, abft.NormConfig(batch, 3, 40, **kw))
+
+
+def test_a_gradient_on_the_rows_leaves_no_record(calls):
+    """dx on x (on h): a further backward would read the gradient as rows."""
+    x, dy, other = _rows(3)
+    op = _norm()
+    op.forward(x)
+    op.backward(dy, x, dx=other)
+    op.backward(dy, x, dx=dy)
+    assert len(calls) == 3
+    assert op.backward(dy, x, dx=x)[0] is x
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, x)
+    saved = abft.NormSaved(op.cfg, "cpu")
+    op.forward(x, saved=saved)
+    op.backward(dy, x, dx=x, saved=saved)
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, x, saved=saved)
+    op.forward(x)
+    op.backward(dy, x)
+
+    for name in ("dx", "dresidual"):
+        op = _norm(abft.ResidualNorm, dropout=0.5)
+        rng = torch.zeros(2, dtype=torch.int64)
+        h, _ = op.forward(x, other, rng=rng)
+        op.backward(dy, h, rng=rng)
+        op.backward(dy, h, rng=rng, **{name: h})
+        with pytest.raises(abft.AbftError):
+            op.backward(dy, h, rng=rng)
+
+
+def test_results_with_another_record_on_the_rows(calls):
+    """The object's own record ends too if a call with another one writes on its rows."""
+    x, dy, other = _rows(3)
+    op = _norm()
+    for write in (lambda s: op.backward(dy, x, dx=x, saved=s), lambda s: op.forward(other, y=x, saved=s),
+                  lambda s: op.forward(x, y=x, saved=s)):
+        saved = abft.NormSaved(op.cfg, "cpu")
+        op.forward(x, saved=saved)
+        op.forward(x)
+        op.forward(x, y=other, saved=saved)
+        op.backward(dy, x)
+        write(saved)
+        with pytest.raises(abft.AbftError):
+            op.backward(dy, x)
+    op = _norm(abft.ResidualNorm)
+    for name in ("h", "y"):
+        saved = abft.NormSaved(op.cfg, "cpu")
+        h, _ = op.forward(x, other)
+        op.backward(dy, h)
+        op.forward(x, other, saved=saved, **{name: h})
+        with pytest.raises(abft.AbftError):
+            op.backward(dy, h)
