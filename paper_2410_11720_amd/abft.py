@@ -11,6 +11,7 @@ import array
 import ctypes
 import dataclasses
 import os
+import weakref
 
 import torch
 
@@ -893,7 +894,18 @@ class NormSaved:
 
     def __init__(self, cfg: NormConfig, device):
         self.stats = torch.empty((cfg.batch, cfg.tokens, 2), dtype=torch.float32, device=device)
-        self._of = None              # where the rows that they belong to are
+        self._of = None              # the rows that they belong to: storage, address, strides
+
+    def _keep(self, rows):
+        # (the storage weakly: the address alone may be another tensor's by the backward)
+        self._of = weakref.ref(rows.untyped_storage()), rows.data_ptr(), rows.stride()
+
+    def _is_of(self, rows):
+        storage, at, strides = self._of
+        if at != rows.data_ptr() or storage() is not rows.untyped_storage():
+            return False
+        return strides == rows.stride() or all(
+            a == b for a, b, n in zip(strides, rows.stride(), rows.shape) if n > 1)
 
 
 class _Norm(_Op):
@@ -944,7 +956,7 @@ class _Norm(_Op):
                      lens, rng, h, y, stats),
                "attn_norm_forward")
         if saved is not None and of is not None:
-            saved._of = of.data_ptr()
+            saved._keep(of)
 
     def _of(self, saved, h):
         """The record of the rows h."""
@@ -952,7 +964,7 @@ class _Norm(_Op):
         saved = self._saved if own else self._record(saved)
         if saved is None or self.workspace is None:
             raise AbftError("backward: made with training=False")
-        if saved._of is None or own and saved._of != h.data_ptr():
+        if saved._of is None or own and not saved._is_of(h):
             raise AbftError("backward: the rows are not those of the last forward"
                             if saved._of is not None
                             else "backward: no forward has left its statistics")
@@ -986,8 +998,9 @@ class _Norm(_Op):
         """The caller's results `written` end the object's record if they are on its rows.
         Returns whether they are on `rows`."""
         at = [t.data_ptr() for t in written if t is not None]
-        if self._saved is not None and self._saved._of in at:
-            self._saved._of = None
+        own = self._saved
+        if own is not None and own._of is not None and own._of[1] in at:
+            own._of = None
         return rows is not None and rows.data_ptr() in at
 
 
@@ -995,10 +1008,11 @@ class LayerNorm(_Norm):
     """Layer norm of rows [batch, tokens, cols]: owns the workspace of one shape
     and one record of what a forward leaves for its backward (`stats`), as
     CrossAttention does; with training=False it has neither. A forward replaces the
-    record: backward raises if x is not the last forward's. Where other forwards come
-    in between, or x has moved since, pass a record of `new_saved` to both calls as
-    `saved`; which x belongs to it is then the caller's to know. Calls run on the
-    current stream of the tensors' device.
+    record: backward raises if x is not the last forward's (its memory and layout; what
+    it holds must not have changed). Where other forwards come in between, or x has
+    moved since, pass a record of `new_saved` to both calls as `saved`; which x belongs
+    to it is then the caller's to know. Calls run on the current stream of the tensors'
+    device. Those that share workspace or record, in graphs too, must not overlap.
 
     weight and bias [cols] may be None (1 and 0); lens [batch] int32: tokens of
     each sequence, behind them nothing is read and results are 0. Any strides with

@@ -70,6 +70,43 @@ def test_a_gradient_on_the_rows_leaves_no_record(calls):
             op.backward(dy, h, rng=rng)
 
 
+def test_rows_that_took_the_place_of_others(calls):
+    """The record is of a tensor's memory and layout: not of what is at its address once
+    it is gone, nor of another view from there."""
+    import numpy as np
+    memory = np.zeros(4000, dtype=np.float32)
+    tensor = lambda: torch.from_numpy(memory)[:240].view(2, 3, 40)   # memory given out again
+    dy = torch.zeros(2, 3, 40)
+    op = _norm(dtype="f32")
+    x = tensor()
+    op.forward(x)
+    op.backward(dy, x)
+    op.backward(dy, x.detach())
+    op.backward(dy, x.view(6, 40).view(2, 3, 40))
+    saved = abft.NormSaved(op.cfg, "cpu")
+    op.forward(x, saved=saved)
+    op.forward(x)
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, x.as_strided((2, 3, 40), (120, 80, 1)))
+    del x
+    x = tensor()
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, x)
+    op.backward(dy, x, saved=saved)        # (the caller's to know)
+    view = x.view(6, 40).view(2, 3, 40)
+    op.forward(view)
+    del view                               # its memory lives on
+    op.backward(dy, x)
+
+    op = _norm(abft.ResidualNorm, dtype="f32")
+    h = tensor()
+    op.forward(x, dy, h=h, y=torch.zeros(2, 3, 40))
+    op.backward(dy, h)
+    del h
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, tensor())
+
+
 def test_results_with_another_record_on_the_rows(calls):
     """The object's own record ends too if a call with another one writes on its rows."""
     x, dy, other = _rows(3)

@@ -786,3 +786,21 @@ def test_eps_past_the_range_of_its_sums(eps):
     with pytest.raises(abft.AbftError):
         abft.attn_norm_workspace_bytes(_cfg(eps=eps))
     assert abft.attn_norm_workspace_bytes(_cfg(eps=1e37)) > 0
+
+
+@pytest.mark.gpu
+def test_rows_at_the_address_of_rows_that_are_gone():
+    """What the allocator gives out again is not the last forward's."""
+    cfg = abft.NormConfig(2, 300, 768)
+    d = _inputs(cfg, 45)
+    op, end = abft.LayerNorm(cfg), abft.ResidualNorm(cfg)
+    op.forward(d["x"], d["w"], d["b"])
+    h = end.forward(d["x"], d["res"], d["w"], d["b"])[0]
+    op.backward(d["dy"], d["x"], d["w"])
+    end.backward(d["dy"], h, d["w"])
+    del d["x"], h
+    for _ in range(4):
+        x = torch.randn((2, 300, 768), device="cuda").bfloat16()
+        for norm in (op, end):
+            with pytest.raises(abft.AbftError):
+                norm.backward(d["dy"], x, d["w"])
