@@ -1094,7 +1094,7 @@ class ResidualNorm(_Norm):
                 dx = torch.empty_like(dy) if drops else dresidual
             if dresidual is None:
                 dresidual = torch.empty_like(dy) if drops else dx
-            second = () if dresidual is dx else (dresidual,)
+            second = () if dresidual is dx and not drops else (dresidual,)
             held, rows = self._records(names, (dy, dh, h, dx, *second), self._shapes)
         if len(rows) == 4:
             rows.append(None)

@@ -107,6 +107,25 @@ def test_rows_that_took_the_place_of_others(calls):
         op.backward(dy, tensor())
 
 
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_one_tensor_for_both_gradients(monkeypatch, p):
+    """With dropout the call gets both, and refuses them."""
+    given = []
+
+    def call(fn, device, *args):
+        given.append(args)
+        return 0 if len(given) == 1 else -1
+    monkeypatch.setattr(abft, "_call", call)
+    x, dy, other = _rows(3)
+    op = _norm(abft.ResidualNorm, dropout=p)
+    rng = torch.zeros(2, dtype=torch.int64)
+    h, _ = op.forward(x, other, rng=rng)
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, h, rng=rng, dx=x, dresidual=x)
+    dx, dresidual = given[1][8:10]
+    assert dx is not None and (dresidual is not None) == (p > 0)
+
+
 def test_results_with_another_record_on_the_rows(calls):
     """The object's own record ends too if a call with another one writes on its rows."""
     x, dy, other = _rows(3)

@@ -804,3 +804,23 @@ def test_rows_at_the_address_of_rows_that_are_gone():
         for norm in (op, end):
             with pytest.raises(abft.AbftError):
                 norm.backward(d["dy"], x, d["w"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_both_gradients_in_one_tensor(p):
+    """Without dropout dx and dresidual are alike and may be one; with it they differ, and
+    one place for both is refused."""
+    cfg = abft.NormConfig(2, 5, 100, dropout=p)
+    d = _inputs(cfg, 46)
+    op = abft.ResidualNorm(cfg)
+    h, _ = op.forward(d["x"], d["res"], d["w"], d["b"], rng=d["rng"])
+    want = op.backward(d["dy"], h, d["w"], rng=d["rng"])
+    t = torch.empty_like(h)
+    if p:
+        with pytest.raises(abft.AbftError):
+            op.backward(d["dy"], h, d["w"], rng=d["rng"], dx=t, dresidual=t)
+        assert not torch.equal(want[0], want[1])
+        return
+    got = op.backward(d["dy"], h, d["w"], dx=t, dresidual=t)
+    assert got[0] is t and got[1] is t and torch.equal(t, want[0]) and torch.equal(t, want[1])
