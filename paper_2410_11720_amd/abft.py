@@ -921,6 +921,7 @@ class _Norm(_Op):
         self._dtype, self._wdtype = _DTYPES[cfg.dtype][1], _DTYPES[cfg.weight_dtype][1]
         self._shape, self._cols = (cfg.batch, cfg.tokens, cfg.cols), (cfg.cols,)
         self._shapes = (self._shape,) * 5
+        self._any = 0 not in self._shape     # (without rows all addresses are 0)
         self._drops = cfg.dropout >= 2.0 ** -17
         if training:
             self._sums = torch.empty(cfg.cols, dtype=torch.float32, device=self.device)
@@ -964,7 +965,7 @@ class _Norm(_Op):
         saved = self._saved if own else self._record(saved)
         if saved is None or self.workspace is None:
             raise AbftError("backward: made with training=False")
-        if saved._of is None or own and not saved._is_of(h):
+        if saved._of is None or own and self._any and not saved._is_of(h):
             raise AbftError("backward: the rows are not those of the last forward"
                             if saved._of is not None
                             else "backward: no forward has left its statistics")
@@ -997,7 +998,7 @@ class _Norm(_Op):
     def _gone(self, written, rows=None):
         """The caller's results `written` end the object's record if they are on its rows.
         Returns whether they are on `rows`."""
-        at = [t.data_ptr() for t in written if t is not None]
+        at = [t.data_ptr() for t in written if t is not None and self._any]
         own = self._saved
         if own is not None and own._of is not None and own._of[1] in at:
             own._of = None
@@ -1032,7 +1033,7 @@ class LayerNorm(_Norm):
         else:
             written = (y,)
             held, (x_, y_) = self._records(("x", "y"), (x, y), self._shapes)
-            kept = x if y.data_ptr() != x.data_ptr() else None
+            kept = x if not self._any or y.data_ptr() != x.data_ptr() else None
         self._forward((x_, None, None, y_), weight, bias, lens, None, saved, kept, written)
         return y
 

@@ -126,6 +126,27 @@ def test_one_tensor_for_both_gradients(monkeypatch, p):
     assert dx is not None and (dresidual is not None) == (p > 0)
 
 
+@pytest.mark.parametrize("kind", [abft.LayerNorm, abft.ResidualNorm])
+def test_no_rows_have_a_backward(calls, kind):
+    """Tensors without elements all have the address 0: none is on another."""
+    op = _norm(kind, batch=0)
+    x, dy, other = _rows(3, shape=(0, 3, 40))
+    first = (x,) if kind is abft.LayerNorm else (x, other)
+    with pytest.raises(abft.AbftError):
+        op.backward(dy, x)
+    op.forward(*first)
+    for kw in ({}, dict(dx=other), dict(dx=x)):
+        op.backward(dy, x, **kw)
+    op.forward(*first, y=x)
+    op.backward(dy, x)
+    saved = abft.NormSaved(op.cfg, "cpu")
+    op.forward(*first, y=x, saved=saved)
+    op.backward(dy, x, dx=x, saved=saved)
+    op.backward(dy, x, saved=saved)
+    op.backward(dy, x)
+    assert len(calls) == 10
+
+
 def test_results_with_another_record_on_the_rows(calls):
     """The object's own record ends too if a call with another one writes on its rows."""
     x, dy, other = _rows(3)

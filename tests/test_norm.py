@@ -824,3 +824,20 @@ def test_both_gradients_in_one_tensor(p):
         return
     got = op.backward(d["dy"], h, d["w"], dx=t, dresidual=t)
     assert got[0] is t and got[1] is t and torch.equal(t, want[0]) and torch.equal(t, want[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,tokens", [(0, 3), (2, 0), (0, 0)])
+def test_no_rows_of_a_norm_alone(batch, tokens):
+    """As of one behind a residual: gradients of nothing are 0, each time."""
+    cfg = abft.NormConfig(batch, tokens, 100)
+    d = _inputs(cfg, 47)
+    op = abft.LayerNorm(cfg)
+    op.workspace.fill_(255)
+    assert op.forward(d["x"], d["w"], d["b"]).shape == (batch, tokens, 100)
+    for out in (None, torch.empty_like(d["x"]), d["x"]):
+        dx, dw, db = op.backward(d["dy"], d["x"], d["w"], dx=out)
+        assert dx.shape == (batch, tokens, 100) and (dw == 0).all() and (db == 0).all()
+    x = d["x"]
+    assert op.forward(x, d["w"], d["b"], y=x) is x
+    assert (op.backward(d["dy"], x, d["w"])[1] == 0).all()
