@@ -758,6 +758,16 @@ def _dtype_of(name, what):
     return _DTYPES[name]
 
 
+def _fits(lo, hi, **sizes):
+    """Raises for a size that its field of the C structures would cut."""
+    for name, n in sizes.items():
+        if not lo <= n < hi:
+            raise AbftError(f"{name}: {n} is not in [{lo}, {hi})")
+
+
+_I32, _U32 = (-2 ** 31, 2 ** 31), (0, 2 ** 32)
+
+
 class _Op:
     """Marshalling that the classes below share: tensors of one type and device
     as records of address and strides."""
@@ -808,6 +818,7 @@ class _Op:
 def attn_dropout_draw(seed: int, offset: int, site: int, row: int, col: int) -> int:
     """The 16-bit draw of an element (host only): it stays if the draw is at least
     floor(65536 p + 1/2)."""
+    _fits(*_U32, site=site, row=row, col=col)
     k = _lib.attn_dropout_draw(seed % 2 ** 64, offset % 2 ** 64, site, row, col)
     if k < 0:
         raise AbftError(f"attn_dropout_draw: {strerror(k)} ({k})")
@@ -824,6 +835,8 @@ class DropoutConfig:
     site: int = 0                # tells calls that share seed and offset apart
 
     def to_c(self) -> DropoutConfigC:
+        _fits(*_I32, batch=self.batch, tokens=self.tokens, cols=self.cols)
+        _fits(*_U32, site=self.site)
         return DropoutConfigC(self.batch, self.tokens, self.cols, _dtype_of(self.dtype, "dtype")[0],
                               self.p, self.site, 0)
 
@@ -876,6 +889,8 @@ class NormConfig:
     site: int = 0
 
     def to_c(self) -> NormConfigC:
+        _fits(*_I32, batch=self.batch, tokens=self.tokens, cols=self.cols)
+        _fits(*_U32, site=self.site)
         return NormConfigC(self.batch, self.tokens, self.cols, _dtype_of(self.dtype, "dtype")[0],
                            _dtype_of(self.weight_dtype, "weight_dtype")[0], self.site, self.dropout,
                            self.eps)
@@ -1123,6 +1138,8 @@ class RotaryConfig:
     magnitude: float = 1.0
 
     def to_c(self) -> RotaryConfigC:
+        _fits(*_I32, batch=self.batch, tokens=self.tokens, heads=self.heads, kv_heads=self.kv_heads,
+              head_dim=self.head_dim, rotary_dim=self.rotary_dim)
         return RotaryConfigC(self.batch, self.tokens, self.heads, self.kv_heads or self.heads,
                              self.head_dim, self.rotary_dim or self.head_dim, int(self.interleaved),
                              _dtype_of(self.dtype, "dtype")[0], self.magnitude)
@@ -1132,6 +1149,7 @@ def attn_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str
                             factor: float = 1.0, original_len: float = 2048,
                             low_turns: float = 1.0, high_turns: float = 32.0) -> list:
     """Radians a position of each pair (host only)."""
+    _fits(*_I32, rotary_dim=rotary_dim)
     kinds = {"none": 0, "linear": 1, "parts": 2}
     if scaling not in kinds:
         raise AbftError(f"scaling: {scaling!r} is none of {sorted(kinds)}")
@@ -1193,6 +1211,8 @@ class Rotary(_Op):
         caches have no such row)."""
         qs, ks = self._q_shape, self._k_shape
         capacity = K_cache.shape[1]
+        if capacity >= 2 ** 31:
+            raise AbftError(f"K_cache: {capacity} rows, at most 2^31 - 1 are supported")
         cs = (ks[0], capacity, ks[2], ks[3])
         names, tensors = ("Q", "K", "V", "K_cache", "V_cache", "Q_out"), (Q, K, V, K_cache, V_cache)
         if Q_out is None:

@@ -169,3 +169,45 @@ def test_results_with_another_record_on_the_rows(calls):
         op.forward(x, other, saved=saved, **{name: h})
         with pytest.raises(abft.AbftError):
             op.backward(dy, h)
+
+
+FAR = 2 ** 32
+
+
+@pytest.mark.parametrize("kind,kw", [
+    (abft.NormConfig, dict(batch=FAR + 2)), (abft.NormConfig, dict(tokens=FAR + 3)),
+    (abft.NormConfig, dict(cols=FAR + 40)), (abft.NormConfig, dict(site=FAR)),
+    (abft.NormConfig, dict(site=-1)), (abft.NormConfig, dict(tokens=2 ** 31)),
+    (abft.DropoutConfig, dict(batch=FAR + 2)), (abft.DropoutConfig, dict(tokens=FAR + 3)),
+    (abft.DropoutConfig, dict(cols=FAR + 40)), (abft.DropoutConfig, dict(site=FAR + 1)),
+    (abft.RotaryConfig, dict(batch=FAR + 2)), (abft.RotaryConfig, dict(tokens=FAR + 3)),
+    (abft.RotaryConfig, dict(heads=FAR + 4)), (abft.RotaryConfig, dict(kv_heads=FAR + 4)),
+    (abft.RotaryConfig, dict(head_dim=FAR + 16)), (abft.RotaryConfig, dict(rotary_dim=FAR + 16))])
+def test_sizes_past_their_fields(kind, kw):
+    """Refused, not cut to their low 32 bits (a tensor of 2^32 + 3 rows would have three
+    of them normalised, site 2^32 the draws of site 0)."""
+    base = dict(batch=2, tokens=3)
+    base.update(dict(heads=4, head_dim=16) if kind is abft.RotaryConfig else dict(cols=40))
+    kind(**base).to_c()
+    with pytest.raises(abft.AbftError):
+        kind(**{**base, **kw}).to_c()
+
+
+def test_places_past_their_fields():
+    assert abft.attn_dropout_draw(1, 2, 3, FAR - 1, 5) >= 0
+    for site, row, col in ((FAR, 0, 0), (-1, 0, 0), (0, FAR, 0), (0, -1, 0), (0, 0, FAR), (0, 0, -8)):
+        with pytest.raises(abft.AbftError):
+            abft.attn_dropout_draw(1, 2, site, row, col)
+    with pytest.raises(abft.AbftError):
+        abft.attn_rotary_frequencies(FAR + 4)
+
+
+def test_a_cache_past_its_field(calls):
+    """A capacity of 2^32 + 4 rows is not one of four."""
+    rot = _host(abft.Rotary, abft.RotaryConfig(1, 1, 1, 2))
+    q = _rows(shape=(1, 1, 1, 2))
+    cache = q.expand(1, FAR + 4, 1, 2)
+    with pytest.raises(abft.AbftError):
+        rot.append(q, q, q, cache, cache)
+    rot.append(q, q, q, cache[:, :9], cache[:, :9])
+    assert len(calls) == 1
