@@ -1057,11 +1057,11 @@ class LayerNorm(_Norm):
         saved, written = self._of(saved, x), None
         if dx is None:
             dx = torch.empty_like(dy)
-            held, (dy, x_, o) = self._records(("dy", "x"), (dy, x), self._shapes, (dx,))
+            held, (dy_, x_, o) = self._records(("dy", "x"), (dy, x), self._shapes, (dx,))
         else:
             written = (dx,)
-            held, (dy, x_, o) = self._records(("dy", "x", "dx"), (dy, x, dx), self._shapes)
-        dweight, dbias = self._backward((dy, None, x_, o, None), weight, lens, None, dweight, dbias,
+            held, (dy_, x_, o) = self._records(("dy", "x", "dx"), (dy, x, dx), self._shapes)
+        dweight, dbias = self._backward((dy_, None, x_, o, None), weight, lens, None, dweight, dbias,
                                         saved, x, written)
         return dx, dweight, dbias
 
