@@ -768,6 +768,14 @@ def _fits(lo, hi, **sizes):
 _I32, _U32 = (-2 ** 31, 2 ** 31), (0, 2 ** 32)
 
 
+def _columns(t):
+    """A new tensor, laid out with contiguous columns if it is not (torch.empty_like of rows
+    that move on by one element is not)."""
+    if t.stride()[-1] != 1 and t.shape[-1] > 1:
+        t.as_strided_(t.shape, torch.empty(t.shape, device="meta").stride())
+    return t
+
+
 class _Op:
     """Marshalling that the classes below share: tensors of one type and device
     as records of address and strides."""
@@ -791,9 +799,12 @@ class _Op:
             fields.append(t.data_ptr())
             fields += st[:-1]
         for t in fresh:
+            st = t.stride()
+            if st[-1] != 1:
+                st = _columns(t).stride()
             at.append(8 * len(fields))
             fields.append(t.data_ptr())
-            fields += t.stride()[:-1]
+            fields += st[:-1]
         held = array.array("q", fields)
         base = held.buffer_info()[0]
         return held, [None if a is None else base + a for a in at]
@@ -847,7 +858,7 @@ class Dropout(_Op):
     int64 tensor (seed, offset) on the device, whose owner advances the offset from
     step to step; a backward takes the values that its forward had. Any strides with
     contiguous columns; results not given are laid out as torch.empty_like of x or
-    dy, and may be an input (in place). Calls run on the current stream of the
+    dy (with contiguous columns), and may be an input (in place). Calls run on the current stream of the
     tensors' device."""
 
     def __init__(self, cfg: DropoutConfig, device="cuda"):
@@ -1033,7 +1044,7 @@ class LayerNorm(_Norm):
     weight and bias [cols] may be None (1 and 0); lens [batch] int32: tokens of
     each sequence, behind them nothing is read and results are 0. Any strides with
     contiguous columns; results not given are laid out as torch.empty_like of x or
-    dy, and may be an input (in place; y or dx on x leaves no record for a backward)."""
+    dy (with contiguous columns), and may be an input (in place; y or dx on x leaves no record for a backward)."""
 
     def __init__(self, cfg: NormConfig, device="cuda", training=True):
         if cfg.dropout != 0.0:
@@ -1084,8 +1095,8 @@ class ResidualNorm(_Norm):
             held, rows = self._records(("x", "residual"), (x, residual), self._shapes, (h, y))
         else:
             written = (h, y)
-            h = torch.empty_like(x) if h is None else h
-            y = torch.empty_like(x) if y is None else y
+            h = _columns(torch.empty_like(x)) if h is None else h
+            y = _columns(torch.empty_like(x)) if y is None else y
             held, rows = self._records(("x", "residual", "h", "y"), (x, residual, h, y), self._shapes)
         self._forward(rows, weight, bias, lens, self._state(rng, self._drops), saved, h, written)
         return h, y
@@ -1107,9 +1118,9 @@ class ResidualNorm(_Norm):
         else:
             written = (dx, dresidual)
             if dx is None:
-                dx = torch.empty_like(dy) if drops else dresidual
+                dx = _columns(torch.empty_like(dy)) if drops else dresidual
             if dresidual is None:
-                dresidual = torch.empty_like(dy) if drops else dx
+                dresidual = _columns(torch.empty_like(dy)) if drops else dx
             second = () if dresidual is dx and not drops else (dresidual,)
             held, rows = self._records(names, (dy, dh, h, dx, *second), self._shapes)
         if len(rows) == 4:
@@ -1165,8 +1176,8 @@ class Rotary(_Op):
     the frequencies of one configuration on the device (`freqs`, fp64, which may be
     replaced by others). Token i of sequence b lies at position q_start[b] + i (q_start
     [batch] int32, None: 0), as CrossAttention has it. Any strides with contiguous
-    dims; results not given are laid out as torch.empty_like of Q or K, and may be Q or
-    K (in place). Calls run on the current stream of the tensors' device."""
+    dims; results not given are laid out as torch.empty_like of Q or K (with contiguous
+    dims), and may be Q or K (in place). Calls run on the current stream of the tensors' device."""
 
     def __init__(self, cfg: RotaryConfig, device="cuda"):
         self.cfg = cfg
@@ -1189,8 +1200,8 @@ class Rotary(_Op):
             Q_out, K_out = torch.empty_like(Q), torch.empty_like(K)
             held, (q, k, qo, ko) = self._records(names, (Q, K), (qs, ks), (Q_out, K_out))
         else:
-            Q_out = torch.empty_like(Q) if Q_out is None else Q_out
-            K_out = torch.empty_like(K) if K_out is None else K_out
+            Q_out = _columns(torch.empty_like(Q)) if Q_out is None else Q_out
+            K_out = _columns(torch.empty_like(K)) if K_out is None else K_out
             held, (q, k, qo, ko) = self._records(names, (Q, K, Q_out, K_out), (qs, ks, qs, ks))
         freqs, start = self._at(q_start)
         _check(_call(_lib.attn_rotary, self.device, self._c, backward, q, k, freqs, start, qo, ko),

@@ -257,3 +257,33 @@ def test_tensors_are_held_until_the_launch(monkeypatch):
         check(method, **{name + "Q": q, name + "K": k, name + "Q_out": o, name + "K_out": p}, q_start=lens)
     check(rot.append, Q=q, K=k, V=v, K_cache=o, V_cache=p, q_start=lens)
     check(rot.append, Q=q, K=k, V=v, K_cache=o, V_cache=p, q_start=lens, Q_out=q)
+
+
+def test_results_beside_overlapping_rows(calls):
+    """Rows that move on by one element (windows of one buffer): torch.empty_like of them
+    has no contiguous columns; the results have."""
+    flat = torch.zeros(4000, dtype=torch.bfloat16)
+    x = flat.as_strided((2, 3, 40), (100, 1, 1))
+    y = flat.as_strided((2, 3, 40), (1, 100, 1))
+    dy = _rows()
+    rng = torch.zeros(2, dtype=torch.int64)
+    assert torch.empty_like(x).stride(2) != 1 and torch.empty_like(y).stride(2) != 1
+    out = []
+    for t in (x, y):
+        norm, end = _norm(), _norm(abft.ResidualNorm, dropout=0.5)
+        out += [norm.forward(t), norm.backward(t, t)[0]]
+        h, n = end.forward(t, dy, rng=rng)
+        out += [h, n, *end.backward(t, h, rng=rng)[:2], *end.backward(t, h, rng=rng, dx=dy)[:2]]
+        out += [end.forward(t, dy, rng=rng, h=dy)[1], end.forward(t, dy, rng=rng, y=dy)[0]]
+        drop = _host(abft.Dropout, abft.DropoutConfig(2, 3, 40))
+        out += [drop.forward(t, rng), drop.backward(t, rng)]
+    rot = _host(abft.Rotary, abft.RotaryConfig(2, 3, 2, 40))
+    q = flat.as_strided((2, 3, 2, 40), (100, 40, 1, 1))
+    k = torch.zeros((2, 3, 2, 40), dtype=torch.bfloat16)
+    assert torch.empty_like(q).stride(3) != 1
+    out += [*rot.forward(q, k), *rot.forward(k, q), *rot.backward(q, k), rot.forward(q, k, K_out=k)[0],
+            rot.forward(k, q, Q_out=k)[1], rot.append(q, k, k, k, k)]
+    for t in out:
+        st = t.stride()
+        assert st[-1] == 1 and t.shape in (x.shape, q.shape) and t.dtype == x.dtype
+        assert t.is_contiguous() or sorted(st)[1] >= 40

@@ -841,3 +841,29 @@ def test_no_rows_of_a_norm_alone(batch, tokens):
     x = d["x"]
     assert op.forward(x, d["w"], d["b"], y=x) is x
     assert (op.backward(d["dy"], x, d["w"])[1] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("strides", [(100, 1, 1), (1, 100, 1), (1, 7, 1), (0, 1, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_are_windows_of_one_buffer(strides, dtype):
+    """Rows that overlap, one element further on: as of a copy of them."""
+    shape = (2, 3, 40)
+    gen = torch.Generator(device="cuda").manual_seed(48)
+    flat = torch.randn(500, generator=gen, device="cuda").to(DT[dtype])
+    cfg = abft.NormConfig(*shape, dtype=dtype)
+    d = _inputs(cfg, 49)
+    rng = torch.tensor(RNG, dtype=torch.int64, device="cuda")
+    runs = []
+    for t in (flat.as_strided(shape, strides), flat.as_strided(shape, strides).contiguous()):
+        op = abft.LayerNorm(cfg)
+        out = [op.forward(t, d["w"], d["b"]), *op.backward(t, t, d["w"])]
+        op = abft.ResidualNorm(abft.NormConfig(*shape, dtype=dtype, dropout=0.5))
+        h, y = op.forward(t, d["res"], d["w"], d["b"], rng=rng)
+        out += [h, y, *op.backward(t, h, d["w"], rng=rng)]
+        drop = abft.Dropout(abft.DropoutConfig(*shape, dtype=dtype, p=0.5))
+        out += [drop.forward(t, rng, residual=t), drop.backward(t, rng)]
+        rot = abft.Rotary(abft.RotaryConfig(2, 3, 1, 40, dtype=dtype))
+        out += [*rot.forward(t.unsqueeze(2), t.unsqueeze(2)), *rot.backward(t.unsqueeze(2), t.unsqueeze(2))]
+        runs.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
