@@ -287,3 +287,67 @@ def test_results_beside_overlapping_rows(calls):
         st = t.stride()
         assert st[-1] == 1 and t.shape in (x.shape, q.shape) and t.dtype == x.dtype
         assert t.is_contiguous() or sorted(st)[1] >= 40
+
+
+def _valid():
+    """A call of each method with tensors as they have to be: name -> (method, arguments)."""
+    x, r, dy, o, p = _rows(5)
+    rng, w = torch.zeros(2, dtype=torch.int64), torch.ones(40)
+    lens = torch.ones(2, dtype=torch.int32)
+    norm, end = _norm(), _norm(abft.ResidualNorm, dropout=0.5)
+    drop = _host(abft.Dropout, abft.DropoutConfig(2, 3, 40))
+    rot = _host(abft.Rotary, abft.RotaryConfig(2, 3, 4, 10, kv_heads=2))
+    norm.forward(x)
+    h, _ = end.forward(x, r, rng=rng)
+    q, k = torch.zeros((2, 3, 4, 10)).bfloat16(), torch.zeros((2, 3, 2, 10)).bfloat16()
+    cache = torch.zeros((2, 9, 2, 10)).bfloat16()
+    return {
+        "norm": (norm.forward, dict(x=x, weight=w, bias=w, lens=lens, y=o)),
+        "norm back": (norm.backward, dict(dy=dy, x=x, weight=w, lens=lens, dx=o, dweight=w, dbias=w)),
+        "end": (end.forward, dict(x=x, residual=r, weight=w, bias=w, rng=rng, lens=lens, h=o, y=p)),
+        "end back": (end.backward, dict(dy=dy, h=h, weight=w, dh=r, rng=rng, lens=lens, dx=o,
+                                        dresidual=p, dweight=w, dbias=w)),
+        "drop": (drop.forward, dict(x=x, rng=rng, residual=r, y=o)),
+        "drop back": (drop.backward, dict(dy=dy, rng=rng, dx=o)),
+        "turn": (rot.forward, dict(Q=q, K=k, q_start=lens, Q_out=q, K_out=k)),
+        "turn back": (rot.backward, dict(dQ=q, dK=k, q_start=lens, dQ_out=q, dK_out=k)),
+        "append": (rot.append, dict(Q=q, K=k, V=k, K_cache=cache, V_cache=cache, q_start=lens, Q_out=q)),
+    }
+
+
+VECTORS = ("weight", "bias", "lens", "rng", "q_start", "dweight", "dbias")
+OPTIONAL = VECTORS + ("y", "dx", "dresidual", "dh", "Q_out", "K_out", "dQ_out", "dK_out")
+
+
+@pytest.mark.parametrize("name", ["norm", "norm back", "end", "end back", "drop", "drop back", "turn",
+                                  "turn back", "append"])
+def test_each_argument_is_looked_at(calls, name):
+    """The call passes as it stands and without what is optional; each tensor of another
+    type, shape or layout is refused, before the library is called, by its name, and tensors
+    of another device are."""
+    method, given = _valid()[name]
+    made = len(calls)
+    method(**given)
+    for arg in given:
+        needed = name.startswith(("end", "drop")) and arg == "rng"
+        if arg in OPTIONAL and not needed:
+            method(**{k: v for k, v in given.items() if k != arg})
+    passed = len(calls)
+    assert passed > made
+    for arg, t in given.items():
+        wide = torch.zeros((*t.shape[:-1], 2 * t.shape[-1]), dtype=t.dtype)
+        bad = [t.half() if t.dtype != torch.int64 else t.int(), t[..., :-1], t[None], wide[..., ::2]]
+        if arg in VECTORS:
+            bad.append(torch.zeros(t.numel() + 1, dtype=t.dtype))
+        elif "cache" not in arg:
+            bad.append(torch.cat([t, t], dim=1))
+        else:
+            bad.append(torch.cat([t, t], dim=0))
+        for other in bad:
+            with pytest.raises(abft.AbftError) as e:
+                method(**{**given, arg: other})
+            assert arg in str(e.value) or "not those of the last forward" in str(e.value), (arg, other.shape)
+    method.__self__.device.index = 0
+    with pytest.raises(abft.AbftError):
+        method(**given)
+    assert len(calls) == passed
