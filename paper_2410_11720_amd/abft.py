@@ -920,18 +920,23 @@ class NormSaved:
 
     def __init__(self, cfg: NormConfig, device):
         self.stats = torch.empty((cfg.batch, cfg.tokens, 2), dtype=torch.float32, device=device)
-        self._of = None              # the rows that they belong to: storage, address, strides
+        self._of = None              # the rows that they belong to
 
-    def _keep(self, rows):
-        # (the storage weakly: the address alone may be another tensor's by the backward)
-        self._of = weakref.ref(rows.untyped_storage()), rows.data_ptr(), rows.stride()
+    def _keep(self, rows, held, at):
+        # (tensor and storage weakly: the address alone may be another tensor's by the
+        # backward; the storage for views that come and go; address and strides: held
+        # from `at` on)
+        self._of = weakref.ref(rows), weakref.ref(rows.untyped_storage()), held, at
 
     def _is_of(self, rows):
-        storage, at, strides = self._of
-        if at != rows.data_ptr() or storage() is not rows.untyped_storage():
+        tensor, storage, held, at = self._of
+        if held[at] != rows.data_ptr():
             return False
-        return strides == rows.stride() or all(
-            a == b for a, b, n in zip(strides, rows.stride(), rows.shape) if n > 1)
+        return tensor() is rows or storage() is rows.untyped_storage() and all(
+            a == b for a, b, n in zip(held[at + 1:], rows.stride(), rows.shape[:2]) if n > 1)
+
+    def _address(self):
+        return None if self._of is None else self._of[2][self._of[3]]
 
 
 class _Norm(_Op):
@@ -966,8 +971,8 @@ class _Norm(_Op):
         return saved
 
     def _forward(self, rows, weight, bias, lens, rng, saved, of, written):
-        """rows: of x, residual, h, y; of: what holds the norm's rows (None: y does not
-        leave them); written: the caller's h and y."""
+        """rows: of x, residual, h, y; of: what holds the norm's rows, and their place in
+        the records (None: y does not leave them); written: the caller's h and y."""
         x, r, h, y = rows
         if lens is not None:
             lens = self._vector(lens, "lens", self._shape[:1], torch.int32)
@@ -983,7 +988,7 @@ class _Norm(_Op):
                      lens, rng, h, y, stats),
                "attn_norm_forward")
         if saved is not None and of is not None:
-            saved._keep(of)
+            saved._keep(*of)
 
     def _of(self, saved, h):
         """The record of the rows h."""
@@ -1026,7 +1031,7 @@ class _Norm(_Op):
         Returns whether they are on `rows`."""
         at = [t.data_ptr() for t in written if t is not None and self._any]
         own = self._saved
-        if own is not None and own._of is not None and own._of[1] in at:
+        if own is not None and own._address() in at:
             own._of = None
         return rows is not None and rows.data_ptr() in at
 
@@ -1052,14 +1057,15 @@ class LayerNorm(_Norm):
         super().__init__(cfg, device, training)
 
     def forward(self, x, weight=None, bias=None, lens=None, y=None, saved=None):
-        kept, written = x, None
+        written = None
         if y is None:
             y = torch.empty_like(x)
             held, (x_, y_) = self._records(("x",), (x,), self._shapes, (y,))
+            kept = x, held, 0
         else:
             written = (y,)
             held, (x_, y_) = self._records(("x", "y"), (x, y), self._shapes)
-            kept = x if not self._any or y.data_ptr() != x.data_ptr() else None
+            kept = (x, held, 0) if not self._any or held[0] != held[3] else None
         self._forward((x_, None, None, y_), weight, bias, lens, None, saved, kept, written)
         return y
 
@@ -1098,7 +1104,8 @@ class ResidualNorm(_Norm):
             h = _columns(torch.empty_like(x)) if h is None else h
             y = _columns(torch.empty_like(x)) if y is None else y
             held, rows = self._records(("x", "residual", "h", "y"), (x, residual, h, y), self._shapes)
-        self._forward(rows, weight, bias, lens, self._state(rng, self._drops), saved, h, written)
+        self._forward(rows, weight, bias, lens, self._state(rng, self._drops), saved, (h, held, 6),
+                      written)
         return h, y
 
     def backward(self, dy, h, weight=None, dh=None, rng=None, lens=None, dx=None, dresidual=None,
