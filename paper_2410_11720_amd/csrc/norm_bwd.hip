@@ -4,9 +4,9 @@
 // over rows. A workgroup takes rows in turn, holds its columns' sums over them in
 // registers and leaves them in the workspace; a second launch joins the
 // workgroups' sums in one order (no atomics: results do not depend on
-// scheduling). Bound by memory (bf16, alone: 8192 x 768 11.0 us, 3.4 TB/s; 4096 x 4096
-// 21.2 us, 4.7 TB/s; with residual and dropout 4096 x 5120 45.6 us, 4.6 TB/s; the join 2 to 5
-// us. Two rows read ahead gain nothing: 10.4 -> 11, 24.6 -> 25.7 us).
+// scheduling). Bound by memory (bf16, alone: 8192 x 768 10.2 us, 3.7 TB/s; 4096 x 4096
+// 21.1 us, 4.8 TB/s; with residual and dropout 4096 x 5120 44.8 us, 4.7 TB/s; the join 3 to
+// 7.5 us).
 #include <algorithm>
 
 #include "rows.hpp"
@@ -41,7 +41,7 @@ template <typename T, typename S, int KIND, int MODE> struct BwdLine {
 // The row after the present one is read ahead. Rows above 8192 columns take up to 1024
 // lanes of two chunks, 128 registers each: there g and xh are formed twice from what
 // was read, and only bf16 rows without a residual are read ahead (4096 x 16384, with
-// spills before: bf16 with residual and dropout 253 -> 143, fp32 alone 243 -> 162 us).
+// spills before: bf16 with residual and dropout 253 -> 145, fp32 alone 243 -> 164 us).
 template <typename T, typename S, int KIND, int MODE>
 __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs a, ShapeAt shape) {
 #pragma clang fp contract(off)  // (the same bits from every form; fused where written so)
@@ -174,10 +174,15 @@ __global__ __launch_bounds__(S::LPR ? 512 : 1024) void norm_bwd_kernel(NormArgs 
   }
 }
 
+// Workgroups of the backward: each leaves sums of its own, so no more than one a CU, or
+// two small ones.
+constexpr int MOST_WGS = 256, MOST_SMALL_WGS = 512;
+
 // dweight and dbias from the workgroups' sums: 32 columns a workgroup, 8 lanes of four
-// columns each, the sums split over 128 such groups: 2 to 8 loads each, all in flight
+// columns each, the sums split over 128 such groups: at most 4 loads each, all in flight
 // at once, then joined in LDS in their order.
 constexpr int JOIN_NT = 1024, JOIN_COLS = 32, JOIN_GROUPS = JOIN_NT * 4 / JOIN_COLS;
+static_assert(MOST_SMALL_WGS <= 4 * JOIN_GROUPS, "loads of a joining group");
 
 __global__ __launch_bounds__(JOIN_NT) void norm_join_kernel(NormArgs a, int wgs) {
   __shared__ float sh[JOIN_GROUPS][JOIN_COLS], sh2[16][JOIN_COLS];
@@ -212,8 +217,8 @@ __global__ __launch_bounds__(JOIN_NT) void norm_join_kernel(NormArgs a, int wgs)
 
 // f(shape, its lanes and rows). Few chunks a lane: it holds their sums, 16 registers a
 // chunk. As many rows a workgroup as fill it: its sums are written once for all of
-// them (4096 x 4096, 512 lanes a row: two rows a workgroup 27.7, one 30.3 us with the
-// join), but no more than leave every CU a workgroup.
+// them (4096 x 4096, 512 lanes a row: two rows a workgroup 23.9, one 24.7 us with the
+// join, 8192 x 768, one row a wave, eight rows 12.8, one 19.1; calls one after another), but no more than leave every CU a workgroup.
 template <typename F> auto with_lines(int chunks, int64_t rows, F f) {
   auto at = [&](int lanes, int threads) {
     const int least = std::max(1, 64 / lanes), most = threads / lanes;
@@ -229,9 +234,8 @@ template <typename F> auto with_lines(int chunks, int64_t rows, F f) {
   return f(Shape<0, 2>(), at((chunks + 127) / 128 * 64, 1024));
 }
 
-// Workgroups: each leaves sums of its own, so no more than one a CU, or two small ones.
 int wgs_of(ShapeAt at, int64_t rows) {
-  const int64_t most = at.threads() <= 256 ? 512 : 256;
+  const int64_t most = at.threads() <= 256 ? MOST_SMALL_WGS : MOST_WGS;
   return int(std::max<int64_t>(1, std::min<int64_t>(most, (rows + at.rows - 1) / at.rows)));
 }
 

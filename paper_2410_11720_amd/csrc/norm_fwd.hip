@@ -3,8 +3,8 @@
 //   h = round(residual + dropout(x)) (or x), y = (h - mean) / sqrt(var + eps) w + b
 // A row is held in the registers of LPR lanes from its one reading to its one
 // writing; mean and variance are two sums over them. Bound by memory (bf16, alone: 8192
-// x 768 8.1 us, 3.1 TB/s; 4096 x 4096 15.3 us, 4.4 TB/s; with residual and dropout 4096 x
-// 5120 36 us, 4.7 TB/s).
+// x 768 8.2 us, 3.1 TB/s; 4096 x 4096 15.3 us, 4.4 TB/s; with residual and dropout 4096 x
+// 5120 35 us, 4.8 TB/s).
 #include <algorithm>
 
 #include "rows.hpp"
@@ -38,7 +38,8 @@ template <typename S> __device__ __forceinline__ float scalar(float x) {
 
 // The row after the present one is read ahead.
 // (rows of several waves in bf16, or alone: five waves a SIMD, as many as a CU is given,
-// which 96 registers allow; 4096 x 5120 with residual and dropout 43 us with 104, 36 with 96)
+// which 96 registers allow; 4096 x 5120 with residual and dropout 43 us with 104, 34 with
+// 96; 4096 x 8191 alone in fp32 62.0 and 61.5)
 template <typename T> constexpr int FIVE = sizeof(T) == 2 ? 5 : 4;
 template <typename T, typename S, int KIND, int MODE>
 __global__ __launch_bounds__(S::LPR ? 256 : 1024,
@@ -184,9 +185,11 @@ template <typename T, int KIND> hipError_t launch(const NormArgs& a, hipStream_t
   return with_lines((a.cols + 7) / 8, [&](auto shape, ShapeAt at) {
     using S = decltype(shape);
     const int64_t wgs = (int64_t(a.rows) + at.rows - 1) / at.rows;
-    // Waves of a CU, by what a lane holds (8192 x 768, three chunks: 8 waves 7.4, 16 7.9
-    // us; 8192 x 2048, two: 16 waves 14.8, 8 17.2 us), in whole workgroups: every CU has
-    // the same number (8192 x 11072, 11 waves a row: 512 workgroups 73.5, 465 80.8 us).
+    // Waves of a CU, by what a lane holds, in whole workgroups: every CU has the same
+    // number. Calls one after another in bf16: three chunks, 8192 x 768 with 8 waves 7.3,
+    // 16 7.5 us, with dropout 12.7 and 13.6 (32768 rows 17.9 and 16.8); two, 8192 x 11072
+    // with 20 waves 73.7, 16 82.1, 8 82.1 us, 4096 x 4096 14.8, 15.0, 17.0 (8192 x 2048
+    // 15.6, 14.5, 16.9); 11 waves a row as 512 workgroups 73.7, as 465 75.0.
     constexpr int WAVES[] = {32, 20, 8};
     const int waves = at.threads() / 64, each = std::max(1, (WAVES[S::NV - 1] + waves / 2) / waves);
     const dim3 grid(int(std::min<int64_t>(wgs, 256 * each)));
