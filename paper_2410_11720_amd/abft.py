@@ -858,8 +858,8 @@ class Dropout(_Op):
     int64 tensor (seed, offset) on the device, whose owner advances the offset from
     step to step; a backward takes the values that its forward had. Any strides with
     contiguous columns; results not given are laid out as torch.empty_like of x or
-    dy (with contiguous columns), and may be an input (in place). Calls run on the current stream of the
-    tensors' device."""
+    dy (with contiguous columns), and may be an input (in place). Calls run on the
+    current stream of the tensors' device."""
 
     def __init__(self, cfg: DropoutConfig, device="cuda"):
         self.cfg = cfg
@@ -1049,7 +1049,8 @@ class LayerNorm(_Norm):
     weight and bias [cols] may be None (1 and 0); lens [batch] int32: tokens of
     each sequence, behind them nothing is read and results are 0. Any strides with
     contiguous columns; results not given are laid out as torch.empty_like of x or
-    dy (with contiguous columns), and may be an input (in place; y or dx on x leaves no record for a backward)."""
+    dy (with contiguous columns), and may be an input (in place; y or dx on x leaves no
+    record for a backward)."""
 
     def __init__(self, cfg: NormConfig, device="cuda", training=True):
         if cfg.dropout != 0.0:
@@ -1184,7 +1185,8 @@ class Rotary(_Op):
     replaced by others). Token i of sequence b lies at position q_start[b] + i (q_start
     [batch] int32, None: 0), as CrossAttention has it. Any strides with contiguous
     dims; results not given are laid out as torch.empty_like of Q or K (with contiguous
-    dims), and may be Q or K (in place). Calls run on the current stream of the tensors' device."""
+    dims), and may be Q or K (in place). Calls run on the current stream of the tensors'
+    device."""
 
     def __init__(self, cfg: RotaryConfig, device="cuda"):
         self.cfg = cfg
