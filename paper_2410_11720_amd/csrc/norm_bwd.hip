@@ -216,9 +216,10 @@ __global__ __launch_bounds__(JOIN_NT) void norm_join_kernel(NormArgs a, int wgs)
 }
 
 // f(shape, its lanes and rows). Few chunks a lane: it holds their sums, 16 registers a
-// chunk. As many rows a workgroup as fill it: its sums are written once for all of
-// them (4096 x 4096, 512 lanes a row: two rows a workgroup 23.9, one 24.7 us with the
-// join, 8192 x 768, one row a wave, eight rows 12.8, one 19.1; calls one after another), but no more than leave every CU a workgroup.
+// chunk. As many rows a workgroup as fill it: its sums are written once for all of them
+// (calls one after another, with the join: 4096 x 4096, 512 lanes a row, two rows a
+// workgroup 23.9, one 24.7 us; 8192 x 768, a wave a row, eight rows 12.8, one 19.1), but
+// no more than leave every CU a workgroup.
 template <typename F> auto with_lines(int chunks, int64_t rows, F f) {
   auto at = [&](int lanes, int threads) {
     const int least = std::max(1, 64 / lanes), most = threads / lanes;

@@ -148,8 +148,8 @@ void norm_fwd_kernel(NormArgs a, ShapeAt shape) {
     // (a scaled row of variance 0 is one value throughout)
     const bool one = scale != 1.f && var == 0.f;
     const float r = 1.f / sqrtf(var + (scale == 1.f || one ? a.eps : a.eps_scaled));
-    const float2 st = cur.ok ? make_float2((base + mean) * (scale == 1.f ? 1.f : 0x1p80f), one ? r : r * scale)
-                             : make_float2(0.f, 0.f);
+    const float unscaled = (base + mean) * (scale == 1.f ? 1.f : 0x1p80f);
+    const float2 st = cur.ok ? make_float2(unscaled, one ? r : r * scale) : make_float2(0.f, 0.f);
     if constexpr (MODE != ROWS_ANY)
       __builtin_amdgcn_raw_buffer_store_b64(
           __builtin_bit_cast(u32x2, st), bytes_at(a.stats, a.stats ? a.rows * 8u : 0u),

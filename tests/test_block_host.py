@@ -239,7 +239,8 @@ def test_tensors_are_held_until_the_launch(monkeypatch):
     norm = _norm()
     for y in (None, a):
         check(norm.forward, x=x, weight=w, bias=w, lens=lens, y=y)
-        check(norm.backward, dy=dy, x=x, weight=w, lens=lens, dx=y, **({} if y is None else dict(dweight=w, dbias=w)))
+        sums = {} if y is None else dict(dweight=w, dbias=w)
+        check(norm.backward, dy=dy, x=x, weight=w, lens=lens, dx=y, **sums)
     end = _norm(abft.ResidualNorm, dropout=0.5)
     check(end.forward, x=x, residual=r, weight=w, bias=w, rng=rng, lens=lens)
     check(end.forward, x=x, residual=r, weight=w, bias=w, rng=rng, lens=lens, h=a, y=b)
@@ -254,7 +255,8 @@ def test_tensors_are_held_until_the_launch(monkeypatch):
     for name in ("", "d"):
         method = rot.backward if name else rot.forward
         check(method, **{name + "Q": q, name + "K": k}, q_start=lens)
-        check(method, **{name + "Q": q, name + "K": k, name + "Q_out": o, name + "K_out": p}, q_start=lens)
+        check(method, q_start=lens,
+              **{name + "Q": q, name + "K": k, name + "Q_out": o, name + "K_out": p})
     check(rot.append, Q=q, K=k, V=v, K_cache=o, V_cache=p, q_start=lens)
     check(rot.append, Q=q, K=k, V=v, K_cache=o, V_cache=p, q_start=lens, Q_out=q)
 
@@ -346,7 +348,8 @@ def test_each_argument_is_looked_at(calls, name):
         for other in bad:
             with pytest.raises(abft.AbftError) as e:
                 method(**{**given, arg: other})
-            assert arg in str(e.value) or "not those of the last forward" in str(e.value), (arg, other.shape)
+            said = str(e.value)
+            assert arg in said or "not those of the last forward" in said, (arg, other.shape)
     method.__self__.device.index = 0
     with pytest.raises(abft.AbftError):
         method(**given)
