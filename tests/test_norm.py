@@ -867,3 +867,32 @@ def test_rows_that_are_windows_of_one_buffer(strides, dtype):
         out += [*rot.forward(t.unsqueeze(2), t.unsqueeze(2)), *rot.backward(t.unsqueeze(2), t.unsqueeze(2))]
         runs.append(out)
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [5, 40, 64, 100, 128, 250, 500, 768, 1000, 3000])
+def test_rows_that_are_summed_again_beside_others(cols, dtype):
+    """Rows of one value, of squares past fp32's range and of both among ordinary ones,
+    which lanes of the same wave hold: each has the bits that it has alone."""
+    cfg = abft.NormConfig(1, 120, cols, dtype=dtype)
+    d = _inputs(cfg, 50)
+    x = d["x"].float()
+    x[:, 1::4] = 3.3e9 * (1 + torch.arange(30, device="cuda").view(1, -1, 1) / 64)
+    x[:, 2::4] *= 2.0 ** 70
+    x[:, 3::12] = 1.83e36
+    x = x.to(DT[dtype])
+    op = abft.LayerNorm(cfg)
+    y = op.forward(x, d["w"], d["b"])
+    stats, (dx, _, _) = op.stats.clone(), op.backward(d["dy"], x, d["w"])
+    for at in (slice(0, 120, 4), slice(1, 120, 4), slice(2, 120, 4), slice(3, 120, 12)):
+        n = len(range(120)[at])
+        one = abft.LayerNorm(abft.NormConfig(1, n, cols, dtype=dtype))
+        part, dy = x[:, at].contiguous(), d["dy"][:, at].contiguous()
+        assert torch.equal(one.forward(part, d["w"], d["b"]), y[:, at])
+        assert torch.equal(one.stats, stats[:, at])
+        assert torch.equal(one.backward(dy, part, d["w"])[0], dx[:, at])
+    want, bound, saved = R.norm(x, d["w"], d["b"], cfg.eps, None, DT[dtype])
+    R.check("y", y, want, bound)
+    inv = saved[2][..., 0]
+    assert ((stats[..., 1].double() - inv).abs() <= (1.5 * (R.K + 4) + 4) * R.U * inv).all()
